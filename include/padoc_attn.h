@@ -315,6 +315,144 @@ padoc_status padoc_cache_from_rows(const void* k_rows, const void* v_rows, void*
                                    int64_t num_blocks, int32_t num_heads_kv, int32_t head_dim,
                                    padoc_dtype dtype, hipStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Rotary positions and head norms: what a decoder layer does to Q and K right
+ * before the attention above (the paper's decoder rotates by several position
+ * axes: time, height and width of image tokens, one running index for text).
+ *
+ *   y  = x                                          without a weight
+ *   y  = w * x / sqrt(mean(x^2) + norm_eps)         with one (per head, over d)
+ *   pair i < rotary_dim/2 of y, members (a, b), angle t = pos[axis[i]] * inv_freq[i]:
+ *     z_a = scale * (y_a cos t - y_b sin t),  z_b = scale * (y_b cos t + y_a sin t)
+ *   every other dimension: z = y
+ *
+ * Computed in fp32 and rounded once.  Positions are int32, negative ones and
+ * ones of any size included: angles are reduced in 64-bit fixed-point turns,
+ * so they stay exact to about 1e-7 radians at every position.
+ * ------------------------------------------------------------------------- */
+typedef enum {
+  PADOC_ROTARY_HALVES = 0,  /* pair i = dimensions i and i + rotary_dim/2 */
+  PADOC_ROTARY_PAIRS = 1    /* pair i = dimensions 2i and 2i + 1          */
+} padoc_rotary_style;
+
+typedef struct {
+  int32_t head_dim;          /* 64 or 128                                     */
+  int32_t rotary_dim;        /* leading dimensions rotated: a multiple of 16,
+                                16 .. head_dim                                */
+  int32_t n_axes;            /* position axes, 1 .. 4                         */
+  int32_t style;             /* padoc_rotary_style                            */
+  const int32_t* axis;       /* [rotary_dim/2] axis of each pair; NULL: 0     */
+  const double* inv_freq;    /* [rotary_dim/2] radians per position, finite;
+                                NULL: base^(-2i/rotary_dim)                   */
+  double base;               /* > 0, finite (used when inv_freq is NULL)      */
+  float scale;               /* finite; cosines and sines are multiplied by it */
+  float norm_eps;            /* >= 0, finite                                  */
+  padoc_dtype dtype;         /* of the rows and the weights                   */
+} padoc_rotary_desc;
+
+/* Host memory only; immutable, may be shared by threads, devices and captured
+   graphs (launches copy what they need of it).  The arrays of the descriptor
+   are read during the call. */
+typedef struct padoc_rotary padoc_rotary;
+padoc_status padoc_rotary_create(const padoc_rotary_desc* desc, padoc_rotary** out);
+void padoc_rotary_destroy(padoc_rotary* rotary);
+
+/* Rows of heads in device memory: head h of row r is the head_dim contiguous
+   elements at data + r * row_stride + h * head_stride (strides in elements,
+   >= 0), as in a slice of a fused projection.  Buffers need their element's
+   alignment only; 16-byte aligned rows are the fast ones.  What is written
+   must not overlap itself, nor anything that the call reads, with one
+   exception: q and q_out (k and k_out, dq_out and dq, ...) may be the very
+   same rows. */
+typedef struct {
+  void* data;
+  int64_t row_stride, head_stride;
+} padoc_heads;
+
+/* z of n_rows rows of q (num_heads_q heads) and k (num_heads_kv), one kernel.
+   Either head count may be 0 (its pointers are not read then).  pos: device
+   int32, position of row r on axis a at pos[a * pos_stride + r].  q_weight /
+   k_weight: device, head_dim elements, or NULL.  n_rows <= 2^31-1, head counts
+   <= 4096.  Nothing is allocated; the launch may be captured. */
+typedef struct {
+  int64_t n_rows;
+  int32_t num_heads_q, num_heads_kv;
+  const int32_t* pos;
+  int64_t pos_stride;
+  padoc_heads q, k, q_out, k_out;
+  const void* q_weight;
+  const void* k_weight;
+} padoc_rotary_fwd_args;
+padoc_status padoc_rotary_fwd(const padoc_rotary* rotary, const padoc_rotary_fwd_args* args, hipStream_t stream);
+
+/* Gradients of padoc_rotary_fwd: from dq_out / dk_out (gradients of its
+   outputs) dq / dk (of its inputs) and, where the pointers are given, the
+   weights' gradients dq_weight / dk_weight: float32 [head_dim], the sum over
+   every row and head, overwritten (zero for no rows), in an order that depends
+   on the sizes alone.  q / k are the forward's inputs; they are read only
+   where there is a weight.  workspace: device, 256-byte aligned, of
+   padoc_rotary_bwd_workspace_bytes bytes; needed (else ignored) when a
+   weight's gradient is asked for.  One kernel, and one more that adds up the
+   weights' gradients. */
+typedef struct {
+  int64_t n_rows;
+  int32_t num_heads_q, num_heads_kv;
+  const int32_t* pos;
+  int64_t pos_stride;
+  padoc_heads q, k, dq_out, dk_out, dq, dk;
+  const void* q_weight;
+  const void* k_weight;
+  float* dq_weight;
+  float* dk_weight;
+} padoc_rotary_bwd_args;
+padoc_status padoc_rotary_bwd_workspace_bytes(const padoc_rotary* rotary, int64_t n_rows, int32_t num_heads_q,
+                                              int32_t num_heads_kv, size_t* bytes);
+padoc_status padoc_rotary_bwd(const padoc_rotary* rotary, const padoc_rotary_bwd_args* args, void* workspace,
+                              size_t workspace_bytes, hipStream_t stream);
+
+/* A decode step's new rows, one kernel: z of n_q rows of q into q_out (the
+   queries of padoc_branch_decode), z of n_new rows of k into the K cache and
+   the rows of v as they are into the V cache (the paged layouts at the top of
+   this file).  slots: device int32 pairs (block id, slot) of each new row; a
+   row whose block id is outside [0, num_blocks) or whose slot is outside
+   [0, 16) is left out (padding), no two rows may name the same slot, and
+   nothing else in the caches is written.  pos as in padoc_rotary_fwd for the
+   new rows, q_pos for the queries' rows (NULL: pos, with n_q == n_new).  v is
+   read only (its row or head stride may be 0).  Nothing is allocated; the
+   launch may be captured. */
+typedef struct {
+  int64_t n_q, n_new;
+  int32_t num_heads_q, num_heads_kv;
+  const int32_t* q_pos;
+  int64_t q_pos_stride;
+  const int32_t* pos;
+  int64_t pos_stride;
+  padoc_heads q, k, v, q_out;
+  const void* q_weight;
+  const void* k_weight;
+  const int32_t* slots;
+  void* k_cache;
+  void* v_cache;
+  int64_t num_blocks;
+} padoc_rotary_append_args;
+padoc_status padoc_rotary_append(const padoc_rotary* rotary, const padoc_rotary_append_args* args,
+                                 hipStream_t stream);
+
+/* Copy whole blocks of paged K/V caches, one kernel: pair i of `pairs`
+   (device int32 [n_pairs][2]) copies block pairs[i][0] of k_src / v_src to
+   block pairs[i][1] of k_dst / v_dst.  Source and destination caches may be
+   the same buffers; then no block may be both a source and a destination.  No
+   destination may appear twice; a source may.  Pairs with an id outside
+   [0, src_blocks) or [0, dst_blocks) are left out.  pairs_host (optional): a
+   host copy of the pairs, used only to check all of this (PADOC_ERR_BOUNDS).
+   The caches are contiguous, in the layouts at the top of this file, 16-byte
+   aligned, head_dim 64 or 128; K and V of one side are distinct buffers.
+   Nothing is allocated; the launch may be captured. */
+padoc_status padoc_cache_copy_blocks(const void* k_src, const void* v_src, int64_t src_blocks, void* k_dst,
+                                     void* v_dst, int64_t dst_blocks, const int32_t* pairs, int64_t n_pairs,
+                                     const int32_t* pairs_host, int32_t num_heads_kv, int32_t head_dim,
+                                     padoc_dtype dtype, hipStream_t stream);
+
 /* Decode step over a paged cache.  Needs a plan with block_size == 16.
    k_cache / v_cache follow the paged layouts above (chunk-major K, d-major
    V).  block_table is the device copy of the table the plan was built for
@@ -526,6 +664,55 @@ padoc_status padoc_session_prepare(padoc_session* session, const int32_t* n_new,
 padoc_status padoc_session_launch(padoc_session* session, const void* q, const void* k_new, const void* v_new,
                                   void* o, float* lse, void* workspace, size_t workspace_bytes,
                                   hipStream_t stream);
+
+/* Fork a stream as a sibling (a sampled alternative, a beam): a new open
+   stream with the parent and fork of kept stream `id`, holding its first `len`
+   tokens (0 <= len <= its length).  The blocks are shared, not copied: the
+   first step that appends to a block two streams share copies it, within its
+   launch.  PADOC_ERR_BOUNDS when the block table cannot hold the new stream;
+   PADOC_ERR_MODE between a prepare and its launch. */
+padoc_status padoc_session_clone(padoc_session* session, int32_t id, int32_t len, int32_t* new_id);
+
+/* Drop the tokens of open stream `id` behind its first `len`: their blocks
+   return to the pool (those no other stream shares).  PADOC_ERR_TREE when a
+   kept child of the stream sees more than `len` of its tokens. */
+padoc_status padoc_session_truncate(padoc_session* session, int32_t id, int32_t len);
+
+/* Move kept blocks with the largest ids to the free blocks with the smallest
+   ids, at most max_moves of them (0: as many as it takes until the kept blocks
+   fill the front of the pool), so that the pool can shrink.  The next step's
+   launch copies them (before it appends) and patches the block table; until
+   then the caches are as they were.  *n_moves (may be NULL) receives their
+   number.  Blocks taken later are the free ones with the smallest ids. */
+padoc_status padoc_session_compact(padoc_session* session, int32_t max_moves, int32_t* n_moves);
+
+/* Change the pool to num_blocks blocks, in caches k_cache / v_cache that hold
+   the present blocks at their ids (a shorter view of the same buffers after a
+   compaction, or larger buffers the caller copied them to; NULL both for a
+   host-only session).  PADOC_ERR_BOUNDS when a kept block does not fit;
+   PADOC_ERR_MODE while a compaction's copies wait for their launch, or
+   between a prepare and its launch. */
+padoc_status padoc_session_resize(padoc_session* session, int64_t num_blocks, void* k_cache, void* v_cache);
+
+/* The block copies of the prepared step, which padoc_session_launch makes
+   before it appends (a caller of padoc_session_commit makes them itself):
+   phase p is the (source, destination) pairs [phase_ptr[p], phase_ptr[p+1])
+   of `pairs`; the pairs of a phase do not depend on each other, a later
+   phase follows an earlier one.  Pointers stay valid until the next session
+   call that changes the tree; all 0 / NULL when no step is prepared. */
+padoc_status padoc_session_copies(const padoc_session* session, int32_t* n_phases, const int32_t** phase_ptr,
+                                  const int32_t** pairs);
+
+/* padoc_session_launch for rows that are not rotated yet: q, k and v of `rows`
+   are the projection's rows, normed and rotated as padoc_rotary_append does
+   (k and v appended, q into rows->q_out, which the attention reads: contiguous
+   [n_q_rows, Hq, d], 16-byte aligned; it may be q itself).  rows->n_q /
+   n_new must be the prepared step's rows and the head counts the session's;
+   slots, k_cache, v_cache and num_blocks are the session's and must be 0 here.
+   The rotary must have the session's head_dim and dtype. */
+padoc_status padoc_session_launch_rotary(padoc_session* session, const padoc_rotary* rotary,
+                                         const padoc_rotary_append_args* rows, void* o, float* lse, void* workspace,
+                                         size_t workspace_bytes, hipStream_t stream);
 
 /* Complete the prepared step without device work, for callers that write
    the step's K/V rows and block-table patches themselves (from the view)

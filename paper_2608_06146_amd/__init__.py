@@ -8,11 +8,15 @@ marshals arguments.  PyTorch provides device memory and the current stream.
                     num_kv_rows=T, num_q_rows=n_q)
     o, lse = tree_attn_fwd(q, k, v, plan)                    # packed forward
     o, lse = branch_decode(q, k_cache, v_cache, bt, plan)    # paged decode step
+
+    rot = Rotary(d, "bf16", sections=(16, 24, 24))           # head norms and positions around it
+    q, k = rotary_fwd(q, k, positions, rot, wq, wk)
 """
 from __future__ import annotations
 
 import ctypes as C
 import math
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -21,7 +25,8 @@ from . import _lib
 from ._lib import PadocError, SEGMENT_DTYPE, WORK_DTYPE, RANGE_DTYPE, BWD_DTYPE
 
 __all__ = ["TreePlan", "segments_from_pages", "segments_layout", "tree_attn_fwd", "tree_attn_bwd", "branch_decode",
-           "DecodeSession", "tree_depths", "tree_remaining", "cache_from_rows", "PadocError", "SEGMENT_DTYPE", "version", "set_kernel_events", "make_workspace"]
+           "DecodeSession", "tree_depths", "tree_remaining", "cache_from_rows", "Rotary", "rotary_fwd", "rotary_bwd",
+           "rotary_append", "cache_copy_blocks", "PadocError", "SEGMENT_DTYPE", "version", "set_kernel_events", "make_workspace"]
 
 _DTYPES = {"f32": _lib.F32, "fp32": _lib.F32, "float32": _lib.F32, "bf16": _lib.BF16, "bfloat16": _lib.BF16}
 
@@ -415,6 +420,317 @@ def tree_attn_bwd(q, k, v, o, lse, dout, plan: TreePlan, dq=None, dk=None, dv=No
     return dq, dk, dv
 
 
+_STYLES = {"halves": 0, "pairs": 1}  # padoc_rotary_style
+
+
+class Rotary:
+    """Head norms and rotary positions of a decoder layer (``padoc_rotary``):
+    the first ``rotary_dim`` dimensions (default: all) of every head are
+    rotated by the positions of up to four axes.  ``axis[i]`` is the axis of
+    pair i, or ``sections`` counts the pairs of each axis in order; neither:
+    one axis.  ``inv_freq`` (radians per position of each pair) replaces
+    ``base ** (-2 i / rotary_dim)``.  ``style``: "halves" pairs dimensions i
+    and i + rotary_dim/2, "pairs" 2i and 2i + 1.  ``scale`` multiplies the
+    cosines and sines; ``eps`` belongs to the norms (used where a call passes
+    weights).  Host memory only."""
+
+    def __init__(self, head_dim: int, dtype: str = "bf16", rotary_dim: Optional[int] = None, sections=None, axis=None,
+                 base: float = 10000.0, inv_freq=None, style: str = "halves", scale: float = 1.0, eps: float = 1e-6):
+        self.head_dim, self.dtype = int(head_dim), dtype
+        self.rotary_dim = self.head_dim if rotary_dim is None else int(rotary_dim)
+        if style not in _STYLES:
+            raise ValueError(f"style {style!r} is not one of {sorted(_STYLES)}")
+        if sections is not None:
+            if axis is not None:
+                raise ValueError("pass sections or axis, not both")
+            axis = np.repeat(np.arange(len(sections)), sections)
+        pairs = self.rotary_dim // 2
+        ax = None if axis is None else np.ascontiguousarray(axis, dtype=np.int32)
+        fr = None if inv_freq is None else np.ascontiguousarray(inv_freq, dtype=np.float64)
+        for name, a in (("axis / sections", ax), ("inv_freq", fr)):
+            if a is not None and a.shape != (pairs,):
+                raise ValueError(f"{name} must cover the {pairs} rotated pairs, got shape {a.shape}")
+        self.n_axes = 1 if ax is None else len(sections) if sections is not None else int(ax.max(initial=0)) + 1
+        desc = _lib.RotaryDesc(self.head_dim, self.rotary_dim, self.n_axes, _STYLES[style],
+                               ax.ctypes.data if ax is not None else None,
+                               fr.ctypes.data if fr is not None else None, float(base), float(scale), float(eps),
+                               _DTYPES[dtype])
+        h = C.c_void_p()
+        _lib.check(_lib.lib().padoc_rotary_create(C.byref(desc), C.byref(h)))
+        self._h = h
+
+    @property
+    def handle(self):
+        if self._h is None:
+            raise ValueError("rotary is closed")
+        return self._h
+
+    def close(self):
+        if getattr(self, "_h", None) is not None:
+            _lib.lib().padoc_rotary_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+_NO_HEADS = (0, 0, 0)
+
+
+def _heads(name, t, like, shape=None):
+    """``(data, row stride, head stride)`` of rows of heads ``[n, H, d]`` on
+    the device and of the dtype of ``like``."""
+    if t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, expected {like.device}")
+    if t.dtype != like.dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {like.dtype}")
+    if t.dim() != 3 or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {'[n, H, d]' if shape is None else tuple(shape)}")
+    rs, hs, es = t.stride()
+    if es != 1:
+        raise ValueError(f"{name}: the head dimension must be contiguous")
+    return t.data_ptr(), rs, hs
+
+
+def _rows_of(rotary, tensors):
+    """The first tensor given, checked against the handle."""
+    import torch
+    like = next((t for t in tensors if t is not None), None)
+    if not isinstance(like, torch.Tensor):
+        raise TypeError("rows must be torch tensors")
+    if not like.is_cuda:
+        raise ValueError(f"rows are on {like.device}, expected a GPU")
+    if like.dtype != _torch_dtype(rotary):
+        raise TypeError(f"rows have dtype {like.dtype}, the rotary is for {rotary.dtype}")
+    if like.dim() != 3 or like.shape[2] != rotary.head_dim:
+        raise ValueError(f"rows must be [n, H, {rotary.head_dim}], got {tuple(like.shape)}")
+    return like
+
+
+def _weight(name, w, like):
+    """Address of a norm's weight ``[d]``, 0 for None."""
+    if w is None:
+        return 0
+    _check_tensor(name, w, like.dtype, like.device)
+    if w.shape != like.shape[2:]:
+        raise ValueError(f"{name} has shape {tuple(w.shape)}, expected {tuple(like.shape[2:])}")
+    return w.data_ptr()
+
+
+def _positions(name, pos, rotary, n, like):
+    """``(address, axis stride)`` of int32 positions ``[n_axes, n]`` (``[n]``
+    for one axis)."""
+    import torch
+    if pos.device != like.device:
+        raise ValueError(f"{name} is on {pos.device}, expected {like.device}")
+    if pos.dtype != torch.int32:
+        raise TypeError(f"{name} has dtype {pos.dtype}, expected torch.int32")
+    if pos.dim() == 1 and rotary.n_axes == 1:
+        pos = pos[None]
+    if pos.dim() != 2 or pos.shape[0] != rotary.n_axes or pos.shape[1] != n:
+        raise ValueError(f"{name} has shape {tuple(pos.shape)}, expected {(rotary.n_axes, n)}")
+    if n > 1 and pos.stride(1) != 1:
+        raise ValueError(f"{name}: the positions of an axis must be contiguous")
+    return pos.data_ptr(), pos.stride(0) if rotary.n_axes > 1 else 0
+
+
+def _launch(f, dev, stream, made, *args):
+    """``f(*args, stream)`` on ``dev`` and ``stream`` (None: its current one);
+    tensors that the call ``made`` stay while a stream of the caller's reads
+    them."""
+    import torch
+    if stream is None:
+        s = torch.cuda.current_stream(dev)
+    else:
+        s = stream
+        if s.device != dev:
+            raise ValueError(f"the stream is on {s.device}, the tensors on {dev}")
+        for t in made:
+            t.record_stream(s)
+    if dev.index == torch.cuda.current_device():
+        _lib.check(f(*args, s.cuda_stream))
+    else:
+        with torch.cuda.device(dev):
+            _lib.check(f(*args, s.cuda_stream))
+
+
+def rotary_fwd(q, k, positions, rotary: Rotary, q_weight=None, k_weight=None, q_out=None, k_out=None, stream=None):
+    """Per-head RMS norm (where weights ``[d]`` are given) and rotation of q
+    ``[n, Hq, d]`` and k ``[n, Hkv, d]`` by ``positions`` (int32 ``[n_axes,
+    n]``; ``padoc_rotary_fwd``).  Rows and heads may be strided, as in slices
+    of a fused projection; q or k may be None, and q_out / k_out may be q / k.
+    Returns ``(q_out, k_out)``."""
+    import torch
+    like = _rows_of(rotary, (q, k))
+    n, dev, made = like.shape[0], like.device, []
+    heads, outs, counts = [], [], []
+    for name, x, out in (("q", q, q_out), ("k", k, k_out)):
+        if x is None:
+            heads.append(_NO_HEADS), heads.append(_NO_HEADS), outs.append(None), counts.append(0)
+            continue
+        shape = (n, x.shape[1], rotary.head_dim)
+        heads.append(_heads(name, x, like, shape))
+        if out is None:
+            out = torch.empty(shape, dtype=x.dtype, device=dev)
+            made.append(out)
+        heads.append(_heads(name + "_out", out, like, shape))
+        outs.append(out)
+        counts.append(shape[1])
+    pos = _positions("positions", positions, rotary, n, like)
+    args = _lib.ROTARY_FWD_ARGS.pack(n, counts[0], counts[1], *pos, *heads[0], *heads[2], *heads[1], *heads[3],
+                                     _weight("q_weight", q_weight, like), _weight("k_weight", k_weight, like))
+    _launch(_lib.lib().padoc_rotary_fwd, dev, stream, made, rotary.handle, args)
+    return outs[0], outs[1]
+
+
+def rotary_bwd(dq_out, dk_out, positions, rotary: Rotary, q=None, k=None, q_weight=None, k_weight=None, dq=None,
+               dk=None, weight_grads: bool = True, stream=None):
+    """Gradients of ``rotary_fwd`` (``padoc_rotary_bwd``): dq_out / dk_out are
+    those of its outputs, q / k its inputs (read only where there is a
+    weight).  Returns ``(dq, dk, dq_weight, dk_weight)``; the weights'
+    gradients are float32 ``[d]``, None without a weight or with
+    ``weight_grads=False``."""
+    import torch
+    like = _rows_of(rotary, (dq_out, dk_out))
+    n, dev, made = like.shape[0], like.device, []
+    heads, outs, counts, ws, dws = [], [], [], [], []
+    for name, g, x, w, out in (("q", dq_out, q, q_weight, dq), ("k", dk_out, k, k_weight, dk)):
+        if g is None:
+            heads.append((_NO_HEADS,) * 3), outs.append(None), counts.append(0), ws.append(0), dws.append(None)
+            continue
+        shape = (n, g.shape[1], rotary.head_dim)
+        hg = _heads(f"d{name}_out", g, like, shape)
+        if w is not None and x is None:
+            raise ValueError(f"the backward of {name}'s norm needs {name}")
+        hx = _heads(name, x, like, shape) if w is not None else _NO_HEADS
+        if out is None:
+            out = torch.empty(shape, dtype=g.dtype, device=dev)
+            made.append(out)
+        heads.append((hg, hx, _heads("d" + name, out, like, shape)))
+        outs.append(out)
+        counts.append(shape[1])
+        ws.append(_weight(name + "_weight", w, like))
+        dws.append(torch.empty(rotary.head_dim, dtype=torch.float32, device=dev) if w is not None and weight_grads else None)
+    made.extend(t for t in dws if t is not None)
+    pos = _positions("positions", positions, rotary, n, like)
+    L, h = _lib.lib(), rotary.handle
+    wptr, wbytes = None, 0
+    if dws[0] is not None or dws[1] is not None:
+        nb = C.c_size_t(0)
+        _lib.check(L.padoc_rotary_bwd_workspace_bytes(h, n, counts[0], counts[1], C.byref(nb)))
+        work = torch.empty(nb.value, dtype=torch.uint8, device=dev)  # the allocator's blocks are 512-byte aligned
+        made.append(work)
+        wptr, wbytes = work.data_ptr(), nb.value
+    (gq, xq, oq), (gk, xk, ok) = heads
+    args = _lib.ROTARY_BWD_ARGS.pack(n, counts[0], counts[1], *pos, *xq, *xk, *gq, *gk, *oq, *ok, ws[0], ws[1],
+                                     *(0 if t is None else t.data_ptr() for t in dws))
+    _launch(L.padoc_rotary_bwd, dev, stream, made, h, args, wptr, wbytes)
+    return outs[0], outs[1], dws[0], dws[1]
+
+
+def _append_args(rotary, q, k, v, positions, q_weight, k_weight, q_positions, q_out, made, slots=0, k_cache=0, v_cache=0,
+                 num_blocks=0):
+    """The packed arguments of an append, and its q_out."""
+    import torch
+    like = _rows_of(rotary, (k, q))
+    dev = like.device
+    nq, hq, hqo, n_q, qpos = 0, _NO_HEADS, _NO_HEADS, 0, (0, 0)
+    n_new, hkv, hk, hv, pos = 0, 0, _NO_HEADS, _NO_HEADS, (0, 0)
+    if k is not None:
+        n_new, hkv = k.shape[0], k.shape[1]
+        hk = _heads("k", k, like)
+        hv = _heads("v", v, like, k.shape)
+        pos = _positions("positions", positions, rotary, n_new, like)
+    if q is not None:
+        shape = (q.shape[0], q.shape[1], rotary.head_dim)
+        n_q, nq = shape[:2]
+        hq = _heads("q", q, like, shape)
+        if q_out is None:
+            q_out = torch.empty(shape, dtype=q.dtype, device=dev)
+            made.append(q_out)
+        hqo = _heads("q_out", q_out, like, shape)
+        if q_positions is not None:
+            qpos = _positions("q_positions", q_positions, rotary, n_q, like)
+        elif k is None:
+            qpos = _positions("positions", positions, rotary, n_q, like)
+    args = _lib.ROTARY_APPEND_ARGS.pack(n_q, n_new, nq, hkv, *qpos, *pos, *hq, *hk, *hv, *hqo,
+                                        _weight("q_weight", q_weight, like), _weight("k_weight", k_weight, like), slots,
+                                        k_cache, v_cache, num_blocks)
+    return args, q_out, dev
+
+
+def _check_caches(k_cache, v_cache, dtype, dev, d=None):
+    """Checks caches in the library's layouts; ``(blocks, Hkv, d)``."""
+    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
+        _check_tensor(name, t, dtype, dev)
+    nb, hkv, d = (v_cache.shape[0], v_cache.shape[1], v_cache.shape[2]) if v_cache.dim() == 4 else (0, 0, 0)
+    if v_cache.shape != (nb, hkv, d, 16) or k_cache.shape != (nb, hkv, d // 8, 16, 8):
+        raise ValueError(f"caches must be K [blocks, Hkv, d/8, 16, 8] and V [blocks, Hkv, d, 16], got "
+                         f"{tuple(k_cache.shape)} and {tuple(v_cache.shape)}")
+    return nb, hkv, d
+
+
+def rotary_append(q, k, v, positions, slots, k_cache, v_cache, rotary: Rotary, q_weight=None, k_weight=None,
+                  q_positions=None, q_out=None, stream=None):
+    """A decode step's rows (``padoc_rotary_append``): q ``[n_q, Hq, d]``
+    normed and rotated into ``q_out``, k and v ``[n_new, Hkv, d]`` into the
+    caches (k normed and rotated) at ``slots`` (int32 ``[n_new, 2]``: block id
+    and slot; a block id of -1 leaves the row out).  ``q_positions`` may be
+    left out when query row i is new row i; q may be None.  Returns q_out."""
+    import torch
+    if k is None or v is None:
+        raise ValueError("rotary_append needs k and v (rotary_fwd rotates q alone)")
+    dt = _torch_dtype(rotary)
+    nb, hkv, d = _check_caches(k_cache, v_cache, dt, k.device)
+    if (hkv, d) != (k.shape[1], rotary.head_dim):
+        raise ValueError(f"the caches hold {hkv} heads of {d}, the rows {k.shape[1]} of {rotary.head_dim}")
+    _check_tensor("slots", slots, torch.int32, k.device)
+    if slots.shape != (k.shape[0], 2):
+        raise ValueError(f"slots has shape {tuple(slots.shape)}, expected {(k.shape[0], 2)}")
+    made = []
+    args, q_out, dev = _append_args(rotary, q, k, v, positions, q_weight, k_weight, q_positions, q_out, made,
+                                    slots.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), nb)
+    _launch(_lib.lib().padoc_rotary_append, dev, stream, made, rotary.handle, args)
+    return q_out
+
+
+def cache_copy_blocks(k_cache, v_cache, pairs, k_dst=None, v_dst=None, pairs_host=None, stream=None):
+    """Copy blocks ``pairs[i, 0]`` of the paged caches to blocks ``pairs[i,
+    1]`` of the same caches, or of ``k_dst`` / ``v_dst``
+    (``padoc_cache_copy_blocks``; int32 ``[n, 2]`` on the device, with an
+    optional host copy that is only checked).  Returns the caches written."""
+    import torch
+    if (k_dst is None) != (v_dst is None):
+        raise ValueError("pass k_dst and v_dst together (or neither)")
+    dev, dt = k_cache.device, k_cache.dtype
+    if not k_cache.is_cuda:
+        raise ValueError(f"k_cache is on {dev}, expected a GPU")
+    if dt not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"caches must be bfloat16 or float32, got {dt}")
+    nb, hkv, d = _check_caches(k_cache, v_cache, dt, dev)
+    if k_dst is None:
+        k_dst, v_dst, nd = k_cache, v_cache, nb
+    else:
+        nd, h2, d2 = _check_caches(k_dst, v_dst, dt, dev)
+        if (h2, d2) != (hkv, d):
+            raise ValueError(f"blocks of {hkv} heads of {d} do not fit caches of {h2} heads of {d2}")
+    _check_tensor("pairs", pairs, torch.int32, dev)
+    if pairs.dim() != 2 or pairs.shape[1] != 2:
+        raise ValueError(f"pairs has shape {tuple(pairs.shape)}, expected [n, 2]")
+    host = None
+    if pairs_host is not None:
+        host = np.ascontiguousarray(pairs_host, dtype=np.int32)
+        if host.shape != pairs.shape:
+            raise ValueError(f"pairs_host has shape {host.shape}, expected {tuple(pairs.shape)}")
+    _launch(_lib.lib().padoc_cache_copy_blocks, dev, stream, (), k_cache.data_ptr(), v_cache.data_ptr(), nb,
+            k_dst.data_ptr(), v_dst.data_ptr(), nd, pairs.data_ptr(), pairs.shape[0],
+            None if host is None else host.ctypes.data, hkv, d, _lib.BF16 if dt == torch.bfloat16 else _lib.F32)
+    return k_dst, v_dst
+
+
 class DecodeSession:
     """Decode session (``padoc_session_*``): the step loop of masked parallel
     decoding (App. E) over caller-owned paged caches.
@@ -509,6 +825,68 @@ class DecodeSession:
             _lib.check(st)
         self.n_open -= 1
 
+    def clone(self, stream_id: int, length: Optional[int] = None) -> int:
+        """A new open stream beside ``stream_id`` (same parent and fork) that
+        holds its first ``length`` tokens (default: all;
+        ``padoc_session_clone``).  Blocks are shared until one of the streams
+        appends to them."""
+        if length is None:
+            length = self._length(stream_id)
+        i = C.c_int32(0)
+        _lib.check(_lib.lib().padoc_session_clone(self.handle, int(stream_id), int(length), C.byref(i)))
+        self.n_open += 1
+        return int(i.value)
+
+    def _length(self, stream_id: int) -> int:
+        v = _lib.SessionView()
+        _lib.check(_lib.lib().padoc_session_view_get(self.handle, C.byref(v)))
+        at = np.nonzero(_carray(v.seg_id, v.n_seg, np.int32) == stream_id)[0]
+        if len(at) == 0:
+            raise ValueError(f"stream {stream_id} is not a kept stream of this session")
+        return int(_carray(v.seg, v.n_seg, SEGMENT_DTYPE)["len"][at[0]])
+
+    def truncate(self, stream_id: int, length: int) -> None:
+        """Drop the tokens of an open stream behind its first ``length``
+        (``padoc_session_truncate``)."""
+        _lib.check(_lib.lib().padoc_session_truncate(self.handle, int(stream_id), int(length)))
+
+    def compact(self, max_moves: int = 0) -> int:
+        """Move kept blocks to the front of the pool, at most ``max_moves`` of
+        them (0: all that it takes); the next launch copies them
+        (``padoc_session_compact``).  Returns their number."""
+        n = C.c_int32(0)
+        _lib.check(_lib.lib().padoc_session_compact(self.handle, int(max_moves), C.byref(n)))
+        return int(n.value)
+
+    def resize(self, num_blocks: int, k_cache=None, v_cache=None) -> None:
+        """Change the pool to ``num_blocks`` blocks
+        (``padoc_session_resize``): with device caches, into ``k_cache`` /
+        ``v_cache`` of that many blocks, which hold the present blocks at their
+        ids (``k_cache[:num_blocks]`` of the old caches after a compaction, or
+        larger ones the caller copied them to)."""
+        if (k_cache is None) != (v_cache is None) or (k_cache is None) != (self.k_cache is None):
+            raise ValueError("pass both caches, or neither for a host-only session")
+        if k_cache is not None:
+            got = _check_caches(k_cache, v_cache, self.k_cache.dtype, self.device)
+            if got != (num_blocks, self.num_heads_kv, self.head_dim):
+                raise ValueError(f"caches hold {got} blocks, heads and dimensions, expected "
+                                 f"{(num_blocks, self.num_heads_kv, self.head_dim)}")
+        _lib.check(_lib.lib().padoc_session_resize(self.handle, int(num_blocks),
+                                                   None if k_cache is None else k_cache.data_ptr(),
+                                                   None if v_cache is None else v_cache.data_ptr()))
+        self.k_cache, self.v_cache, self.num_blocks = k_cache, v_cache, int(num_blocks)
+
+    def copies(self):
+        """The prepared step's block copies: one ``[n, 2]`` array of (source,
+        destination) per phase (``padoc_session_copies``)."""
+        n, ptr, pairs = C.c_int32(0), C.c_void_p(), C.c_void_p()
+        _lib.check(_lib.lib().padoc_session_copies(self.handle, C.byref(n), C.byref(ptr), C.byref(pairs)))
+        if n.value == 0:
+            return []
+        p = _carray(ptr.value, n.value + 1, np.int32)
+        all_pairs = _carray(pairs.value, 2 * int(p[-1]), np.int32).reshape(-1, 2)
+        return [all_pairs[a:b] for a, b in zip(p[:-1], p[1:])]
+
     def select(self, max_rows: int, priority=None):
         """``(n_new, n_query)`` for a step that takes at most ``max_rows``
         rows (``padoc_session_select``): the open streams with the largest
@@ -591,6 +969,64 @@ class DecodeSession:
                                                    p(v_new, self.n_kv_rows), p(out, self.n_q_rows),
                                                    p(lse, self.n_q_rows), _ptr(ws), ws.numel(),
                                                    C.c_void_p(s.cuda_stream)))
+        return out, lse
+
+    def launch_rotary(self, q, k_new, v_new, positions, rotary: Rotary, q_weight=None, k_weight=None, q_positions=None,
+                      q_rot=None, out=None, lse=None, workspace=None, stream=None):
+        """``launch`` for rows that are not rotated yet
+        (``padoc_session_launch_rotary``): q, k_new and v_new are rows of the
+        projections (they may be strided), ``positions`` int32 ``[n_axes,
+        n_kv_rows]``; ``q_positions`` may be left out when every new token is a
+        query.  ``q_rot`` receives the rotated queries (contiguous).  Returns
+        ``(O, LSE)``."""
+        import torch
+        if self.device is None:
+            raise RuntimeError("host-only session: use commit()")
+        n_q, n_kv = self.n_q_rows, self.n_kv_rows
+        dt, dev = self.k_cache.dtype, self.device
+        if _torch_dtype(rotary) != dt:
+            raise TypeError(f"the rotary is for {rotary.dtype}, the session's caches are {dt}")
+        if rotary.head_dim != self.head_dim:
+            raise ValueError(f"the rotary is for heads of {rotary.head_dim}, the session's have {self.head_dim}")
+        if n_kv:
+            for name, t in (("k_new", k_new), ("v_new", v_new)):
+                if not isinstance(t, torch.Tensor):
+                    raise TypeError(f"{name} must be a torch tensor")
+                if tuple(t.shape) != (n_kv, self.num_heads_kv, self.head_dim):
+                    raise ValueError(f"{name} must be [{n_kv}, {self.num_heads_kv}, {self.head_dim}]")
+        if n_q:
+            if not isinstance(q, torch.Tensor):
+                raise TypeError("q must be a torch tensor")
+            if tuple(q.shape) != (n_q, self.num_heads_q, self.head_dim):
+                raise ValueError(f"q must be [{n_q}, {self.num_heads_q}, {self.head_dim}]")
+        made = []
+        if out is None:
+            out = torch.empty(n_q, self.num_heads_q, self.head_dim, dtype=dt, device=dev)
+            made.append(out)
+        if lse is None:
+            lse = torch.empty(n_q, self.num_heads_q, dtype=torch.float32, device=dev)
+            made.append(lse)
+        if n_q:
+            _check_tensor("out", out, dt, dev)
+            _check_tensor("lse", lse, torch.float32, dev)
+            if tuple(out.shape) != tuple(q.shape) or tuple(lse.shape) != tuple(q.shape[:2]):
+                raise ValueError("out / lse shape does not match q")
+            if q_rot is not None:
+                _check_tensor("q_rot", q_rot, dt, dev)
+        if n_q and n_kv and q_positions is None and n_q != n_kv:
+            raise ValueError(f"{n_q} query rows of {n_kv} new ones need q_positions")
+        if n_q or n_kv:
+            args, _, rows_dev = _append_args(rotary, q if n_q else None, k_new if n_kv else None, v_new, positions,
+                                             q_weight, k_weight, q_positions, q_rot, made)
+            if rows_dev != dev:
+                raise ValueError(f"rows are on {rows_dev}, expected {dev}")
+        else:
+            args = _lib.ROTARY_APPEND_ARGS.pack(*[0] * 26)
+        # head counts are the session's also where a step has no rows of a kind
+        args = args[:16] + struct.pack("=ii", self.num_heads_q, self.num_heads_kv) + args[24:]
+        ws = self.workspace() if workspace is None else workspace
+        _launch(_lib.lib().padoc_session_launch_rotary, dev, stream, made, self.handle, rotary.handle, args,
+                out.data_ptr() if n_q else None, lse.data_ptr() if n_q else None, ws.data_ptr(), ws.numel())
         return out, lse
 
     def step(self, q, k_new, v_new, n_new=None, n_query=None, **kw):

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -81,6 +82,19 @@ class SessionView(C.Structure):
                 ("workspace_bytes", C.c_size_t)]
 
 
+class RotaryDesc(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("n_axes", C.c_int32), ("style", C.c_int32),
+                ("axis", C.c_void_p), ("inv_freq", C.c_void_p), ("base", C.c_double), ("scale", C.c_float),
+                ("norm_eps", C.c_float), ("dtype", C.c_int32)]
+
+
+# The argument structs of the rotary calls, packed without a ctypes.Structure
+# (a call's smallest cost is the host's): a padoc_heads is (data, row stride,
+# head stride).
+ROTARY_FWD_ARGS = struct.Struct("=qiiQq" + 4 * "Qqq" + "QQ")
+ROTARY_BWD_ARGS = struct.Struct("=qiiQq" + 6 * "Qqq" + "QQQQ")
+ROTARY_APPEND_ARGS = struct.Struct("=qqiiQqQq" + 4 * "Qqq" + "QQQQQq")
+
 EXPORTED = [
     "padoc_tree_from_pages", "padoc_tree_layout", "padoc_plan_create", "padoc_plan_workspace_bytes",
     "padoc_plan_export", "padoc_plan_destroy", "padoc_tree_attn_fwd", "padoc_branch_decode",
@@ -90,6 +104,10 @@ EXPORTED = [
     "padoc_session_create", "padoc_session_destroy", "padoc_session_open", "padoc_session_close",
     "padoc_session_prepare", "padoc_session_launch", "padoc_session_commit", "padoc_session_view_get",
     "padoc_tree_depths", "padoc_tree_remaining", "padoc_session_select", "padoc_cache_from_rows",
+    "padoc_rotary_create", "padoc_rotary_destroy", "padoc_rotary_fwd", "padoc_rotary_bwd_workspace_bytes",
+    "padoc_rotary_bwd", "padoc_rotary_append", "padoc_cache_copy_blocks", "padoc_session_launch_rotary",
+    "padoc_session_clone", "padoc_session_truncate", "padoc_session_compact", "padoc_session_resize",
+    "padoc_session_copies",
 ]
 
 _lib = None
@@ -133,6 +151,20 @@ def lib():
     L.padoc_tree_remaining.argtypes = [vp, i32, vp, vp]
     L.padoc_session_select.argtypes = [vp, i32, vp, vp, vp]
     L.padoc_cache_from_rows.argtypes = [vp, vp, vp, vp, C.c_int64, i32, i32, C.c_int, vp]
+    L.padoc_rotary_create.argtypes = [C.POINTER(RotaryDesc), C.POINTER(vp)]
+    L.padoc_rotary_destroy.argtypes = [vp]
+    L.padoc_rotary_destroy.restype = None
+    L.padoc_rotary_fwd.argtypes = [vp, C.c_char_p, vp]
+    L.padoc_rotary_bwd_workspace_bytes.argtypes = [vp, i64, i32, i32, C.POINTER(sz)]
+    L.padoc_rotary_bwd.argtypes = [vp, C.c_char_p, vp, sz, vp]
+    L.padoc_rotary_append.argtypes = [vp, C.c_char_p, vp]
+    L.padoc_cache_copy_blocks.argtypes = [vp, vp, i64, vp, vp, i64, vp, i64, vp, i32, i32, C.c_int, vp]
+    L.padoc_session_launch_rotary.argtypes = [vp, vp, C.c_char_p, vp, vp, vp, sz, vp]
+    L.padoc_session_clone.argtypes = [vp, i32, i32, C.POINTER(i32)]
+    L.padoc_session_truncate.argtypes = [vp, i32, i32]
+    L.padoc_session_compact.argtypes = [vp, i32, C.POINTER(i32)]
+    L.padoc_session_resize.argtypes = [vp, i64, vp, vp]
+    L.padoc_session_copies.argtypes = [vp, C.POINTER(i32), C.POINTER(vp), C.POINTER(vp)]
     L.padoc_last_error.argtypes = []
     L.padoc_last_error.restype = C.c_char_p
     L.padoc_set_kernel_events.argtypes = [vp, vp]
@@ -144,7 +176,10 @@ def lib():
                  "padoc_plan_backward_workspace_bytes", "padoc_tree_attn_bwd", "padoc_session_create",
                  "padoc_session_open", "padoc_session_close", "padoc_session_prepare", "padoc_session_launch",
                  "padoc_session_commit", "padoc_session_view_get", "padoc_tree_depths",
-                 "padoc_tree_remaining", "padoc_session_select", "padoc_cache_from_rows"):
+                 "padoc_tree_remaining", "padoc_session_select", "padoc_cache_from_rows", "padoc_rotary_create",
+                 "padoc_rotary_fwd", "padoc_rotary_bwd_workspace_bytes", "padoc_rotary_bwd", "padoc_rotary_append",
+                 "padoc_cache_copy_blocks", "padoc_session_launch_rotary", "padoc_session_clone",
+                 "padoc_session_truncate", "padoc_session_compact", "padoc_session_resize", "padoc_session_copies"):
         getattr(L, name).restype = C.c_int
     _lib = L
     return L

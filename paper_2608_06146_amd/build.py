@@ -30,6 +30,7 @@ STREAMS_SOURCE = "csrc/python/streams.cpp"
 SOURCES = [
     "csrc/host/plan.cpp",
     "csrc/host/session.cpp",
+    "csrc/host/rotary.cpp",
     "csrc/abi.hip",
     "csrc/kernels/tile_mfma_bf16.hip",
     "csrc/kernels/decode_step.hip",
@@ -39,6 +40,8 @@ SOURCES = [
     "csrc/kernels/append.hip",
     "csrc/kernels/relayout.hip",
     "csrc/kernels/upload.hip",
+    "csrc/kernels/rotary.hip",
+    "csrc/kernels/copy_blocks.hip",
 ]
 # Every header under csrc/ (and the public header) enters each object's
 # digest, so an edit to any of them rebuilds every object.

@@ -7,6 +7,7 @@
 #include <mutex>
 
 #include "host/plan.hpp"
+#include "host/rotary.hpp"
 #include "host/session.hpp"
 
 namespace padoc {
@@ -23,6 +24,10 @@ hipError_t launch_upload(void* dst0, const void* src0, size_t bytes0, void* dst1
 hipError_t launch_append_kv(const void* k_new, const void* v_new, void* k_cache, void* v_cache, const int32_t* slots,
                             int64_t n_rows, int Hkv, int D, bool bf16, const int32_t* patch, int64_t n_patch,
                             int32_t* block_table, hipStream_t s);
+hipError_t launch_rotary_fwd(RotaryParams p, int D, bool bf16, bool pairs, hipStream_t s);
+hipError_t launch_rotary_bwd(RotaryParams p, int D, bool bf16, bool pairs, float* dwq, float* dwk, hipStream_t s);
+hipError_t launch_rotary_append(RotaryParams p, int D, bool bf16, bool pairs, hipStream_t s);
+hipError_t launch_copy_blocks(const CopyParams& p, hipStream_t s);
 
 namespace {
 thread_local hipEvent_t t_ev_before = nullptr;
@@ -30,6 +35,13 @@ thread_local hipEvent_t t_ev_after = nullptr;
 
 padoc_status hip_fail(const char* what, hipError_t e) {
   return set_error(PADOC_ERR_HIP, "%s failed: %s (%d)", what, hipGetErrorString(e), (int)e);
+}
+
+// The profiling events around the kernels of a call (where they are set).
+padoc_status record(hipEvent_t ev, hipStream_t stream) {
+  if (!t_ev_before || !t_ev_after) return PADOC_OK;
+  const hipError_t e = hipEventRecord(ev, stream);
+  return e == hipSuccess ? PADOC_OK : hip_fail("hipEventRecord", e);
 }
 
 template <class T>
@@ -344,6 +356,149 @@ extern "C" padoc_status padoc_cache_from_rows(const void* k_rows, const void* v_
   return PADOC_OK;
 }
 
+// The binding packs these by hand.
+static_assert(sizeof(padoc_rotary_fwd_args) == 144 && sizeof(padoc_rotary_bwd_args) == 208 &&
+              sizeof(padoc_rotary_append_args) == 200, "argument structs");
+
+namespace padoc {
+namespace {
+RotaryParams rotary_params(const padoc_rotary* r, int64_t n, int32_t Hq, int32_t Hkv, const int32_t* pos,
+                           int64_t pos_stride) {
+  RotaryParams p{};
+  p.table = r->table;
+  p.pos = pos;
+  p.pos_stride = pos_stride;
+  p.n_axes = r->n_axes;
+  p.pairs = r->pairs;
+  p.scale = r->scale;
+  p.eps = r->eps;
+  p.n = (int32_t)n;
+  p.Hq = Hq;
+  p.Hkv = Hkv;
+  return p;
+}
+
+// A step's rows on their way into the caches (checked: check_rotary_append).
+RotaryParams append_params(const padoc_rotary* r, const padoc_rotary_append_args* a) {
+  RotaryParams p = rotary_params(r, a->n_new, a->num_heads_q, a->num_heads_kv, a->pos, a->pos_stride);
+  p.n_q = (int32_t)a->n_q;
+  p.q_pos = a->q_pos ? a->q_pos : a->pos;
+  p.q_pos_stride = a->q_pos ? a->q_pos_stride : a->pos_stride;
+  p.q = a->q;
+  p.k = a->k;
+  p.v = a->v;
+  p.qo = a->q_out;
+  p.wq = a->q_weight;
+  p.wk = a->k_weight;
+  p.slots = a->slots;
+  p.k_cache = a->k_cache;
+  p.v_cache = a->v_cache;
+  p.n_blocks = a->num_blocks;
+  return p;
+}
+}  // namespace
+}  // namespace padoc
+
+extern "C" padoc_status padoc_rotary_fwd(const padoc_rotary* r, const padoc_rotary_fwd_args* a, hipStream_t stream) {
+  clear_error();
+  padoc_status st = check_rotary_fwd(r, a);
+  if (st != PADOC_OK) return st;
+  if (a->n_rows == 0 || a->num_heads_q + a->num_heads_kv == 0) return PADOC_OK;
+  RotaryParams p = rotary_params(r, a->n_rows, a->num_heads_q, a->num_heads_kv, a->pos, a->pos_stride);
+  p.q = a->q;
+  p.k = a->k;
+  p.qo = a->q_out;
+  p.ko = a->k_out;
+  p.wq = a->q_weight;
+  p.wk = a->k_weight;
+  if ((st = record(t_ev_before, stream)) != PADOC_OK) return st;
+  const hipError_t e = launch_rotary_fwd(p, r->D, r->dtype == PADOC_BF16, r->style == PADOC_ROTARY_PAIRS, stream);
+  if (e != hipSuccess) return hip_fail("rotary kernel launch", e);
+  return record(t_ev_after, stream);
+}
+
+extern "C" padoc_status padoc_rotary_bwd_workspace_bytes(const padoc_rotary* r, int64_t n_rows, int32_t num_heads_q,
+                                                         int32_t num_heads_kv, size_t* bytes) {
+  clear_error();
+  if (!bytes) return set_error(PADOC_ERR_ARG, "bytes is null");
+  padoc_rotary_bwd_args sizes{};
+  sizes.num_heads_q = num_heads_q;
+  sizes.num_heads_kv = num_heads_kv;
+  padoc_status st = check_rotary_bwd(r, &sizes);
+  if (st != PADOC_OK) return st;
+  if (n_rows < 0 || n_rows > INT32_MAX)
+    return set_error(n_rows < 0 ? PADOC_ERR_ARG : PADOC_ERR_BOUNDS, "n_rows=%lld must be in [0, 2^31-1]",
+                     (long long)n_rows);
+  const BwdGrid g = rotary_bwd_grid(n_rows, num_heads_q, num_heads_kv, r->D);
+  *bytes = std::max<size_t>(256, (size_t)g.x * g.y * 2 * r->D * sizeof(float));
+  return PADOC_OK;
+}
+
+extern "C" padoc_status padoc_rotary_bwd(const padoc_rotary* r, const padoc_rotary_bwd_args* a, void* workspace,
+                                         size_t workspace_bytes, hipStream_t stream) {
+  clear_error();
+  padoc_status st = check_rotary_bwd(r, a);
+  if (st != PADOC_OK) return st;
+  const bool sums = a->dq_weight || a->dk_weight;
+  if (sums) {
+    const BwdGrid g = rotary_bwd_grid(a->n_rows, a->num_heads_q, a->num_heads_kv, r->D);
+    const size_t need = (size_t)g.x * g.y * 2 * r->D * sizeof(float);
+    if (!workspace) return set_error(PADOC_ERR_WORKSPACE, "workspace is null");
+    if (((uintptr_t)workspace) & 255) return set_error(PADOC_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+    if (workspace_bytes < need)
+      return set_error(PADOC_ERR_WORKSPACE, "workspace of %zu bytes is smaller than the %zu the backward needs",
+                       workspace_bytes, need);
+  }
+  const bool rows = a->n_rows > 0 && a->num_heads_q + a->num_heads_kv > 0;
+  if (!rows && !sums) return PADOC_OK;
+  RotaryParams p = rotary_params(r, a->n_rows, a->num_heads_q, a->num_heads_kv, a->pos, a->pos_stride);
+  p.inverse = 1;
+  p.q = a->dq_out;
+  p.k = a->dk_out;
+  p.qo = a->dq;
+  p.ko = a->dk;
+  p.xq = a->q;
+  p.xk = a->k;
+  p.wq = a->q_weight;
+  p.wk = a->k_weight;
+  p.part = sums ? static_cast<float*>(workspace) : nullptr;
+  const bool bf16 = r->dtype == PADOC_BF16, pairs = r->style == PADOC_ROTARY_PAIRS;
+  if ((st = record(t_ev_before, stream)) != PADOC_OK) return st;
+  const hipError_t e = p.wq || p.wk ? launch_rotary_bwd(p, r->D, bf16, pairs, a->dq_weight, a->dk_weight, stream)
+                                    : launch_rotary_fwd(p, r->D, bf16, pairs, stream);
+  if (e != hipSuccess) return hip_fail("rotary backward kernel launch", e);
+  return record(t_ev_after, stream);
+}
+
+extern "C" padoc_status padoc_rotary_append(const padoc_rotary* r, const padoc_rotary_append_args* a,
+                                            hipStream_t stream) {
+  clear_error();
+  padoc_status st = check_rotary_append(r, a, /*session=*/false);
+  if (st != PADOC_OK) return st;
+  if ((a->n_q == 0 || a->num_heads_q == 0) && (a->n_new == 0 || a->num_heads_kv == 0)) return PADOC_OK;
+  if ((st = record(t_ev_before, stream)) != PADOC_OK) return st;
+  const hipError_t e =
+      launch_rotary_append(append_params(r, a), r->D, r->dtype == PADOC_BF16, r->style == PADOC_ROTARY_PAIRS, stream);
+  if (e != hipSuccess) return hip_fail("rotary append kernel launch", e);
+  return record(t_ev_after, stream);
+}
+
+extern "C" padoc_status padoc_cache_copy_blocks(const void* k_src, const void* v_src, int64_t src_blocks, void* k_dst,
+                                                void* v_dst, int64_t dst_blocks, const int32_t* pairs, int64_t n_pairs,
+                                                const int32_t* pairs_host, int32_t num_heads_kv, int32_t head_dim,
+                                                padoc_dtype dtype, hipStream_t stream) {
+  clear_error();
+  padoc_status st = check_copy_blocks(k_src, v_src, src_blocks, k_dst, v_dst, dst_blocks, pairs, n_pairs, pairs_host,
+                                      num_heads_kv, head_dim, dtype);
+  if (st != PADOC_OK || n_pairs == 0) return st;
+  CopyParams p{k_src, v_src, k_dst, v_dst, pairs, n_pairs, src_blocks, dst_blocks,
+               (int64_t)num_heads_kv * head_dim * (dtype == PADOC_BF16 ? 2 : 4)};
+  if ((st = record(t_ev_before, stream)) != PADOC_OK) return st;
+  const hipError_t e = launch_copy_blocks(p, stream);
+  if (e != hipSuccess) return hip_fail("block copy kernel launch", e);
+  return record(t_ev_after, stream);
+}
+
 extern "C" padoc_status padoc_tree_attn_bwd(const padoc_plan* plan, const void* q, const void* k, const void* v,
                                             const void* o, const float* lse, const void* dout, void* dq, void* dk,
                                             void* dv, void* workspace, size_t workspace_bytes, hipStream_t stream) {
@@ -435,13 +590,16 @@ extern "C" void padoc_plan_destroy(padoc_plan* plan) {
   delete plan;
 }
 
+namespace padoc {
+namespace {
 // One step of a decode session: upload the step's slot list, block-table
-// patches and schedule in one copy, append the new K/V rows (and patch the
-// table), then the attention kernels.
-extern "C" padoc_status padoc_session_launch(padoc_session* s, const void* q, const void* k_new, const void* v_new,
-                                             void* o, float* lse, void* workspace, size_t workspace_bytes,
-                                             hipStream_t stream) {
-  clear_error();
+// patches, block copies and schedule in one copy, copy the blocks, append the
+// new K/V rows (and patch the table), then the attention kernels.  With
+// `rotary`, the rows come from `rows` and are normed and rotated on the way;
+// q, k_new and v_new are then null.
+padoc_status launch_step(padoc_session* s, const void* q, const void* k_new, const void* v_new,
+                         const padoc_rotary* rotary, const padoc_rotary_append_args* rows, void* o, float* lse,
+                         void* workspace, size_t workspace_bytes, hipStream_t stream) {
   if (!s) return set_error(PADOC_ERR_ARG, "session is null");
   if (!s->prepared) return set_error(PADOC_ERR_MODE, "no step is prepared");
   const padoc_session_desc& d = s->desc;
@@ -451,7 +609,20 @@ extern "C" padoc_status padoc_session_launch(padoc_session* s, const void* q, co
     return set_error(PADOC_ERR_ARG, "the caches must be 16-byte aligned");
   const int64_t n_new = s->new_off.back(), n_q = s->q_off.back();
   const size_t esz = d.dtype == PADOC_BF16 ? 2 : 4;
-  if (n_new > 0 && (!k_new || !v_new)) return set_error(PADOC_ERR_ARG, "k_new / v_new is null");
+  if (rows) {
+    if (rotary->D != d.head_dim || rows->num_heads_q != d.num_heads_q || rows->num_heads_kv != d.num_heads_kv)
+      return set_error(PADOC_ERR_SHAPE, "the rotary's head_dim or the rows' head counts are not the session's");
+    if (rotary->dtype != d.dtype) return set_error(PADOC_ERR_DTYPE, "the rotary's dtype is not the session's");
+    if (rows->n_q != n_q || rows->n_new != n_new)
+      return set_error(PADOC_ERR_BOUNDS, "%lld query rows and %lld new rows, the prepared step has %lld and %lld",
+                       (long long)rows->n_q, (long long)rows->n_new, (long long)n_q, (long long)n_new);
+    if (n_q > 0 && ((d.num_heads_q > 1 && rows->q_out.head_stride != d.head_dim) ||
+                    (n_q > 1 && rows->q_out.row_stride != (int64_t)d.num_heads_q * d.head_dim)))
+      return set_error(PADOC_ERR_BOUNDS, "q_out must be contiguous");
+    q = rows->q_out.data;
+  } else if (n_new > 0 && (!k_new || !v_new)) {
+    return set_error(PADOC_ERR_ARG, "k_new / v_new is null");
+  }
   if (((uintptr_t)k_new | (uintptr_t)v_new) & (esz - 1))
     return set_error(PADOC_ERR_ARG, "k_new / v_new are not aligned to their element size");
   const padoc_plan* P = &s->plan;
@@ -493,6 +664,7 @@ extern "C" padoc_status padoc_session_launch(padoc_session* s, const void* q, co
     char* h = static_cast<char*>(s->stage[k]);
     if (n_new > 0) std::memcpy(h, s->new_slot.data(), (size_t)n_new * 8);
     if (n_patch > 0) std::memcpy(h + s->off_patch, s->patch.data(), (size_t)n_patch * 8);
+    if (!s->copy_pairs.empty()) std::memcpy(h + s->off_copy, s->copy_pairs.data(), s->copy_pairs.size() * 4);
     if (!P->blob.empty()) std::memcpy(h + s->ws_records, P->blob.data(), P->blob.size());
     e = copy_pinned(ws, h, up, stream);
     if (e != hipSuccess) return hip_fail("copy of the step's records", e);
@@ -507,7 +679,26 @@ extern "C" padoc_status padoc_session_launch(padoc_session* s, const void* q, co
     e = hipEventRecord(t_ev_before, stream);
     if (e != hipSuccess) return hip_fail("hipEventRecord", e);
   }
-  if (n_new > 0 || n_patch > 0) {
+  for (size_t ph = 0; ph + 1 < s->copy_ptr.size(); ++ph) {
+    const int32_t c0 = s->copy_ptr[ph];
+    const CopyParams cp{d.k_cache, d.v_cache, d.k_cache, d.v_cache, at<int32_t>(ws, s->off_copy) + 2 * (int64_t)c0,
+                        s->copy_ptr[ph + 1] - c0, d.num_blocks, d.num_blocks,
+                        (int64_t)d.num_heads_kv * d.head_dim * (int64_t)esz};
+    e = launch_copy_blocks(cp, stream);
+    if (e != hipSuccess) return hip_fail("block copy kernel launch", e);
+  }
+  if (rows) {
+    RotaryParams rp = append_params(rotary, rows);
+    rp.slots = at<int32_t>(ws, 0);
+    rp.k_cache = d.k_cache;
+    rp.v_cache = d.v_cache;
+    rp.n_blocks = d.num_blocks;
+    rp.patch = at<int32_t>(ws, s->off_patch);
+    rp.n_patch = n_patch;
+    rp.block_table = d.block_table;
+    e = launch_rotary_append(rp, rotary->D, d.dtype == PADOC_BF16, rotary->style == PADOC_ROTARY_PAIRS, stream);
+    if (e != hipSuccess) return hip_fail("rotary append kernel launch", e);
+  } else if (n_new > 0 || n_patch > 0) {
     e = launch_append_kv(k_new, v_new, d.k_cache, d.v_cache, at<int32_t>(ws, 0), n_new, d.num_heads_kv, d.head_dim,
                          d.dtype == PADOC_BF16, at<int32_t>(ws, s->off_patch), n_patch, d.block_table, stream);
     if (e != hipSuccess) return hip_fail("append kernel launch", e);
@@ -520,6 +711,24 @@ extern "C" padoc_status padoc_session_launch(padoc_session* s, const void* q, co
     if (e != hipSuccess) return hip_fail("hipEventRecord", e);
   }
   return PADOC_OK;
+}
+}  // namespace
+}  // namespace padoc
+
+extern "C" padoc_status padoc_session_launch(padoc_session* s, const void* q, const void* k_new, const void* v_new,
+                                             void* o, float* lse, void* workspace, size_t workspace_bytes,
+                                             hipStream_t stream) {
+  clear_error();
+  return launch_step(s, q, k_new, v_new, nullptr, nullptr, o, lse, workspace, workspace_bytes, stream);
+}
+
+extern "C" padoc_status padoc_session_launch_rotary(padoc_session* s, const padoc_rotary* rotary,
+                                                    const padoc_rotary_append_args* rows, void* o, float* lse,
+                                                    void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  clear_error();
+  const padoc_status st = check_rotary_append(rotary, rows, /*session=*/true);
+  if (st != PADOC_OK) return st;
+  return launch_step(s, nullptr, nullptr, nullptr, rotary, rows, o, lse, workspace, workspace_bytes, stream);
 }
 
 extern "C" void padoc_session_destroy(padoc_session* s) {

@@ -53,6 +53,37 @@ void erase_sorted(std::vector<int32_t>& v, int32_t id) {
   if (it != v.end() && *it == id) v.erase(it);
 }
 
+int32_t take_block(padoc_session* s) {
+  const int32_t b = s->free_blocks.back();
+  s->free_blocks.pop_back();
+  s->block_refs[b] = 1;
+  return b;
+}
+
+void drop_block(padoc_session* s, int32_t b) {
+  if (--s->block_refs[b] == 0) s->free_blocks.push_back(b);
+}
+
+// Copy block src to dst in the next launch, after the copies before it that
+// write src or dst or read dst.  `grow` was called for it.
+void add_copy(padoc_session* s, int32_t src, int32_t dst) {
+  const int32_t phase = std::max({0, s->write_phase[src] + 1, s->write_phase[dst] + 1, s->read_phase[dst] + 1});
+  s->write_phase[dst] = phase;
+  s->read_phase[src] = std::max(s->read_phase[src], phase);
+  s->pending_copies.push_back({src, dst, phase});
+}
+
+template <class V>
+void grow(V& v, size_t more) {  // room for `more` entries, at least doubling
+  if (v.capacity() - v.size() < more) v.reserve(std::max(v.size() + more, 2 * v.size()));
+}
+
+// Whether a step that appends to stream x has to copy its last block first,
+// when `copied` other streams of the step already do.
+bool shares_last_block(const padoc_session* s, const padoc_session::Stream& x, int32_t copied) {
+  return x.len % kBlk != 0 && s->block_refs[x.blocks.back()] - copied > 1;
+}
+
 // Release `id` and then its ancestors while they are closed and have no kept
 // child: blocks back to the pool, region back to its free list.
 void release_upwards(padoc_session* s, int32_t id) {
@@ -60,7 +91,7 @@ void release_upwards(padoc_session* s, int32_t id) {
     padoc_session::Stream& x = s->st[id];
     if (x.open || !x.kept || x.kept_children > 0) return;
     x.kept = false;
-    for (auto it = x.blocks.rbegin(); it != x.blocks.rend(); ++it) s->free_blocks.push_back(*it);
+    for (auto it = x.blocks.rbegin(); it != x.blocks.rend(); ++it) drop_block(s, *it);
     x.blocks.clear();
     x.blocks.shrink_to_fit();
     if (x.cls >= 0) free_region(s, x.cls, x.bt_off);
@@ -80,6 +111,23 @@ padoc_status check_unprepared(const padoc_session* s) {
   if (s->prepared)
     return set_error(PADOC_ERR_MODE, "a prepared step has not been launched or committed");
   return PADOC_OK;
+}
+
+// The pending copies by phase, into copy_ptr and copy_pairs (which have room).
+void order_copies(padoc_session* s) {
+  std::stable_sort(s->pending_copies.begin(), s->pending_copies.end(),
+                   [](const padoc_session::Copy& a, const padoc_session::Copy& b) { return a.phase < b.phase; });
+  s->copy_ptr.clear();
+  s->copy_pairs.clear();
+  int32_t phase = -1;
+  for (const padoc_session::Copy& c : s->pending_copies) {
+    for (; phase < c.phase; ++phase) s->copy_ptr.push_back((int32_t)(s->copy_pairs.size() / 2));
+    s->copy_pairs.push_back(c.src);
+    s->copy_pairs.push_back(c.dst);
+    s->write_phase[c.src] = s->write_phase[c.dst] = s->read_phase[c.src] = s->read_phase[c.dst] = -1;
+  }
+  s->copy_ptr.push_back((int32_t)(s->copy_pairs.size() / 2));
+  s->pending_copies.clear();
 }
 
 // The step's tree: every kept stream in id order with its length after the
@@ -153,6 +201,10 @@ extern "C" padoc_status padoc_session_create(const padoc_session_desc* d, padoc_
     s->free_blocks.resize((size_t)d->num_blocks);
     for (int64_t i = 0; i < d->num_blocks; ++i) s->free_blocks[(size_t)i] = (int32_t)(d->num_blocks - 1 - i);
     s->bt_host.assign((size_t)d->block_table_capacity, -1);
+    s->block_refs.assign((size_t)d->num_blocks, 0);
+    s->write_phase.assign((size_t)d->num_blocks, -1);
+    s->read_phase.assign((size_t)d->num_blocks, -1);
+    s->taken.assign((size_t)d->num_blocks, 0);
     *out = s.release();
   } catch (const std::bad_alloc&) {
     return set_error(PADOC_ERR_ARG, "out of host memory creating the session");
@@ -203,6 +255,177 @@ extern "C" padoc_status padoc_session_close(padoc_session* s, int32_t id) {
   return PADOC_OK;
 }
 
+extern "C" padoc_status padoc_session_clone(padoc_session* s, int32_t id, int32_t len, int32_t* new_id) {
+  clear_error();
+  padoc_status st = check_session(s);
+  if (st != PADOC_OK) return st;
+  if ((st = check_unprepared(s)) != PADOC_OK) return st;
+  if (!new_id) return set_error(PADOC_ERR_ARG, "new_id is null");
+  if (id < 0 || id >= (int32_t)s->st.size() || !s->st[id].kept)
+    return set_error(PADOC_ERR_ARG, "stream %d is not a kept stream of this session", id);
+  if (len < 0 || len > s->st[id].len)
+    return set_error(PADOC_ERR_TREE, "len %d outside [0, %d] (stream %d)", len, s->st[id].len, id);
+  if ((int64_t)s->st.size() >= kI32Max) return set_error(PADOC_ERR_ARG, "too many streams");
+  const int64_t nb = ceil_div(len, kBlk);
+  try {
+    const padoc_session::Stream& from = s->st[id];
+    padoc_session::Stream x;
+    x.parent = from.parent;
+    x.fork = from.fork;
+    x.len = len;
+    x.blocks.assign(from.blocks.begin(), from.blocks.begin() + nb);
+    grow(s->st, 1);  // from here on nothing throws
+    grow(s->open_ids, 1);
+    grow(s->kept_ids, 1);
+    grow(s->pending_entries, (size_t)nb);
+    if (nb > 0) {
+      const int32_t cls = class_for(nb);
+      if (!alloc_region(s, cls, x.bt_off))
+        return set_error(PADOC_ERR_BOUNDS, "the block table (%lld entries) cannot hold the clone",
+                         (long long)s->desc.block_table_capacity);
+      x.cls = cls;
+    }
+    for (int64_t j = 0; j < nb; ++j) {
+      ++s->block_refs[x.blocks[(size_t)j]];
+      s->bt_host[(size_t)(x.bt_off + j)] = x.blocks[(size_t)j];
+      s->pending_entries.push_back(x.bt_off + j);
+    }
+    const int32_t nid = (int32_t)s->st.size();
+    if (x.parent >= 0) ++s->st[x.parent].kept_children;
+    s->st.push_back(std::move(x));
+    s->open_ids.push_back(nid);
+    s->kept_ids.push_back(nid);
+    *new_id = nid;
+  } catch (const std::bad_alloc&) {
+    return set_error(PADOC_ERR_ARG, "out of host memory");
+  }
+  return PADOC_OK;
+}
+
+extern "C" padoc_status padoc_session_truncate(padoc_session* s, int32_t id, int32_t len) {
+  clear_error();
+  padoc_status st = check_session(s);
+  if (st != PADOC_OK) return st;
+  if ((st = check_unprepared(s)) != PADOC_OK) return st;
+  if (id < 0 || id >= (int32_t)s->st.size() || !s->st[id].open)
+    return set_error(PADOC_ERR_ARG, "stream %d is not open", id);
+  padoc_session::Stream& x = s->st[id];
+  if (len < 0 || len > x.len) return set_error(PADOC_ERR_TREE, "len %d outside [0, %d] (stream %d)", len, x.len, id);
+  if (x.kept_children > 0)
+    for (int32_t c : s->kept_ids)
+      if (s->st[c].parent == id && s->st[c].fork > len)
+        return set_error(PADOC_ERR_TREE, "stream %d sees %d tokens of stream %d, more than %d", c, s->st[c].fork, id,
+                         len);
+  const size_t nb = (size_t)ceil_div(len, kBlk);
+  for (size_t j = x.blocks.size(); j > nb; --j) {
+    drop_block(s, x.blocks[j - 1]);  // (free_blocks has held every block of the pool: no allocation)
+    s->bt_host[(size_t)x.bt_off + j - 1] = -1;
+  }
+  x.blocks.resize(nb);
+  x.len = len;
+  return PADOC_OK;
+}
+
+extern "C" padoc_status padoc_session_compact(padoc_session* s, int32_t max_moves, int32_t* n_moves) {
+  clear_error();
+  padoc_status st = check_session(s);
+  if (st != PADOC_OK) return st;
+  if ((st = check_unprepared(s)) != PADOC_OK) return st;
+  if (max_moves < 0) return set_error(PADOC_ERR_ARG, "max_moves = %d is negative", max_moves);
+  try {
+    const int32_t n = (int32_t)s->desc.num_blocks;
+    const int32_t used = n - (int32_t)s->free_blocks.size();
+    // The moves: the i-th largest kept id to the i-th smallest free one.
+    std::vector<int32_t> to((size_t)n, -1);
+    std::vector<std::pair<int32_t, int32_t>> moves;
+    for (int32_t dst = 0, src = n - 1; max_moves == 0 || (int32_t)moves.size() < max_moves; ++dst, --src) {
+      while (dst < used && s->block_refs[dst] > 0) ++dst;
+      if (dst >= used) break;
+      while (s->block_refs[src] == 0) --src;  // (a free id below `used` leaves a kept one behind it)
+      moves.push_back({src, dst});
+      to[src] = dst;
+    }
+    int64_t entries = 0;
+    for (int32_t id : s->kept_ids)
+      for (int32_t b : s->st[id].blocks) entries += to[b] >= 0;
+    grow(s->pending_entries, (size_t)entries);  // from here on nothing throws
+    grow(s->pending_copies, moves.size());
+    for (const auto& m : moves) {
+      add_copy(s, m.first, m.second);
+      s->block_refs[m.second] = s->block_refs[m.first];
+      s->block_refs[m.first] = 0;
+    }
+    if (!moves.empty())
+      for (int32_t id : s->kept_ids) {
+        padoc_session::Stream& x = s->st[id];
+        for (size_t j = 0; j < x.blocks.size(); ++j) {
+          if (to[x.blocks[j]] < 0) continue;
+          x.blocks[j] = to[x.blocks[j]];
+          const int64_t e = x.bt_off + (int64_t)j;
+          s->bt_host[(size_t)e] = x.blocks[j];
+          s->pending_entries.push_back(e);
+        }
+      }
+    s->free_blocks.clear();
+    for (int32_t b = n - 1; b >= 0; --b)
+      if (s->block_refs[b] == 0) s->free_blocks.push_back(b);
+    if (n_moves) *n_moves = (int32_t)moves.size();
+  } catch (const std::bad_alloc&) {
+    return set_error(PADOC_ERR_ARG, "out of host memory");
+  }
+  return PADOC_OK;
+}
+
+extern "C" padoc_status padoc_session_resize(padoc_session* s, int64_t num_blocks, void* k_cache, void* v_cache) {
+  clear_error();
+  padoc_status st = check_session(s);
+  if (st != PADOC_OK) return st;
+  if ((st = check_unprepared(s)) != PADOC_OK) return st;
+  if (num_blocks < 0 || num_blocks > kI32Max)
+    return set_error(PADOC_ERR_ARG, "num_blocks=%lld must be in [0, 2^31-1]", (long long)num_blocks);
+  if (!s->pending_copies.empty())
+    return set_error(PADOC_ERR_MODE, "block copies wait for the launch of a step");
+  if ((k_cache != nullptr) != (s->desc.k_cache != nullptr) || (v_cache != nullptr) != (s->desc.v_cache != nullptr))
+    return set_error(PADOC_ERR_ARG, "a session has device caches or none, from its creation on");
+  const int64_t old = s->desc.num_blocks;
+  for (int64_t b = num_blocks; b < old; ++b)
+    if (s->block_refs[(size_t)b] > 0)
+      return set_error(PADOC_ERR_BOUNDS, "block %lld is in use, behind the %lld blocks of the new pool", (long long)b,
+                       (long long)num_blocks);
+  try {
+    std::vector<int32_t> free_blocks;
+    free_blocks.reserve((size_t)num_blocks);
+    for (int64_t b = num_blocks - 1; b >= old; --b) free_blocks.push_back((int32_t)b);  // taken last
+    for (int32_t b : s->free_blocks)
+      if (b < num_blocks) free_blocks.push_back(b);
+    const size_t n = (size_t)num_blocks;
+    for (std::vector<int32_t>* v : {&s->block_refs, &s->write_phase, &s->read_phase, &s->taken}) v->reserve(n);
+    s->block_refs.resize(n, 0);
+    s->write_phase.resize(n, -1);
+    s->read_phase.resize(n, -1);
+    s->taken.resize(n, 0);
+    s->free_blocks.swap(free_blocks);
+    s->desc.num_blocks = num_blocks;
+    s->desc.k_cache = k_cache;
+    s->desc.v_cache = v_cache;
+  } catch (const std::bad_alloc&) {
+    return set_error(PADOC_ERR_ARG, "out of host memory");
+  }
+  return PADOC_OK;
+}
+
+extern "C" padoc_status padoc_session_copies(const padoc_session* s, int32_t* n_phases, const int32_t** phase_ptr,
+                                             const int32_t** pairs) {
+  clear_error();
+  padoc_status st = check_session(s);
+  if (st != PADOC_OK) return st;
+  if (!n_phases || !phase_ptr || !pairs) return set_error(PADOC_ERR_ARG, "null pointer");
+  *n_phases = s->prepared ? (int32_t)s->copy_ptr.size() - 1 : 0;
+  *phase_ptr = s->prepared ? s->copy_ptr.data() : nullptr;
+  *pairs = s->prepared ? s->copy_pairs.data() : nullptr;
+  return PADOC_OK;
+}
+
 extern "C" padoc_status padoc_session_select(const padoc_session* s, int32_t max_rows, const int64_t* priority,
                                              int32_t* n_new, int32_t* n_query) {
   clear_error();
@@ -240,7 +463,7 @@ extern "C" padoc_status padoc_session_prepare(padoc_session* s, const int32_t* n
     if (!n_new_in || !n_query_in) ones.assign(R, 1);
     const int32_t* n_new = n_new_in ? n_new_in : ones.data();
     const int32_t* n_query = n_query_in ? n_query_in : ones.data();
-    int64_t total_new = 0, total_q = 0, need_blocks = 0;
+    int64_t total_new = 0, total_q = 0, need_blocks = 0, n_shared = 0;
     for (size_t i = 0; i < R; ++i) {
       const padoc_session::Stream& x = s->st[s->open_ids[i]];
       if (n_new[i] < 0 || n_query[i] < 0 || n_query[i] > n_new[i])
@@ -250,6 +473,21 @@ extern "C" padoc_status padoc_session_prepare(padoc_session* s, const int32_t* n
       total_q += n_query[i];
       need_blocks += ceil_div((int64_t)x.len + n_new[i], kBlk) - (int64_t)x.blocks.size();
     }
+    // Streams that append to a block others hold copy it, all but the last of
+    // a block's holders.
+    for (size_t i = 0; i < R; ++i) {
+      const padoc_session::Stream& x = s->st[s->open_ids[i]];
+      if (n_new[i] > 0 && x.len % kBlk != 0 && shares_last_block(s, x, s->taken[x.blocks.back()])) {
+        ++s->taken[x.blocks.back()];
+        ++n_shared;
+      }
+    }
+    if (n_shared > 0)
+      for (size_t i = 0; i < R; ++i) {
+        const padoc_session::Stream& x = s->st[s->open_ids[i]];
+        if (!x.blocks.empty()) s->taken[x.blocks.back()] = 0;
+      }
+    need_blocks += n_shared;
     if (total_new > kI32Max || total_q > kI32Max) return set_error(PADOC_ERR_BOUNDS, "step exceeds 2^31-1 rows");
     if (need_blocks > (int64_t)s->free_blocks.size())
       return set_error(PADOC_ERR_BOUNDS, "the step needs %lld blocks, the pool has %zu free", (long long)need_blocks,
@@ -303,6 +541,10 @@ extern "C" padoc_status padoc_session_prepare(padoc_session* s, const int32_t* n
     }
     // Commit: blocks, regions, patches, slots of the new rows.
     s->new_slot.resize((size_t)total_new * 2);
+    grow(s->pending_copies, (size_t)n_shared);
+    grow(s->pending_entries, (size_t)n_shared);
+    s->copy_ptr.reserve(s->pending_copies.size() + (size_t)n_shared + 1);
+    s->copy_pairs.reserve(2 * (s->pending_copies.size() + (size_t)n_shared));
     s->patch.clear();
     s->row_id.assign(s->open_ids.begin(), s->open_ids.end());
     s->row_n_new.assign(n_new, n_new + R);
@@ -312,6 +554,19 @@ extern "C" padoc_status padoc_session_prepare(padoc_session* s, const int32_t* n
     for (size_t i = 0; i < R; ++i) {
       s->new_off[i + 1] = s->new_off[i] + n_new[i];
       s->q_off[i + 1] = s->q_off[i] + n_query[i];
+    }
+    for (size_t i = 0; n_shared > 0 && i < R; ++i) {
+      padoc_session::Stream& x = s->st[s->open_ids[i]];
+      if (n_new[i] == 0 || x.len % kBlk == 0 || !shares_last_block(s, x, 0)) continue;
+      const int32_t b = take_block(s);
+      add_copy(s, x.blocks.back(), b);
+      --s->block_refs[x.blocks.back()];
+      x.blocks.back() = b;
+      if (x.moving_to < 0) {  // (a moving stream's entries are all written below)
+        const int64_t e = x.bt_off + (int64_t)x.blocks.size() - 1;
+        s->bt_host[(size_t)e] = b;
+        s->pending_entries.push_back(e);
+      }
     }
     for (const Move& m : moves) {
       padoc_session::Stream& x = s->st[m.id];
@@ -329,8 +584,7 @@ extern "C" padoc_status padoc_session_prepare(padoc_session* s, const int32_t* n
       padoc_session::Stream& x = s->st[s->open_ids[i]];
       const int64_t nb = ceil_div((int64_t)x.len + n_new[i], kBlk);
       while ((int64_t)x.blocks.size() < nb) {
-        const int32_t b = s->free_blocks.back();
-        s->free_blocks.pop_back();
+        const int32_t b = take_block(s);
         const int64_t e = x.bt_off + (int64_t)x.blocks.size();
         x.blocks.push_back(b);
         s->bt_host[(size_t)e] = b;
@@ -345,8 +599,24 @@ extern "C" padoc_status padoc_session_prepare(padoc_session* s, const int32_t* n
       }
       x.len += n_new[i];
     }
+    // Entries that clones, compactions and copies left to write, each once,
+    // as they are now (free ones stay); what this step patches above is not
+    // among them, or the same.
+    if (!s->pending_entries.empty()) {
+      std::sort(s->pending_entries.begin(), s->pending_entries.end());
+      s->pending_entries.erase(std::unique(s->pending_entries.begin(), s->pending_entries.end()),
+                               s->pending_entries.end());
+      for (int64_t e : s->pending_entries)
+        if (s->bt_host[(size_t)e] >= 0) {
+          s->patch.push_back((int32_t)e);
+          s->patch.push_back(s->bt_host[(size_t)e]);
+        }
+      s->pending_entries.clear();
+    }
+    order_copies(s);
     s->off_patch = align256((size_t)total_new * 8);
-    s->rec_bytes = s->off_patch + s->patch.size() * 4;
+    s->off_copy = align256(s->off_patch + s->patch.size() * 4);
+    s->rec_bytes = s->off_copy + s->copy_pairs.size() * 4;
     s->ws_records = align256(s->rec_bytes);
     s->ws_bytes = s->ws_records + s->plan.ws_bytes;
     s->prepared = true;

@@ -33,13 +33,29 @@ struct padoc_session {
   int64_t bt_top = 0;                       // table entries handed out so far
   std::vector<int32_t> bt_host;             // host copy of the device table
 
+  // Streams that hold each pool block (0: free).  A clone shares its blocks;
+  // prepare copies a shared block before a stream appends to it.
+  std::vector<int32_t> block_refs;
+  // Block copies the next launch makes, with the phase each can run in at the
+  // earliest (0: the caches as they are), and the phases that last write and
+  // read each block (-1: none).
+  struct Copy {
+    int32_t src, dst, phase;
+  };
+  std::vector<Copy> pending_copies;
+  std::vector<int32_t> write_phase, read_phase;
+  std::vector<int64_t> pending_entries;  // block-table entries to write in the next launch
+
   // The prepared step.
   bool prepared = false;
   padoc_plan plan;
   std::vector<padoc_segment> seg;
   std::vector<int32_t> seg_id, row_id, new_off, q_off, new_slot, patch;
   std::vector<int32_t> row_n_new;
-  size_t off_patch = 0, rec_bytes = 0;  // workspace: slots at 0, patches at off_patch
+  std::vector<int32_t> copy_ptr, copy_pairs;  // per phase (copy_ptr: phases + 1), (source, destination)
+  std::vector<int32_t> taken;           // scratch of prepare: shared blocks' streams that copy it
+  size_t off_patch = 0, off_copy = 0;   // workspace: slots at 0, patches, copies
+  size_t rec_bytes = 0;
   size_t ws_records = 0, ws_bytes = 0;  // records area (aligned), total
 
   // Launch side: two pinned staging buffers and the events of their last

@@ -1,0 +1,212 @@
+"""The operators together, as they are used: a training step (norm and rotate,
+packed forward, its backward, the rotation's backward) and a served page (raw
+rows into a session's steps, streams cloned, truncated, closed, the pool
+compacted and resized between them), against the oracle at every step."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from oracle import dense as od
+import padoc_synth as syn
+import paper_2608_06146_amd as pa
+from _cases import compare
+from _rotary import Setup, check, f64, normal, positions
+
+pytestmark = pytest.mark.gpu
+
+
+def test_a_training_step():
+    hq, hkv, d = 8, 2, 128
+    pages = [syn.Page(70, 70, 20, 20, (syn.Branch(5, 33, 33), syn.Branch(20, 9, 9))),
+             syn.Page(40, 40, 7, 7, (syn.Branch(7, 12, 12),))]
+    nodes, segs, n = od.page_nodes(pages), pa.segments_from_pages(pages, 0), syn.count_tokens(pages)
+    plan = pa.TreePlan(segs, hq, hkv, d, "bf16", 0, num_kv_rows=n, num_q_rows=n)
+    st, scale = Setup(d, "bf16", base=1e6), 1.0 / math.sqrt(d)
+    qkv = normal((n, (hq + 2 * hkv), d), 1, "bf16")
+    q, k, v = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
+    pos, wq, wk, g = positions(3, n, 2), normal((d,), 3, "bf16"), normal((d,), 4, "bf16"), normal((n, hq, d), 5, "bf16")
+    print(f"[case] training step, {n} tokens", flush=True)
+    zq, zk = pa.rotary_fwd(q, k, pos, st.handle, wq, wk)
+    check("q", zq, *st.forward(q, pos, wq))
+    check("k", zk, *st.forward(k, pos, wk))
+    vc = v.contiguous()
+    o, lse = pa.tree_attn_fwd(zq, zk, vc, plan)
+    O, L = oracle.tree_attention(nodes, zq, zk, vc, scale, hq, hkv)
+    compare("attention", o, lse, O, L, "bf16")
+    dzq, dzk, dv = pa.tree_attn_bwd(zq, zk, vc, o, lse, g, plan)
+    # The backward takes probabilities from the stored LSE: those of the exact
+    # one times c = exp(LSE exact - stored), row by row.  P, and with it dS = P
+    # (dP - D), then stand c times as large: as if dO were.
+    _, _, P = oracle.tree_attention(nodes, zq, zk, vc, scale, hq, hkv, return_probs=True)
+    c = np.exp(L - f64(lse))[..., None]
+    g64, o64, grp = f64(g), f64(o), hq // hkv
+    ref = oracle.tree_attention_backward(nodes, zq, zk, vc, g64 * c, scale, hq, hkv, o=o)
+    # P and dS are rounded to bf16 (2^-8 of each) before they are multiplied; a
+    # quarter of that more holds P's fp32 error (scores off by 130 u of 64 or
+    # so), 2^-16 >= 130 u that of dP - D.  Results are rounded by 2^-8.
+    K, V, Q = (np.repeat(f64(x), grp, 1) if x is not zq else f64(x) for x in (zk, vc, zq))
+    D = (g64 * o64).sum(-1)[..., None]
+    dP, dPmag = np.einsum("ihd,jhd->ihj", g64, V), np.einsum("ihd,jhd->ihj", np.abs(g64), np.abs(V))
+    e = P * c * (1.25 * 2 ** -8 * np.abs(dP - D) + 2 ** -16 * (dPmag + (np.abs(g64 * o64)).sum(-1)[..., None]))
+    heads = lambda x: x.reshape(n, hkv, grp, d).sum(2)  # noqa: E731
+    tols = (scale * np.einsum("ihj,jhd->ihd", e, np.abs(K)), heads(scale * np.einsum("ihj,ihd->jhd", e, np.abs(Q))),
+            heads(1.25 * 2 ** -8 * np.einsum("ihj,ihd->jhd", P * c, np.abs(g64))))
+    for name, x, r, tol in zip(("dq", "dk", "dv"), (dzq, dzk, dv), ref, tols):
+        check(name, x, r, tol + 2 ** -8 * (np.abs(r) + tol))
+    dqkv = torch.zeros_like(qkv)
+    dq, dk, dwq, dwk = pa.rotary_bwd(dzq, dzk, pos, st.handle, q, k, wq, wk, dq=dqkv[:, :hq], dk=dqkv[:, hq:hq + hkv])
+    for dx, dw, dz, x, w in ((dq, dwq, dzq, q, wq), (dk, dwk, dzk, k, wk)):
+        want, tol, dwant, dtol = st.backward(dz, x, pos, w)
+        check("dx", dx, want, tol)
+        check("dw", dw, dwant, dtol)
+    assert not dqkv[:, hq + hkv:].any()
+
+
+class Server:
+    """A session and the test's own record of every stream's raw rows."""
+
+    def __init__(self, hq, hkv, d, dtype, blocks, style):
+        self.hq, self.hkv, self.d, self.dtype = hq, hkv, d, dtype
+        self.st = Setup(d, dtype, style=style, base=1e6)
+        t = normal((1,), 0, dtype).dtype
+        self.kc = torch.full((blocks, hkv, d // 8, 16, 8), float("nan"), dtype=t, device="cuda")
+        self.vc = torch.full((blocks, hkv, d, 16), float("nan"), dtype=t, device="cuda")
+        table = torch.full((1024,), -1, dtype=torch.int32, device="cuda")
+        self.s = pa.DecodeSession(hq, hkv, d, blocks, dtype, self.kc, self.vc, table)
+        self.wq, self.wk = normal((d,), 1, dtype), normal((d,), 2, dtype)
+        self.rows = {}  # stream -> (k [len, Hkv, d] raw, v, positions [3, len])
+        self.seed = 10
+
+    def open(self, parent=-1, fork=0):
+        i = self.s.open(parent, fork)
+        z = torch.empty((0, self.hkv, self.d), dtype=self.kc.dtype, device="cuda")
+        self.rows[i] = (z, z, torch.empty((3, 0), dtype=torch.int32, device="cuda"))
+        return i
+
+    def clone(self, i, n=None):
+        c = self.s.clone(i, n)
+        n = len(self.rows[i][0]) if n is None else n
+        k, v, p = self.rows[i]
+        self.rows[c] = (k[:n], v[:n], p[:, :n])
+        return c
+
+    def truncate(self, i, n):
+        self.s.truncate(i, n)
+        k, v, p = self.rows[i]
+        self.rows[i] = (k[:n], v[:n], p[:, :n])
+
+    def step(self, n_new=None, n_query=None):
+        """One step; returns the block copies of its phases."""
+        nk, nq, _ = self.s.prepare(n_new, n_query)
+        view, copies = self.s.view(), self.s.copies()
+        self.seed += 10
+        w = self.hq + 2 * self.hkv
+        x = normal((max(nk, 1), w, self.d), self.seed, self.dtype)[:nk]
+        q, k, v = x[:, :self.hq], x[:, self.hq:self.hq + self.hkv], x[:, self.hq + self.hkv:]
+        pos = positions(3, nk, self.seed + 1, 2000)
+        at = []
+        for i, a, b, qa, qb in zip(view["row_id"], view["new_off"], view["new_off"][1:], view["q_off"], view["q_off"][1:]):
+            ko, vo, po = self.rows[int(i)]
+            self.rows[int(i)] = (torch.cat([ko, k[a:b]]), torch.cat([vo, v[a:b]]), torch.cat([po, pos[:, a:b]], 1))
+            at += range(b - (qb - qa), b)
+        every = nq == nk
+        print(f"[case] step of {nk} rows, {nq} queries, copies {[len(c) for c in copies]}", flush=True)
+        q, qpos = (q, None) if every else (q[at].contiguous(), pos[:, at].contiguous())
+        o, lse = self.s.launch_rotary(q, k, v, pos, self.st.handle, self.wq, self.wk, q_positions=qpos)
+        torch.cuda.synchronize()
+        if nq:
+            nodes = [(int(g["parent"]), int(g["fork"]), int(g["len"]), int(g["q_len"])) for g in view["seg"]]
+            rows = [self.rows[int(i)] for i in view["seg_id"]]
+            assert [n[2] for n in nodes] == [len(r[0]) for r in rows]
+            K, V, P = (torch.cat([r[j] for r in rows], 1 if j == 2 else 0) for j in range(3))
+            zk, _ = self.st.forward(K, P, self.wk)
+            zq, _ = self.st.forward(q, pos if every else qpos, self.wq)
+            as_stored = lambda z: torch.from_numpy(z).to(self.kc.dtype)  # noqa: E731
+            O, L = oracle.tree_attention(nodes, as_stored(zq), as_stored(zk), V, 1 / math.sqrt(self.d), self.hq, self.hkv)
+            if self.dtype == "bf16":
+                compare("step", o, lse, O, L, "bf16")
+            else:  # q and k rounded to fp32 twice (here and there): 2^-24 of 64 products of order 8, before the 1e-5 of the step
+                assert np.abs(f64(o) - O).max() <= 1e-4 and np.abs(f64(lse) - L).max() <= 1e-4
+        return [len(c) for c in copies]
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,d,style", [("bf16", 8, 2, 128, "halves"), ("f32", 4, 2, 64, "pairs")])
+def test_a_served_page(dtype, hq, hkv, d, style):
+    s = Server(hq, hkv, d, dtype, 60, style)
+    root, other = s.open(), s.open()
+    s.step([75, 33], [0, 0])                       # two prefixes
+    lay = s.open(root, 75)
+    second = s.open(other, 33)
+    s.s.close(root), s.s.close(other)
+    s.step([21, 5], [21, 5])
+    a = s.open(lay, 10)
+    b = s.open(lay, 21)
+    s.step([1, 1, 7, 12], [1, 1, 3, 12])           # fewer queries than tokens
+    c = s.clone(b)                                  # sampled alternatives of a branch
+    e = s.clone(b, 9)
+    assert s.step() == [2]                          # b and c copy the block that e keeps
+    assert s.step() == []
+    s.truncate(a, 2)
+    s.s.close(second)
+    moves = s.s.compact()
+    assert moves > 0
+    f = s.clone(c)
+    copies = s.step()
+    assert len(copies) == 2 and copies[0] >= moves  # moved, then copied for its second stream
+    kept = 60 - s.s.view()["free_blocks"]
+    s.s.resize(kept + 4, s.kc[:kept + 4], s.vc[:kept + 4])
+    s.kc[kept + 4:].fill_(float("nan"))
+    s.step()
+    # larger caches that the caller copies to, whole blocks
+    old = kept + 4
+    ids = np.stack([np.arange(old), np.arange(old)], 1).astype(np.int32)
+    kc = torch.full((80, *s.kc.shape[1:]), float("nan"), dtype=s.kc.dtype, device="cuda")
+    vc = torch.full((80, *s.vc.shape[1:]), float("nan"), dtype=s.kc.dtype, device="cuda")
+    pa.cache_copy_blocks(s.kc[:old], s.vc[:old], torch.from_numpy(ids).cuda(), kc, vc, pairs_host=ids)
+    s.s.resize(80, kc, vc)
+    s.kc, s.vc = kc, vc
+    s.step([40, 1, 0, 1, 30, 1], [40, 1, 0, 1, 2, 1])
+    for i in (lay, a, b, c, e, f):
+        s.s.close(i)
+    assert s.s.view()["free_blocks"] == 80
+
+
+def test_copies_run_before_a_plain_launch_too():
+    """A session whose rows come rotated already."""
+    s = Server(8, 2, 128, "bf16", 20, "halves")
+    a = s.s.open()
+    k = normal((19, 2, 128), 1, "bf16")
+    s.s.step(None, k, k, [19], [0])
+    b = s.s.clone(a)
+    q, new = normal((2, 8, 128), 2, "bf16"), normal((2, 2, 128), 3, "bf16")
+    o, lse = s.s.step(q, new, new)
+    torch.cuda.synchronize()
+    for i in range(2):
+        rows = torch.cat([k, new[i:i + 1]])
+        O, L = oracle.tree_attention([(-1, 0, 20, 1)], q[i:i + 1], rows, rows, 1 / math.sqrt(128), 8, 2)
+        compare(f"stream {(a, b)[i]}", o[i:i + 1], lse[i:i + 1], O, L, "bf16")
+
+
+def test_session_refusals():
+    s = Server(8, 2, 128, "bf16", 20, "halves")
+    s.open()
+    s.s.prepare([3], [3])
+    q, k, pos = normal((3, 8, 128), 1, "bf16"), normal((3, 2, 128), 2, "bf16"), positions(3, 3, 1)
+    h = s.st.handle
+    with pytest.raises(TypeError, match="f32"):
+        s.s.launch_rotary(q, k, k, pos, pa.Rotary(128, "f32"))
+    with pytest.raises(ValueError, match="64"):
+        s.s.launch_rotary(q, k, k, pos, pa.Rotary(64, "bf16"))
+    with pytest.raises(ValueError, match="k_new"):
+        s.s.launch_rotary(q, k[:2], k, pos, h)
+    with pytest.raises(ValueError, match="positions"):
+        s.s.launch_rotary(q, k, k, pos[:, :2], h)
+    with pytest.raises(ValueError, match="q_rot must be contiguous"):
+        s.s.launch_rotary(q, k, k, pos, h, q_rot=normal((3, 16, 128), 1, "bf16")[:, :8])
+    assert s.s.view()["prepared"]  # nothing ran
+    s.s.launch_rotary(q, k, k, pos, h)
+    with pytest.raises(pa.PadocError, match="prepared"):
+        s.s.launch_rotary(q, k, k, pos, h)
