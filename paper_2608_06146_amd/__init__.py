@@ -458,6 +458,7 @@ class Rotary:
         h = C.c_void_p()
         _lib.check(_lib.lib().padoc_rotary_create(C.byref(desc), C.byref(h)))
         self._h = h
+        self.torch_dtype = _torch_dtype(self)
 
     @property
     def handle(self):
@@ -480,81 +481,85 @@ class Rotary:
 _NO_HEADS = (0, 0, 0)
 
 
-def _heads(name, t, like, shape=None):
+def _heads(name, t, dt, device, shape):
     """``(data, row stride, head stride)`` of rows of heads ``[n, H, d]`` on
-    the device and of the dtype of ``like``."""
-    if t.device != like.device:
-        raise ValueError(f"{name} is on {t.device}, expected {like.device}")
-    if t.dtype != like.dtype:
-        raise TypeError(f"{name} has dtype {t.dtype}, expected {like.dtype}")
-    if t.dim() != 3 or (shape is not None and t.shape != shape):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {'[n, H, d]' if shape is None else tuple(shape)}")
+    GPU ``device``."""
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, expected cuda:{device}")
+    if t.dtype is not dt:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dt}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     rs, hs, es = t.stride()
     if es != 1:
         raise ValueError(f"{name}: the head dimension must be contiguous")
     return t.data_ptr(), rs, hs
 
 
-def _rows_of(rotary, tensors):
-    """The first tensor given, checked against the handle."""
+def _rows_of(rotary, like):
+    """GPU index and dtype of the rows of a call, by one of their tensors."""
     import torch
-    like = next((t for t in tensors if t is not None), None)
     if not isinstance(like, torch.Tensor):
         raise TypeError("rows must be torch tensors")
-    if not like.is_cuda:
+    device, dt = like.get_device(), rotary.torch_dtype
+    if device < 0:
         raise ValueError(f"rows are on {like.device}, expected a GPU")
-    if like.dtype != _torch_dtype(rotary):
+    if like.dtype is not dt:
         raise TypeError(f"rows have dtype {like.dtype}, the rotary is for {rotary.dtype}")
     if like.dim() != 3 or like.shape[2] != rotary.head_dim:
         raise ValueError(f"rows must be [n, H, {rotary.head_dim}], got {tuple(like.shape)}")
-    return like
+    return device, dt
 
 
-def _weight(name, w, like):
+def _weight(name, w, dt, device, d):
     """Address of a norm's weight ``[d]``, 0 for None."""
     if w is None:
         return 0
-    _check_tensor(name, w, like.dtype, like.device)
-    if w.shape != like.shape[2:]:
-        raise ValueError(f"{name} has shape {tuple(w.shape)}, expected {tuple(like.shape[2:])}")
+    if w.dtype is not dt or w.get_device() != device or not w.is_contiguous():
+        import torch
+        _check_tensor(name, w, dt, torch.device("cuda", device))
+    if w.shape != (d,):
+        raise ValueError(f"{name} has shape {tuple(w.shape)}, expected {(d,)}")
     return w.data_ptr()
 
 
-def _positions(name, pos, rotary, n, like):
+def _positions(name, pos, rotary, n, device):
     """``(address, axis stride)`` of int32 positions ``[n_axes, n]`` (``[n]``
     for one axis)."""
     import torch
-    if pos.device != like.device:
-        raise ValueError(f"{name} is on {pos.device}, expected {like.device}")
-    if pos.dtype != torch.int32:
+    if pos.get_device() != device:
+        raise ValueError(f"{name} is on {pos.device}, expected cuda:{device}")
+    if pos.dtype is not torch.int32:
         raise TypeError(f"{name} has dtype {pos.dtype}, expected torch.int32")
-    if pos.dim() == 1 and rotary.n_axes == 1:
+    axes = rotary.n_axes
+    if axes == 1 and pos.dim() == 1:
         pos = pos[None]
-    if pos.dim() != 2 or pos.shape[0] != rotary.n_axes or pos.shape[1] != n:
-        raise ValueError(f"{name} has shape {tuple(pos.shape)}, expected {(rotary.n_axes, n)}")
-    if n > 1 and pos.stride(1) != 1:
+    if pos.shape != (axes, n):
+        raise ValueError(f"{name} has shape {tuple(pos.shape)}, expected {(axes, n)}")
+    rs, es = pos.stride()
+    if n > 1 and es != 1:
         raise ValueError(f"{name}: the positions of an axis must be contiguous")
-    return pos.data_ptr(), pos.stride(0) if rotary.n_axes > 1 else 0
+    return pos.data_ptr(), rs if axes > 1 else 0
 
 
-def _launch(f, dev, stream, made, *args):
-    """``f(*args, stream)`` on ``dev`` and ``stream`` (None: its current one);
-    tensors that the call ``made`` stay while a stream of the caller's reads
-    them."""
+def _launch(f, device, stream, made, *args):
+    """``f(*args, stream)`` on GPU ``device`` and ``stream`` (None: its current
+    one); tensors that the call ``made`` stay while a stream of the caller's
+    reads them."""
     import torch
     if stream is None:
-        s = torch.cuda.current_stream(dev)
+        s = torch._C._cuda_getCurrentRawStream(device)  # current_stream().cuda_stream, 1.7 us sooner
     else:
-        s = stream
-        if s.device != dev:
-            raise ValueError(f"the stream is on {s.device}, the tensors on {dev}")
+        if stream.device.index != device:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on cuda:{device}")
         for t in made:
-            t.record_stream(s)
-    if dev.index == torch.cuda.current_device():
-        _lib.check(f(*args, s.cuda_stream))
+            t.record_stream(stream)
+        s = stream.cuda_stream
+    if device == torch._C._cuda_getDevice():
+        _lib.check(f(*args, s))
     else:
-        with torch.cuda.device(dev):
-            _lib.check(f(*args, s.cuda_stream))
+        with torch.cuda.device(device):
+            _lib.check(f(*args, s))
 
 
 def rotary_fwd(q, k, positions, rotary: Rotary, q_weight=None, k_weight=None, q_out=None, k_out=None, stream=None):
@@ -563,27 +568,37 @@ def rotary_fwd(q, k, positions, rotary: Rotary, q_weight=None, k_weight=None, q_
     n]``; ``padoc_rotary_fwd``).  Rows and heads may be strided, as in slices
     of a fused projection; q or k may be None, and q_out / k_out may be q / k.
     Returns ``(q_out, k_out)``."""
-    import torch
-    like = _rows_of(rotary, (q, k))
-    n, dev, made = like.shape[0], like.device, []
-    heads, outs, counts = [], [], []
-    for name, x, out in (("q", q, q_out), ("k", k, k_out)):
-        if x is None:
-            heads.append(_NO_HEADS), heads.append(_NO_HEADS), outs.append(None), counts.append(0)
-            continue
-        shape = (n, x.shape[1], rotary.head_dim)
-        heads.append(_heads(name, x, like, shape))
-        if out is None:
-            out = torch.empty(shape, dtype=x.dtype, device=dev)
-            made.append(out)
-        heads.append(_heads(name + "_out", out, like, shape))
-        outs.append(out)
-        counts.append(shape[1])
-    pos = _positions("positions", positions, rotary, n, like)
-    args = _lib.ROTARY_FWD_ARGS.pack(n, counts[0], counts[1], *pos, *heads[0], *heads[2], *heads[1], *heads[3],
-                                     _weight("q_weight", q_weight, like), _weight("k_weight", k_weight, like))
-    _launch(_lib.lib().padoc_rotary_fwd, dev, stream, made, rotary.handle, args)
-    return outs[0], outs[1]
+    like = k if q is None else q
+    device, dt = _rows_of(rotary, like)
+    n, d = like.shape[0], rotary.head_dim
+    hq = hk = 0
+    q_in = q_to = k_in = k_to = _NO_HEADS
+    made = []
+    if q is not None:
+        hq = q.shape[1]
+        shape = (n, hq, d)
+        q_in = _heads("q", q, dt, device, shape)
+        if q_out is None:
+            q_out = q.new_empty(shape)
+            made.append(q_out)
+            q_to = q_out.data_ptr(), hq * d, d
+        else:
+            q_to = _heads("q_out", q_out, dt, device, shape)
+    if k is not None:
+        hk = k.shape[1] if k.dim() == 3 else 0
+        shape = (n, hk, d)
+        k_in = _heads("k", k, dt, device, shape)
+        if k_out is None:
+            k_out = k.new_empty(shape)
+            made.append(k_out)
+            k_to = k_out.data_ptr(), hk * d, d
+        else:
+            k_to = _heads("k_out", k_out, dt, device, shape)
+    args = _lib.ROTARY_FWD_ARGS.pack(n, hq, hk, *_positions("positions", positions, rotary, n, device), *q_in, *k_in,
+                                     *q_to, *k_to, _weight("q_weight", q_weight, dt, device, d),
+                                     _weight("k_weight", k_weight, dt, device, d))
+    _launch(_lib.lib().padoc_rotary_fwd, device, stream, made, rotary.handle, args)
+    return (None if q is None else q_out), (None if k is None else k_out)
 
 
 def rotary_bwd(dq_out, dk_out, positions, rotary: Rotary, q=None, k=None, q_weight=None, k_weight=None, dq=None,
@@ -594,80 +609,86 @@ def rotary_bwd(dq_out, dk_out, positions, rotary: Rotary, q=None, k=None, q_weig
     gradients are float32 ``[d]``, None without a weight or with
     ``weight_grads=False``."""
     import torch
-    like = _rows_of(rotary, (dq_out, dk_out))
-    n, dev, made = like.shape[0], like.device, []
-    heads, outs, counts, ws, dws = [], [], [], [], []
+    like = dk_out if dq_out is None else dq_out
+    device, dt = _rows_of(rotary, like)
+    n, d = like.shape[0], rotary.head_dim
+    made, heads, counts, outs, ws, dws = [], [], [], [], [], []
     for name, g, x, w, out in (("q", dq_out, q, q_weight, dq), ("k", dk_out, k, k_weight, dk)):
         if g is None:
-            heads.append((_NO_HEADS,) * 3), outs.append(None), counts.append(0), ws.append(0), dws.append(None)
+            heads.append((_NO_HEADS,) * 3), counts.append(0), outs.append(None), ws.append(0), dws.append(None)
             continue
-        shape = (n, g.shape[1], rotary.head_dim)
-        hg = _heads(f"d{name}_out", g, like, shape)
-        if w is not None and x is None:
-            raise ValueError(f"the backward of {name}'s norm needs {name}")
-        hx = _heads(name, x, like, shape) if w is not None else _NO_HEADS
+        h = g.shape[1] if g.dim() == 3 else 0
+        shape = (n, h, d)
+        g_in, x_in = _heads(f"d{name}_out", g, dt, device, shape), _NO_HEADS
+        if w is not None:
+            if x is None:
+                raise ValueError(f"the backward of {name}'s norm needs {name}")
+            x_in = _heads(name, x, dt, device, shape)
         if out is None:
-            out = torch.empty(shape, dtype=g.dtype, device=dev)
+            out = g.new_empty(shape)
             made.append(out)
-        heads.append((hg, hx, _heads("d" + name, out, like, shape)))
-        outs.append(out)
-        counts.append(shape[1])
-        ws.append(_weight(name + "_weight", w, like))
-        dws.append(torch.empty(rotary.head_dim, dtype=torch.float32, device=dev) if w is not None and weight_grads else None)
-    made.extend(t for t in dws if t is not None)
-    pos = _positions("positions", positions, rotary, n, like)
-    L, h = _lib.lib(), rotary.handle
+            to = out.data_ptr(), h * d, d
+        else:
+            to = _heads("d" + name, out, dt, device, shape)
+        heads.append((x_in, g_in, to)), counts.append(h), outs.append(out)
+        ws.append(_weight(name + "_weight", w, dt, device, d))
+        dws.append(g.new_empty(d, dtype=torch.float32) if w is not None and weight_grads else None)
+    hq, hk = counts
+    L, handle = _lib.lib(), rotary.handle
     wptr, wbytes = None, 0
     if dws[0] is not None or dws[1] is not None:
         nb = C.c_size_t(0)
-        _lib.check(L.padoc_rotary_bwd_workspace_bytes(h, n, counts[0], counts[1], C.byref(nb)))
-        work = torch.empty(nb.value, dtype=torch.uint8, device=dev)  # the allocator's blocks are 512-byte aligned
-        made.append(work)
+        _lib.check(L.padoc_rotary_bwd_workspace_bytes(handle, n, hq, hk, C.byref(nb)))
+        work = like.new_empty(nb.value, dtype=torch.uint8)  # the allocator's blocks are 512-byte aligned
+        made.extend(t for t in (work, *dws) if t is not None)
         wptr, wbytes = work.data_ptr(), nb.value
-    (gq, xq, oq), (gk, xk, ok) = heads
-    args = _lib.ROTARY_BWD_ARGS.pack(n, counts[0], counts[1], *pos, *xq, *xk, *gq, *gk, *oq, *ok, ws[0], ws[1],
-                                     *(0 if t is None else t.data_ptr() for t in dws))
-    _launch(L.padoc_rotary_bwd, dev, stream, made, h, args, wptr, wbytes)
+    (xq, gq, oq), (xk, gk, ok) = heads
+    args = _lib.ROTARY_BWD_ARGS.pack(n, hq, hk, *_positions("positions", positions, rotary, n, device), *xq, *xk, *gq,
+                                     *gk, *oq, *ok, *ws, *(0 if t is None else t.data_ptr() for t in dws))
+    _launch(L.padoc_rotary_bwd, device, stream, made, handle, args, wptr, wbytes)
     return outs[0], outs[1], dws[0], dws[1]
 
 
 def _append_args(rotary, q, k, v, positions, q_weight, k_weight, q_positions, q_out, made, slots=0, k_cache=0, v_cache=0,
                  num_blocks=0):
-    """The packed arguments of an append, and its q_out."""
-    import torch
-    like = _rows_of(rotary, (k, q))
-    dev = like.device
-    nq, hq, hqo, n_q, qpos = 0, _NO_HEADS, _NO_HEADS, 0, (0, 0)
-    n_new, hkv, hk, hv, pos = 0, 0, _NO_HEADS, _NO_HEADS, (0, 0)
+    """The packed arguments of an append, its q_out and the GPU's index."""
+    device, dt = _rows_of(rotary, q if k is None else k)
+    d = rotary.head_dim
+    n_q = hq = n = hk = 0
+    q_in = q_to = k_in = v_in = _NO_HEADS
+    q_pos = pos = (0, 0)
     if k is not None:
-        n_new, hkv = k.shape[0], k.shape[1]
-        hk = _heads("k", k, like)
-        hv = _heads("v", v, like, k.shape)
-        pos = _positions("positions", positions, rotary, n_new, like)
+        n, hk, _ = shape = k.shape
+        k_in, v_in = _heads("k", k, dt, device, shape), _heads("v", v, dt, device, shape)
+        pos = _positions("positions", positions, rotary, n, device)
     if q is not None:
-        shape = (q.shape[0], q.shape[1], rotary.head_dim)
-        n_q, nq = shape[:2]
-        hq = _heads("q", q, like, shape)
+        if q.dim() != 3:
+            raise ValueError(f"q has shape {tuple(q.shape)}, expected [n, H, {d}]")
+        n_q, hq, _ = q.shape
+        shape = (n_q, hq, d)
+        q_in = _heads("q", q, dt, device, shape)
         if q_out is None:
-            q_out = torch.empty(shape, dtype=q.dtype, device=dev)
+            q_out = q.new_empty(shape)
             made.append(q_out)
-        hqo = _heads("q_out", q_out, like, shape)
+            q_to = q_out.data_ptr(), hq * d, d
+        else:
+            q_to = _heads("q_out", q_out, dt, device, shape)
         if q_positions is not None:
-            qpos = _positions("q_positions", q_positions, rotary, n_q, like)
+            q_pos = _positions("q_positions", q_positions, rotary, n_q, device)
         elif k is None:
-            qpos = _positions("positions", positions, rotary, n_q, like)
-    args = _lib.ROTARY_APPEND_ARGS.pack(n_q, n_new, nq, hkv, *qpos, *pos, *hq, *hk, *hv, *hqo,
-                                        _weight("q_weight", q_weight, like), _weight("k_weight", k_weight, like), slots,
-                                        k_cache, v_cache, num_blocks)
-    return args, q_out, dev
+            q_pos = _positions("positions", positions, rotary, n_q, device)
+    args = _lib.ROTARY_APPEND_ARGS.pack(n_q, n, hq, hk, *q_pos, *pos, *q_in, *k_in, *v_in, *q_to,
+                                        _weight("q_weight", q_weight, dt, device, d),
+                                        _weight("k_weight", k_weight, dt, device, d), slots, k_cache, v_cache, num_blocks)
+    return args, None if q is None else q_out, device
 
 
-def _check_caches(k_cache, v_cache, dtype, dev, d=None):
+def _check_caches(k_cache, v_cache, dtype, dev):
     """Checks caches in the library's layouts; ``(blocks, Hkv, d)``."""
-    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
-        _check_tensor(name, t, dtype, dev)
-    nb, hkv, d = (v_cache.shape[0], v_cache.shape[1], v_cache.shape[2]) if v_cache.dim() == 4 else (0, 0, 0)
-    if v_cache.shape != (nb, hkv, d, 16) or k_cache.shape != (nb, hkv, d // 8, 16, 8):
+    _check_tensor("k_cache", k_cache, dtype, dev)
+    _check_tensor("v_cache", v_cache, dtype, dev)
+    nb, hkv, d, slots = v_cache.shape if v_cache.dim() == 4 else (0, 0, 0, 0)
+    if slots != 16 or k_cache.shape != (nb, hkv, d // 8, 16, 8):
         raise ValueError(f"caches must be K [blocks, Hkv, d/8, 16, 8] and V [blocks, Hkv, d, 16], got "
                          f"{tuple(k_cache.shape)} and {tuple(v_cache.shape)}")
     return nb, hkv, d
@@ -683,17 +704,17 @@ def rotary_append(q, k, v, positions, slots, k_cache, v_cache, rotary: Rotary, q
     import torch
     if k is None or v is None:
         raise ValueError("rotary_append needs k and v (rotary_fwd rotates q alone)")
-    dt = _torch_dtype(rotary)
-    nb, hkv, d = _check_caches(k_cache, v_cache, dt, k.device)
-    if (hkv, d) != (k.shape[1], rotary.head_dim):
-        raise ValueError(f"the caches hold {hkv} heads of {d}, the rows {k.shape[1]} of {rotary.head_dim}")
-    _check_tensor("slots", slots, torch.int32, k.device)
+    dev = k.device
+    nb, hkv, d = _check_caches(k_cache, v_cache, rotary.torch_dtype, dev)
+    if k.shape[1:] != (hkv, d) or d != rotary.head_dim:
+        raise ValueError(f"the caches hold {hkv} heads of {d}, the rows are {tuple(k.shape)}")
+    _check_tensor("slots", slots, torch.int32, dev)
     if slots.shape != (k.shape[0], 2):
         raise ValueError(f"slots has shape {tuple(slots.shape)}, expected {(k.shape[0], 2)}")
     made = []
-    args, q_out, dev = _append_args(rotary, q, k, v, positions, q_weight, k_weight, q_positions, q_out, made,
-                                    slots.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), nb)
-    _launch(_lib.lib().padoc_rotary_append, dev, stream, made, rotary.handle, args)
+    args, q_out, device = _append_args(rotary, q, k, v, positions, q_weight, k_weight, q_positions, q_out, made,
+                                       slots.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), nb)
+    _launch(_lib.lib().padoc_rotary_append, device, stream, made, rotary.handle, args)
     return q_out
 
 
@@ -725,7 +746,7 @@ def cache_copy_blocks(k_cache, v_cache, pairs, k_dst=None, v_dst=None, pairs_hos
         host = np.ascontiguousarray(pairs_host, dtype=np.int32)
         if host.shape != pairs.shape:
             raise ValueError(f"pairs_host has shape {host.shape}, expected {tuple(pairs.shape)}")
-    _launch(_lib.lib().padoc_cache_copy_blocks, dev, stream, (), k_cache.data_ptr(), v_cache.data_ptr(), nb,
+    _launch(_lib.lib().padoc_cache_copy_blocks, dev.index, stream, (), k_cache.data_ptr(), v_cache.data_ptr(), nb,
             k_dst.data_ptr(), v_dst.data_ptr(), nd, pairs.data_ptr(), pairs.shape[0],
             None if host is None else host.ctypes.data, hkv, d, _lib.BF16 if dt == torch.bfloat16 else _lib.F32)
     return k_dst, v_dst
@@ -1016,16 +1037,16 @@ class DecodeSession:
         if n_q and n_kv and q_positions is None and n_q != n_kv:
             raise ValueError(f"{n_q} query rows of {n_kv} new ones need q_positions")
         if n_q or n_kv:
-            args, _, rows_dev = _append_args(rotary, q if n_q else None, k_new if n_kv else None, v_new, positions,
+            args, _, device = _append_args(rotary, q if n_q else None, k_new if n_kv else None, v_new, positions,
                                              q_weight, k_weight, q_positions, q_rot, made)
-            if rows_dev != dev:
-                raise ValueError(f"rows are on {rows_dev}, expected {dev}")
+            if device != dev.index:
+                raise ValueError(f"rows are on cuda:{device}, expected {dev}")
         else:
             args = _lib.ROTARY_APPEND_ARGS.pack(*[0] * 26)
         # head counts are the session's also where a step has no rows of a kind
         args = args[:16] + struct.pack("=ii", self.num_heads_q, self.num_heads_kv) + args[24:]
         ws = self.workspace() if workspace is None else workspace
-        _launch(_lib.lib().padoc_session_launch_rotary, dev, stream, made, self.handle, rotary.handle, args,
+        _launch(_lib.lib().padoc_session_launch_rotary, dev.index, stream, made, self.handle, rotary.handle, args,
                 out.data_ptr() if n_q else None, lse.data_ptr() if n_q else None, ws.data_ptr(), ws.numel())
         return out, lse
 
