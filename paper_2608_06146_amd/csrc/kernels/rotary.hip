@@ -10,9 +10,12 @@
 // A row of one head is shared by D / 16 lanes (a group).  Lane l of a group
 // holds 16 dimensions: the eight pairs 8l .. 8l+7, so that a rotation stays
 // inside a lane and its memory accesses are 16 bytes each; where only the
-// leading dimensions are rotated, the lanes behind them hold the rest.  A group
-// takes several heads of one row one after the other: it computes the row's
-// eight cosines and sines per lane once.
+// leading dimensions are rotated, the lanes behind them hold the rest.
+//
+// A workgroup takes a tile of rows of one tensor (q or k).  Its lanes compute
+// the cosines and sines of the tile's rows once, a pair each, into LDS; its
+// groups then take the tile's (row, head) pairs in order, neighbours reading
+// neighbouring heads, with the rows of the next ones in flight.
 //
 // Angles: a position times the pair's 64-bit fraction of a turn, modulo 2^64,
 // is the angle in turns; its leading 32 bits are split into a quadrant and an
@@ -35,26 +38,41 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 
-// Eight elements at an address aligned to one element.
-__device__ __forceinline__ void load8(const __bf16* p, float* x) {
+// A lane's 16 elements of a head as they were loaded: its two chunks of eight,
+// one after the other, at addresses aligned to one element.
+template <typename T>
+struct Raw;
+template <>
+struct Raw<__bf16> {
   typedef u32x4 unit __attribute__((aligned(2)));
-  const u32x4 u = *reinterpret_cast<const unit*>(p);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(u[i] << 16);
-    x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+  u32x4 u[2];
+  __device__ __forceinline__ void load(const __bf16* p, const int (&at)[2]) {
+    u[0] = *reinterpret_cast<const unit*>(p + at[0]);
+    u[1] = *reinterpret_cast<const unit*>(p + at[1]);
   }
-}
-__device__ __forceinline__ void load8(const float* p, float* x) {
+  __device__ __forceinline__ void get(float (&x)[16]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x[2 * i] = __uint_as_float(u[i / 4][i % 4] << 16);
+      x[2 * i + 1] = __uint_as_float(u[i / 4][i % 4] & 0xffff0000u);
+    }
+  }
+};
+template <>
+struct Raw<float> {
   typedef f32x4 unit __attribute__((aligned(4)));
-  const f32x4 a = reinterpret_cast<const unit*>(p)[0], b = reinterpret_cast<const unit*>(p)[1];
+  f32x4 u[4];
+  __device__ __forceinline__ void load(const float* p, const int (&at)[2]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[i] = a[i];
-    x[4 + i] = b[i];
+    for (int i = 0; i < 4; ++i) u[i] = *reinterpret_cast<const unit*>(p + at[i / 2] + 4 * (i % 2));
   }
-}
-// Rounded to nearest-even once, here (NaN stays NaN).
+  __device__ __forceinline__ void get(float (&x)[16]) const {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = u[i / 4][i % 4];
+  }
+};
+
+// Eight elements, rounded to nearest-even once, here (NaN stays NaN).
 __device__ __forceinline__ void store8(__bf16* p, const float* x) {
   typedef u32x4 unit __attribute__((aligned(2)));
   const bf16x8 b = __builtin_convertvector((f32x8{x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]}), bf16x8);
@@ -66,18 +84,6 @@ __device__ __forceinline__ void store8(float* p, const float* x) {
   typedef f32x4 unit __attribute__((aligned(4)));
   reinterpret_cast<unit*>(p)[0] = f32x4{x[0], x[1], x[2], x[3]};
   reinterpret_cast<unit*>(p)[1] = f32x4{x[4], x[5], x[6], x[7]};
-}
-
-// A lane's 16 values of a head: its two chunks, one after the other.
-template <typename T>
-__device__ __forceinline__ void load16v(const T* p, const int (&at)[2], float (&x)[16]) {
-  load8(p + at[0], x);
-  load8(p + at[1], x + 8);
-}
-template <typename T>
-__device__ __forceinline__ void store16v(T* p, const int (&at)[2], const float (&x)[16]) {
-  store8(p + at[0], x);
-  store8(p + at[1], x + 8);
 }
 
 // Sum over the L (4 or 8) lanes of a group, in every one of them.
@@ -126,26 +132,43 @@ struct Angles {
   float c[8], s[8];
 };
 
-// Cosines and sines of a lane's pairs for a row (scaled; the sine negated for
-// the inverse rotation).
-__device__ __forceinline__ Angles angles(const RotaryParams& p, const int32_t* pos, int64_t stride, int64_t row,
-                                         int first_pair, bool turned) {
-  Angles a;
-  if (!turned) return a;
-  int32_t at[kMaxAxes];
-#pragma unroll
-  for (int x = 0; x < kMaxAxes; ++x) at[x] = x < p.n_axes ? pos[x * stride + row] : 0;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int ax = p.table.axis[first_pair + j];
-    const int32_t m = ax == 0 ? at[0] : ax == 1 ? at[1] : ax == 2 ? at[2] : at[3];
-    float s, c;
-    sincos_turns((uint32_t)((uint64_t)(int64_t)m * p.table.turn[first_pair + j] >> 32), s, c);
-    a.c[j] = c * p.scale;
-    a.s[j] = p.inverse ? -s * p.scale : s * p.scale;
+// Cosines and sines of a tile's rows: per row and quarter i of a lane's pairs
+// (two of them), the lanes' 16 bytes side by side.
+template <int D>
+struct AngleTable {
+  static constexpr int kLanes = D / 16;
+  static constexpr int kRows = 4096 / D;  // rows of a tile, at most
+  f32x4 at[kRows][4][kLanes];
+
+  // Fill rows [0, n): thread t takes pair t % (D / 2) of rows t / (D / 2), ...;
+  // scaled, the sine negated for the inverse rotation.
+  __device__ __forceinline__ void fill(const RotaryParams& p, const int32_t* pos, int64_t stride, int64_t row0, int n) {
+    constexpr int kPairs = D / 2;
+    const int pair = threadIdx.x % kPairs;
+    if (pair >= p.pairs) return;
+    const uint64_t turn = p.table.turn[pair];
+    pos += p.table.axis[pair] * stride + row0;
+    float* dst = reinterpret_cast<float*>(&at[0][pair % 8 / 2][pair / 8]) + pair % 2 * 2;
+    for (int r = threadIdx.x / kPairs; r < n; r += kThreads / kPairs) {
+      float s, c;
+      sincos_turns((uint32_t)((uint64_t)(int64_t)pos[r] * turn >> 32), s, c);
+      dst[r * (D / 16 * 16)] = c * p.scale;
+      dst[r * (D / 16 * 16) + 1] = p.inverse ? -s * p.scale : s * p.scale;
+    }
   }
-  return a;
-}
+  __device__ __forceinline__ Angles get(int row, int lane) const {
+    Angles a;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 x = at[row][i][lane];
+      a.c[2 * i] = x[0];
+      a.s[2 * i] = x[1];
+      a.c[2 * i + 1] = x[2];
+      a.s[2 * i + 1] = x[3];
+    }
+    return a;
+  }
+};
 
 // Rotate a lane's pairs.
 template <bool PAIRS>
@@ -172,128 +195,221 @@ __device__ __forceinline__ const T* head_row(const padoc_heads& x, int64_t row, 
   return static_cast<const T*>(x.data) + row * x.row_stride + h * x.head_stride;
 }
 
-// Heads [h0, h1) of a row of one tensor: norm, rotation, and `put(h, values)`.
-template <typename T, int D, bool PAIRS, class Put>
-__device__ __forceinline__ void turn_heads(const padoc_heads& in, const void* w, int64_t row, int h0, int h1,
-                                           const Place<D, PAIRS>& pl, const Angles& t, float eps, Put put) {
-  float wt[16];
-  if (w) load16v(static_cast<const T*>(w), pl.at, wt);
-  for (int h = h0; h < h1; ++h) {
-    float x[16];
-    load16v(head_row<T>(in, row, h), pl.at, x);
-    if (w) {
-      const float rho = rms_scale<D>(x, eps);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] *= rho * wt[i];
+// Rows that a lane has in flight at once.
+template <typename T>
+constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;
+
+// A tile of one tensor (q's or k's) as a workgroup sees it.
+struct Tile {
+  padoc_heads in, out, x;
+  const void* w;
+  int heads, h0;   // heads of the tile, from h0 on
+  int64_t row0;
+  int rows;
+};
+
+// Tile `b` of the launch; q's tiles come first.
+__device__ __forceinline__ Tile tile_of(const RotaryParams& p, int64_t b) {
+  Tile t;
+  const bool is_q = b < p.tiles_q.items;
+  const TileGrid& g = is_q ? p.tiles_q : p.tiles_k;
+  if (!is_q) b -= p.tiles_q.items;
+  const int64_t block = b / g.head_runs;
+  t.h0 = (int)(b - block * g.head_runs) * g.heads;
+  t.heads = min(g.heads, (is_q ? p.Hq : p.Hkv) - t.h0);
+  t.row0 = block * g.rows;
+  t.rows = (int)min((int64_t)g.rows, (int64_t)(is_q ? p.n_q : p.n) - t.row0);
+  t.in = is_q ? p.q : p.k;
+  t.out = is_q ? p.qo : p.ko;
+  t.x = is_q ? p.xq : p.xk;
+  t.w = is_q ? p.wq : p.wk;
+  return t;
+}
+
+// A group's place among the (row, head) pairs of a tile, which the workgroup's
+// groups take in turn.
+struct Cursor {
+  int row, h;
+  __device__ __forceinline__ Cursor(const Tile& t, int group) : row(group / t.heads), h(group - row * t.heads) {}
+  // To the place `groups` pairs on: dr rows and dh heads (groups = dr * heads + dh).
+  __device__ __forceinline__ void next(const Tile& t, int dr, int dh) {
+    row += dr;
+    h += dh;
+    if (h >= t.heads) {
+      h -= t.heads;
+      ++row;
     }
-    if (pl.turned) turn<PAIRS>(x, t);
-    put(h, x);
   }
+  template <typename T>
+  __device__ __forceinline__ T* at(const padoc_heads& x, const Tile& t) const {
+    return static_cast<T*>(x.data) + (t.row0 + row) * x.row_stride + (t.h0 + h) * x.head_stride;
+  }
+};
+
+// Rows of a tile: norm, rotation, and `put(row, head, values)`.  The first
+// rows are asked for before the angles are computed, the others kAhead turns
+// before theirs.
+template <typename T, int D, bool PAIRS, class Put>
+__device__ __forceinline__ void turn_tile(const RotaryParams& p, const Tile& t, const int32_t* pos, int64_t pos_stride,
+                                          AngleTable<D>& table, const Place<D, PAIRS>& pl, Put put) {
+  constexpr int L = D / 16, R = kThreads / L, U = kAhead<T>;
+  const int dr = R / t.heads, dh = R - dr * t.heads;
+  Cursor ahead(t, threadIdx.x / L), at = ahead;
+  Raw<T> raw[U], rw;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (ahead.row < t.rows) raw[u].load(ahead.at<const T>(t.in, t), pl.at);
+    ahead.next(t, dr, dh);
+  }
+  if (t.w) rw.load(static_cast<const T*>(t.w), pl.at);
+  table.fill(p, pos, pos_stride, t.row0, t.rows);
+  __syncthreads();
+  float wt[16];
+  if (t.w) rw.get(wt);
+  while (at.row < t.rows) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (at.row >= t.rows) break;
+      float x[16];
+      raw[u].get(x);
+      if (ahead.row < t.rows) raw[u].load(ahead.at<const T>(t.in, t), pl.at);
+      ahead.next(t, dr, dh);
+      if (t.w) {
+        const float rho = rms_scale<D>(x, p.eps);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] *= rho * wt[i];
+      }
+      if (pl.turned) turn<PAIRS>(x, table.get(at.row, threadIdx.x % L));
+      put(at, x);
+      at.next(t, dr, dh);
+    }
+  }
+  __syncthreads();
 }
 
 // Forward (and, with `inverse`, the backward of a rotation without norms).
-// blockIdx.x, + gridDim.x, ...: kThreads / L rows, a group each; blockIdx.y: a
-// run of heads, q's before k's.
 template <typename T, int D, bool PAIRS>
 __global__ __launch_bounds__(kThreads) void rotary_fwd_kernel(const RotaryParams p) {
-  constexpr int L = D / 16, R = kThreads / L;
-  const Place<D, PAIRS> pl(threadIdx.x % L, p.pairs);
-  const int h0 = blockIdx.y * p.heads_per_group, h1 = min(h0 + p.heads_per_group, p.Hq + p.Hkv);
-  for (int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / L; row < p.n; row += (int64_t)gridDim.x * R) {
-    const Angles t = angles(p, p.pos, p.pos_stride, row, pl.first_pair, pl.turned);
-    turn_heads<T, D, PAIRS>(p.q, p.wq, row, h0, min(h1, p.Hq), pl, t, p.eps, [&](int h, const float (&x)[16]) {
-      store16v(const_cast<T*>(head_row<T>(p.qo, row, h)), pl.at, x);
-    });
-    turn_heads<T, D, PAIRS>(p.k, p.wk, row, max(h0 - p.Hq, 0), h1 - p.Hq, pl, t, p.eps, [&](int h, const float (&x)[16]) {
-      store16v(const_cast<T*>(head_row<T>(p.ko, row, h)), pl.at, x);
+  __shared__ AngleTable<D> table;
+  const Place<D, PAIRS> pl(threadIdx.x % (D / 16), p.pairs);
+  for (int64_t b = blockIdx.x; b < p.items; b += gridDim.x) {
+    const Tile t = tile_of(p, b);
+    turn_tile<T, D, PAIRS>(p, t, p.pos, p.pos_stride, table, pl, [&](const Cursor& c, const float (&x)[16]) {
+      T* dst = c.at<T>(t.out, t);
+      store8(dst + pl.at[0], x);
+      store8(dst + pl.at[1], x + 8);
     });
   }
 }
 
-// Backward of heads [h0, h1) of a row: dx, and the weight's gradient added up
-// in acc.
-template <typename T, int D, bool PAIRS>
-__device__ __forceinline__ void turn_heads_bwd(const padoc_heads& dz, const padoc_heads& xin, const padoc_heads& out,
-                                               const void* w, int64_t row, int h0, int h1, const Place<D, PAIRS>& pl,
-                                               const Angles& t, float eps, float (&acc)[16]) {
-  float wt[16];
-  if (w) load16v(static_cast<const T*>(w), pl.at, wt);
-  for (int h = h0; h < h1; ++h) {
-    float g[16];
-    load16v(head_row<T>(dz, row, h), pl.at, g);
-    if (pl.turned) turn<PAIRS>(g, t);
-    if (w) {
-      float x[16];
-      load16v(head_row<T>(xin, row, h), pl.at, x);
-      const float rho = rms_scale<D>(x, eps);
-      float dot = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        x[i] *= rho;
-        acc[i] += g[i] * x[i];
-        g[i] *= wt[i];
-        dot += g[i] * x[i];
-      }
-      const float mean = group_sum<D / 16>(dot) * (1.f / D);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) g[i] = rho * (g[i] - x[i] * mean);
-    }
-    store16v(const_cast<T*>(head_row<T>(out, row, h)), pl.at, g);
-  }
-}
-
-// A workgroup takes rows blockIdx.x, + gridDim.x, ... in units of kThreads / L.
-// Its sums of the weights' gradients (fp32, over its rows and heads) go to
-// part[workgroup][q, k][D]: lanes of equal l over the wavefront, then the four
-// wavefronts through LDS.
+// Backward: dx of p.passes tiles one after the other, and the weight's gradient
+// over them (fp32): in acc, lane by lane, then over the lanes of equal l of a
+// wavefront and over the four wavefronts through LDS, into part[item][D].
 template <typename T, int D, bool PAIRS>
 __global__ __launch_bounds__(kThreads) void rotary_bwd_kernel(const RotaryParams p) {
-  constexpr int L = D / 16, R = kThreads / L;
+  constexpr int L = D / 16, R = kThreads / L, U = kAhead<T> / 2;
+  __shared__ AngleTable<D> table;
+  __shared__ float sums[kThreads / 64][D];
   const Place<D, PAIRS> pl(threadIdx.x % L, p.pairs);
-  const int h0 = blockIdx.y * p.heads_per_group, h1 = min(h0 + p.heads_per_group, p.Hq + p.Hkv);
-  float acc[2][16] = {};
-  for (int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / L; row < p.n; row += (int64_t)gridDim.x * R) {
-    const Angles t = angles(p, p.pos, p.pos_stride, row, pl.first_pair, pl.turned);
-    turn_heads_bwd<T, D, PAIRS>(p.q, p.xq, p.qo, p.wq, row, h0, min(h1, p.Hq), pl, t, p.eps, acc[0]);
-    turn_heads_bwd<T, D, PAIRS>(p.k, p.xk, p.ko, p.wk, row, max(h0 - p.Hq, 0), h1 - p.Hq, pl, t, p.eps, acc[1]);
-  }
-  if (!p.part) return;
-  __shared__ float sums[kThreads / 64][2][D];
+  for (int64_t b = blockIdx.x; b < p.items; b += gridDim.x) {
+    Tile t = tile_of(p, b);
+    const int64_t row_end = t.row0 + t.rows;
+    const int dr = R / t.heads, dh = R - dr * t.heads;
+    float acc[16] = {}, wt[16];
+    if (t.w) {
+      Raw<T> rw;
+      rw.load(static_cast<const T*>(t.w), pl.at);
+      rw.get(wt);
+    }
+    for (; t.row0 < row_end; t.row0 += p.tile_rows[b >= p.tiles_q.items]) {
+      t.rows = (int)min((int64_t)p.tile_rows[b >= p.tiles_q.items], row_end - t.row0);
+      Cursor ahead(t, threadIdx.x / L), at = ahead;
+      Raw<T> rg[U], rx[U];
 #pragma unroll
-  for (int w = 0; w < 2; ++w)
+      for (int u = 0; u < U; ++u) {
+        if (ahead.row < t.rows) {
+          rg[u].load(ahead.at<const T>(t.in, t), pl.at);
+          if (t.w) rx[u].load(ahead.at<const T>(t.x, t), pl.at);
+        }
+        ahead.next(t, dr, dh);
+      }
+      table.fill(p, p.pos, p.pos_stride, t.row0, t.rows);
+      __syncthreads();
+      while (at.row < t.rows) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (at.row >= t.rows) break;
+          float g[16], x[16];
+          rg[u].get(g);
+          if (t.w) rx[u].get(x);
+          if (ahead.row < t.rows) {
+            rg[u].load(ahead.at<const T>(t.in, t), pl.at);
+            if (t.w) rx[u].load(ahead.at<const T>(t.x, t), pl.at);
+          }
+          ahead.next(t, dr, dh);
+          if (pl.turned) turn<PAIRS>(g, table.get(at.row, threadIdx.x % L));
+          if (t.w) {
+            const float rho = rms_scale<D>(x, p.eps);
+            float dot = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              x[i] *= rho;
+              acc[i] += g[i] * x[i];
+              g[i] *= wt[i];
+              dot += g[i] * x[i];
+            }
+            const float mean = group_sum<D / 16>(dot) * (1.f / D);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) g[i] = rho * (g[i] - x[i] * mean);
+          }
+          T* dst = at.at<T>(t.out, t);
+          store8(dst + pl.at[0], g);
+          store8(dst + pl.at[1], g + 8);
+          at.next(t, dr, dh);
+        }
+      }
+      __syncthreads();
+    }
+    if (!p.part) continue;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      float v = acc[w][i];
+      float v = acc[i];
 #pragma unroll
       for (int m = L; m < 64; m *= 2) v += __shfl_xor(v, m);
-      if (threadIdx.x % 64 < L) sums[threadIdx.x / 64][w][pl.at[i / 8] + i % 8] = v;
+      if (threadIdx.x % 64 < L) sums[threadIdx.x / 64][pl.at[i / 8] + i % 8] = v;
     }
-  __syncthreads();
-  float* part = p.part + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (2 * D);
-  for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
-    float v = 0.f;
+    __syncthreads();
+    if (threadIdx.x < D) {
+      float v = 0.f;
 #pragma unroll
-    for (int k = 0; k < kThreads / 64; ++k) v += sums[k][i / D][i % D];
-    part[i] = v;
+      for (int k = 0; k < kThreads / 64; ++k) v += sums[k][threadIdx.x];
+      p.part[b * D + threadIdx.x] = v;
+    }
+    __syncthreads();
   }
 }
 
-// Sums of the workgroups' parts in a fixed order: 16 columns of [q, k][D] a
-// workgroup, 64 of its rows side by side.
-__global__ __launch_bounds__(1024) void rotary_bwd_sum_kernel(const float* __restrict__ part, int n_part, int D,
-                                                              float* dwq, float* dwk) {
+// Sums of the items' parts in a fixed order: 16 columns of one tensor a
+// workgroup (q's, then k's), 64 of its rows side by side.
+__global__ __launch_bounds__(1024) void rotary_bwd_sum_kernel(const float* __restrict__ part, int64_t n_q, int64_t n_k,
+                                                              int D, float* dwq, float* dwk) {
   __shared__ float sums[64][17];
   const int col = threadIdx.x % 16, r0 = threadIdx.x / 16;
-  const int at = blockIdx.x * 16 + col;
+  const bool is_q = (int)blockIdx.x * 16 < D;
+  const int at = blockIdx.x * 16 + col - (is_q ? 0 : D);
+  float* dw = is_q ? dwq : dwk;
+  if (!dw) return;
+  const float* src = part + (is_q ? 0 : n_q * D) + at;
+  const int64_t n = is_q ? n_q : n_k;
   float v = 0.f;
-  for (int r = r0; r < n_part; r += 64) v += part[(int64_t)r * (2 * D) + at];
+#pragma unroll 4
+  for (int64_t r = r0; r < n; r += 64) v += src[r * D];
   sums[r0][col] = v;
   __syncthreads();
   if (threadIdx.x >= 16) return;
   v = 0.f;
   for (int r = 0; r < 64; ++r) v += sums[r][col];
-  float* dw = at < D ? dwq : dwk;
-  if (dw) dw[at < D ? at : at - D] = v;
+  dw[at] = v;
 }
 
 __device__ __forceinline__ bool slot_of(const RotaryParams& p, int64_t row, int32_t& blk, int32_t& slot) {
@@ -302,72 +418,145 @@ __device__ __forceinline__ bool slot_of(const RotaryParams& p, int64_t row, int3
   return blk >= 0 && blk < p.n_blocks && slot >= 0 && slot < kBlock;
 }
 
-// Append: items of four roles, one after the other: q's rows into q_out, k's
-// rows into their slots of the K cache (kThreads / L rows and a run of heads
-// each), v's rows into the V cache (one (row, head) of D elements per 64
-// lanes), block-table patches.
-template <typename T, int D, bool PAIRS>
-__device__ __forceinline__ void append_item(const RotaryParams& p, int64_t b) {
-  constexpr int L = D / 16, R = kThreads / L;
-  const int lane = threadIdx.x % L;
-  const int hp = p.heads_per_group;
-  if (b < p.items_q) {
-    const int runs = (p.Hq + hp - 1) / hp;
-    const int64_t row = b / runs * R + threadIdx.x / L;
-    if (row >= p.n_q) return;
-    const Place<D, PAIRS> pl(lane, p.pairs);
-    const Angles t = angles(p, p.q_pos, p.q_pos_stride, row, pl.first_pair, pl.turned);
-    const int h0 = (int)(b % runs) * hp;
-    turn_heads<T, D, PAIRS>(p.q, p.wq, row, h0, min(h0 + hp, p.Hq), pl, t, p.eps, [&](int h, const float (&x)[16]) {
-      store16v(const_cast<T*>(head_row<T>(p.qo, row, h)), pl.at, x);
-    });
-    return;
+// V rows into the d-major cache: ROWS consecutive new rows of one head a
+// workgroup.  A run of rows that go to consecutive slots of one half of a block
+// (eight tokens) is written together: for each dimension one 16-byte store
+// (bf16) where the half is whole, else its elements one by one.  A run belongs
+// to the workgroup that its first row is in, so the rows are staged with the
+// seven after them; two runs are written side by side, so that both halves of a
+// block leave as 32 contiguous bytes a dimension.
+template <typename T, int D, int ROWS>
+struct VTile {
+  static constexpr int kRows = ROWS + 7;
+  static constexpr int kStride = D + 4 / (int)sizeof(T);  // bf16: two runs eight rows apart lie in other banks
+  T tile[kRows * kStride];
+  int64_t place[kRows + 1];  // slot of row first - 1 + i, counted through the pool; -2: none
+  int32_t runs[ROWS];        // first row | length << 8
+  int32_t n_runs;
+};
+
+template <typename T, int D, int ROWS>
+__device__ __forceinline__ void append_v(const RotaryParams& p, int64_t item, VTile<T, D, ROWS>& m) {
+  constexpr int kRows = VTile<T, D, ROWS>::kRows, kStride = VTile<T, D, ROWS>::kStride;
+  constexpr int E = 16 / (int)sizeof(T);  // elements per 16-byte unit
+  T* tile = m.tile;
+  int64_t* place = m.place;
+  int32_t* runs = m.runs;
+  const int64_t tiles = ((int64_t)p.n + ROWS - 1) / ROWS;
+  const int h = (int)(item / tiles);
+  const int64_t first = (item - h * tiles) * ROWS;
+  const int tid = threadIdx.x;
+  if (tid <= kRows) {
+    const int64_t row = first - 1 + tid;
+    int32_t blk, slot;
+    const bool ok = row >= 0 && row < p.n && slot_of(p, row, blk, slot);
+    place[tid] = ok ? (int64_t)blk * kBlock + slot : -2;
   }
-  b -= p.items_q;
-  int32_t blk, slot;
-  if (b < p.items_k) {
-    const int runs = (p.Hkv + hp - 1) / hp;
-    const int64_t row = b / runs * R + threadIdx.x / L;
-    if (row >= p.n || !slot_of(p, row, blk, slot)) return;
-    const Place<D, PAIRS> pl(lane, p.pairs);
-    const Angles t = angles(p, p.pos, p.pos_stride, row, pl.first_pair, pl.turned);
-    const int h0 = (int)(b % runs) * hp;
-    T* cache = static_cast<T*>(p.k_cache);
-    turn_heads<T, D, PAIRS>(p.k, p.wk, row, h0, min(h0 + hp, p.Hkv), pl, t, p.eps, [&](int h, const float (&x)[16]) {
-      store8(cache + paged_k_offset<D>(blk, h, p.Hkv, slot, pl.at[0] / 8), x);
-      store8(cache + paged_k_offset<D>(blk, h, p.Hkv, slot, pl.at[1] / 8), x + 8);
-    });
-    return;
+  constexpr int kUnits = kRows * D / E;
+#pragma unroll 4
+  for (int u = tid; u < kUnits; u += kThreads) {
+    const int r = u / (D / E), c = u % (D / E) * E;
+    if (first + r < p.n) {
+      const auto x = *reinterpret_cast<const typename Raw<T>::unit*>(head_row<T>(p.v, first + r, h) + c);
+      T y[E];
+      __builtin_memcpy(y, &x, 16);
+#pragma unroll
+      for (int e = 0; e < E; e += 4 / (int)sizeof(T))
+        __builtin_memcpy(&tile[r * kStride + c + e], &y[e], 4);
+    }
   }
-  b -= p.items_k;
-  if (b < p.items_v) {
-    const int64_t item = b * (kThreads / 64) + threadIdx.x / 64;
-    const int64_t row = item / p.Hkv;
-    if (row >= p.n || !slot_of(p, row, blk, slot)) return;
-    const int h = (int)(item - row * p.Hkv);
-    const T* src = head_row<T>(p.v, row, h);
-    T* dst = static_cast<T*>(p.v_cache) + ((int64_t)blk * p.Hkv + h) * (D * kBlock) + slot;
-    for (int c = threadIdx.x % 64; c < D; c += 64) dst[c * kBlock] = src[c];
-    return;
+  __syncthreads();
+  if (tid < 64) {
+    const int64_t s = tid < ROWS ? place[tid + 1] : -2;
+    const bool leads = s >= 0 && (s % 8 == 0 || place[tid] != s - 1);
+    int len = 1;
+    while (leads && len < 8 - (int)(s % 8) && place[tid + 1 + len] == s + len) ++len;
+    const uint64_t all = __ballot(leads);
+    if (leads) runs[__popcll(all & ((1ull << tid) - 1))] = tid | len << 8;
+    if (tid == 0) m.n_runs = __popcll(all);
   }
-  const int64_t i = (b - p.items_v) * kThreads + threadIdx.x;
-  if (i < p.n_patch) p.block_table[p.patch[2 * i]] = p.patch[2 * i + 1];
+  __syncthreads();
+  const int lane = tid % 64, n = m.n_runs;
+  for (int step = tid / 64; step < (n + 1) / 2 * (D / 32); step += kThreads / 64) {
+    const int run = step / (D / 32) * 2 + lane % 2;
+    if (run >= n) continue;
+    const int c = step % (D / 32) * 32 + lane / 2;
+    const int r = runs[run] & 255, len = runs[run] >> 8;
+    const int64_t s = place[r + 1];
+    T* dst = static_cast<T*>(p.v_cache) + ((s / kBlock * p.Hkv + h) * D + c) * kBlock + s % kBlock;
+    const T* src = tile + r * kStride + c;
+    if (len == 8) {
+      T y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = src[i * kStride];
+      __builtin_memcpy(__builtin_assume_aligned(dst, 16), y, sizeof(y));
+    } else {
+      for (int i = 0; i < len; ++i) dst[i] = src[i * kStride];
+    }
+  }
+  __syncthreads();
 }
 
-template <typename T, int D, bool PAIRS>
+// Append: items of four roles, one after the other: v's rows into the V cache,
+// tiles of q's rows into q_out, tiles of k's rows into their slots of the K
+// cache, block-table patches.
+template <typename T, int D, bool PAIRS, int ROWS>
 __global__ __launch_bounds__(kThreads) void rotary_append_kernel(const RotaryParams p) {
-  for (int64_t b = blockIdx.x; b < p.items; b += gridDim.x) append_item<T, D, PAIRS>(p, b);
+  __shared__ union Shared {
+    AngleTable<D> table;
+    VTile<T, D, ROWS> v;
+    __device__ Shared() {}
+  } shared;
+  const Place<D, PAIRS> pl(threadIdx.x % (D / 16), p.pairs);
+  for (int64_t b = blockIdx.x; b < p.items; b += gridDim.x) {
+    if (b < p.items_v) {
+      append_v<T, D, ROWS>(p, b, shared.v);
+      continue;
+    }
+    const int64_t i = b - p.items_v, n_q = p.tiles_q.items, n_turned = n_q + p.tiles_k.items;
+    if (i >= n_turned) {
+      const int64_t e = (i - n_turned) * kThreads + threadIdx.x;
+      if (e < p.n_patch) p.block_table[p.patch[2 * e]] = p.patch[2 * e + 1];
+      continue;
+    }
+    const Tile t = tile_of(p, i);
+    const bool is_q = i < n_q;
+    T* cache = static_cast<T*>(p.k_cache);
+    turn_tile<T, D, PAIRS>(p, t, is_q ? p.q_pos : p.pos, is_q ? p.q_pos_stride : p.pos_stride, shared.table, pl,
+                           [&](const Cursor& c, const float (&x)[16]) {
+      if (is_q) {
+        T* dst = c.at<T>(t.out, t);
+        store8(dst + pl.at[0], x);
+        store8(dst + pl.at[1], x + 8);
+        return;
+      }
+      int32_t blk, slot;
+      if (!slot_of(p, t.row0 + c.row, blk, slot)) return;
+      store8(cache + paged_k_offset<D>(blk, t.h0 + c.h, p.Hkv, slot, pl.at[0] / 8), x);
+      store8(cache + paged_k_offset<D>(blk, t.h0 + c.h, p.Hkv, slot, pl.at[1] / 8), x + 8);
+    });
+  }
 }
 
 constexpr int64_t kMaxGrid = 1 << 20;  // workgroups of a launch: the rest by strides
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Heads of a row that a group takes: as many as leave the chip about `groups`
-// groups, so that a short call spreads its heads over more of them and a long
-// one computes its cosines once per row.
-int heads_per_group(int64_t n, int H, int64_t groups) {
-  return (int)std::min<int64_t>(H, std::max<int64_t>(1, n * H / groups));
+// Tiles of n rows of H heads (of H_all that the launch turns): as many turns a
+// group (up to kMaxTurns) as leave the chip about kItems workgroups, so that a
+// short call is spread over the chip.
+constexpr int64_t kItems = 1024;
+constexpr int kMaxTurns = 8;
+TileGrid tile_grid(int64_t n, int H, int H_all, int D) {
+  TileGrid g{};
+  if (n == 0 || H == 0) return g;
+  const int64_t groups = kThreads / (D / 16);
+  const int64_t turns = std::min<int64_t>(kMaxTurns, std::max<int64_t>(1, n * H_all / (groups * kItems)));
+  g.heads = (int32_t)std::min<int64_t>(H, groups * turns);
+  g.head_runs = (int32_t)ceil_div(H, g.heads);
+  g.rows = (int32_t)std::max<int64_t>(1, std::min<int64_t>({groups * turns / g.heads, 4096 / D, n}));
+  g.items = ceil_div(n, g.rows) * g.head_runs;
+  return g;
 }
 
 template <template <typename, int, bool> class Call>
@@ -398,57 +587,75 @@ struct Bwd {
     hipLaunchKernelGGL((rotary_bwd_kernel<T, D, PAIRS>), grid, dim3(kThreads), 0, s, p);
   }
 };
-template <typename T, int D, bool PAIRS>
+template <int ROWS>
 struct Append {
-  static void go(const RotaryParams& p, dim3 grid, hipStream_t s) {
-    hipLaunchKernelGGL((rotary_append_kernel<T, D, PAIRS>), grid, dim3(kThreads), 0, s, p);
-  }
+  template <typename T, int D, bool PAIRS>
+  struct Call {
+    static void go(const RotaryParams& p, dim3 grid, hipStream_t s) {
+      hipLaunchKernelGGL((rotary_append_kernel<T, D, PAIRS, ROWS>), grid, dim3(kThreads), 0, s, p);
+    }
+  };
 };
+
+dim3 grid_of(int64_t items) { return dim3((unsigned)std::min(items, kMaxGrid)); }
+
+// The backward's items: some tiles each, so that about kItems of them leave
+// their D sums.
+void bwd_grids(int64_t n, int Hq, int Hkv, int D, TileGrid& q, TileGrid& k, int32_t (&tile_rows)[2]) {
+  q = tile_grid(n, Hq, Hq + Hkv, D);
+  k = tile_grid(n, Hkv, Hq + Hkv, D);
+  tile_rows[0] = q.rows;
+  tile_rows[1] = k.rows;
+  const int64_t passes = std::max<int64_t>(1, ceil_div(q.items + k.items, kItems));
+  for (TileGrid* g : {&q, &k}) {
+    if (g->items == 0) continue;
+    g->rows = (int32_t)std::min<int64_t>(g->rows * passes, n);
+    g->items = ceil_div(n, g->rows) * g->head_runs;
+  }
+}
 
 }  // namespace
 
-BwdGrid rotary_bwd_grid(int64_t n, int Hq, int Hkv, int D) {
-  BwdGrid g{};
-  const int H = Hq + Hkv;
-  if (n == 0 || H == 0) return g;
-  g.heads_per_group = heads_per_group(n, H, 16384);
-  g.y = (int32_t)ceil_div(H, g.heads_per_group);
-  g.x = (int32_t)std::min<int64_t>(ceil_div(n, kThreads / (D / 16)), std::max<int64_t>(1, 1024 / g.y));
-  return g;
+size_t rotary_bwd_parts(int64_t n, int Hq, int Hkv, int D) {
+  TileGrid q, k;
+  int32_t tile_rows[2];
+  bwd_grids(n, Hq, Hkv, D, q, k, tile_rows);
+  return (size_t)(q.items + k.items);
 }
 
 hipError_t launch_rotary_fwd(RotaryParams p, int D, bool bf16, bool pairs, hipStream_t s) {
-  const int H = p.Hq + p.Hkv;
-  if (p.n == 0 || H == 0) return hipSuccess;
-  p.heads_per_group = heads_per_group(p.n, H, 16384);
-  const unsigned y = (unsigned)ceil_div(H, p.heads_per_group);
-  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(p.n, kThreads / (D / 16)), std::max<int64_t>(1, kMaxGrid / y)), y);
-  return dispatch<Fwd>(p, D, bf16, pairs, grid, s);
+  p.n_q = p.n;
+  p.tiles_q = tile_grid(p.n, p.Hq, p.Hq + p.Hkv, D);
+  p.tiles_k = tile_grid(p.n, p.Hkv, p.Hq + p.Hkv, D);
+  p.items = p.tiles_q.items + p.tiles_k.items;
+  if (p.items == 0) return hipSuccess;
+  return dispatch<Fwd>(p, D, bf16, pairs, grid_of(p.items), s);
 }
 
 hipError_t launch_rotary_bwd(RotaryParams p, int D, bool bf16, bool pairs, float* dwq, float* dwk, hipStream_t s) {
-  const BwdGrid g = rotary_bwd_grid(p.n, p.Hq, p.Hkv, D);
-  if (g.x > 0) {
-    p.heads_per_group = g.heads_per_group;
-    const hipError_t e = dispatch<Bwd>(p, D, bf16, pairs, dim3((unsigned)g.x, (unsigned)g.y), s);
+  p.n_q = p.n;
+  bwd_grids(p.n, p.Hq, p.Hkv, D, p.tiles_q, p.tiles_k, p.tile_rows);
+  p.items = p.tiles_q.items + p.tiles_k.items;
+  if (p.items > 0) {
+    const hipError_t e = dispatch<Bwd>(p, D, bf16, pairs, grid_of(p.items), s);
     if (e != hipSuccess) return e;
   }
   if (dwq || dwk)
-    hipLaunchKernelGGL(rotary_bwd_sum_kernel, dim3(2 * D / 16), dim3(1024), 0, s, p.part, g.x * g.y, D, dwq, dwk);
+    hipLaunchKernelGGL(rotary_bwd_sum_kernel, dim3(2 * D / 16), dim3(1024), 0, s, p.part, p.tiles_q.items,
+                       p.tiles_k.items, D, dwq, dwk);
   return hipGetLastError();
 }
 
 hipError_t launch_rotary_append(RotaryParams p, int D, bool bf16, bool pairs, hipStream_t s) {
-  const int R = kThreads / (D / 16);
-  p.heads_per_group = heads_per_group(std::max(p.n, p.n_q), p.Hq + p.Hkv, 16384);
-  const int hp = std::max(1, p.heads_per_group);
-  p.heads_per_group = hp;
-  p.items_q = p.Hq ? ceil_div(p.n_q, R) * ceil_div(p.Hq, hp) : 0;
-  p.items_k = p.Hkv ? ceil_div(p.n, R) * ceil_div(p.Hkv, hp) : 0;
-  p.items_v = ceil_div((int64_t)p.n * p.Hkv, kThreads / 64);
-  p.items = p.items_q + p.items_k + p.items_v + ceil_div(p.n_patch, kThreads);
+  p.tiles_q = tile_grid(p.n_q, p.Hq, p.Hq + p.Hkv, D);
+  p.tiles_k = tile_grid(p.n, p.Hkv, p.Hq + p.Hkv, D);
+  const bool tall = (int64_t)p.n * p.Hkv >= 16384;  // 64 rows a workgroup where that leaves every compute unit one
+  p.items_v = ceil_div(p.n, tall ? 64 : 16) * p.Hkv;
+  p.items = p.items_v + p.tiles_q.items + p.tiles_k.items + ceil_div(p.n_patch, kThreads);
   if (p.items == 0) return hipSuccess;
-  return dispatch<Append>(p, D, bf16, pairs, dim3((unsigned)std::min(p.items, kMaxGrid)), s);
+  const dim3 grid = grid_of(p.items);
+  return tall ? dispatch<Append<64>::Call>(p, D, bf16, pairs, grid, s)
+              : dispatch<Append<16>::Call>(p, D, bf16, pairs, grid, s);
 }
 
 }  // namespace padoc

@@ -2,6 +2,7 @@
 // entry points and the kernels.
 #pragma once
 
+#include <stddef.h>
 #include <stdint.h>
 
 #include "padoc_attn.h"
@@ -19,6 +20,14 @@ struct RotaryTable {
   uint8_t axis[kMaxPairs];
 };
 
+// How the rows of one tensor are cut into tiles, one workgroup each.
+struct TileGrid {
+  int32_t rows;       // rows of a tile
+  int32_t heads;      // heads of a tile
+  int32_t head_runs;  // tiles side by side over the heads
+  int64_t items;
+};
+
 struct RotaryParams {
   RotaryTable table;
   const int32_t* pos;  // [n_axes][stride]
@@ -26,19 +35,21 @@ struct RotaryParams {
   int32_t n_axes, pairs;  // pairs: rotary_dim / 2
   float scale, eps;
   int32_t inverse;  // rotate by the negative angle
-  int32_t n, Hq, Hkv;
-  int32_t heads_per_group;  // heads of a row that one lane group takes
+  int32_t n, n_q;   // rows of k (and v), of q
+  int32_t Hq, Hkv;
+  TileGrid tiles_q, tiles_k;
+  int32_t tile_rows[2];  // backward: rows of a tile of q, of k (the grids' rows: of an item)
+  int64_t items;       // workgroup items of all kinds
   padoc_heads q, k;    // in: rows, or (inverse, backward) gradients of the outputs
   padoc_heads qo, ko;  // out
   const void* wq;
   const void* wk;
   // backward with weights
   padoc_heads xq, xk;  // the forward's rows
-  float* part;         // [blocks][2][D] sums of the weights' gradients, or null
+  float* part;         // [items of q, then of k][D] sums of the weights' gradients, or null
   // append
   const int32_t* q_pos;
   int64_t q_pos_stride;
-  int32_t n_q;
   padoc_heads v;
   const int32_t* slots;
   void* k_cache;
@@ -47,7 +58,7 @@ struct RotaryParams {
   const int32_t* patch;  // (entry, block id) pairs of the block table
   int64_t n_patch;
   int32_t* block_table;
-  int64_t items_q, items_k, items_v, items;  // workgroup items of each role, and all
+  int64_t items_v;
 };
 
 struct CopyParams {
@@ -60,11 +71,7 @@ struct CopyParams {
   int64_t units;  // 16-byte units of a block, per tensor
 };
 
-// Grid of the backward's kernel over rows and heads: the partial sums it
-// leaves are counted by the host before any launch.
-struct BwdGrid {
-  int32_t x, y, heads_per_group;
-};
-BwdGrid rotary_bwd_grid(int64_t n, int Hq, int Hkv, int D);
+// Items of a backward: each leaves D sums in the workspace.
+size_t rotary_bwd_parts(int64_t n, int Hq, int Hkv, int D);
 
 }  // namespace padoc
