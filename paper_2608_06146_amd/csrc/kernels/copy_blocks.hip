@@ -3,7 +3,12 @@
 // last block, a compaction moves blocks to the front of the pool).
 //
 // A copy, bound by memory.  One workgroup copies up to 8 KB of one tensor of one
-// pair: two 16-byte loads in flight per lane.
+// pair: two 16-byte loads in flight per lane, past the caches both ways.
+// Measured on one MI355X, 16,384 pairs drawn over a pool of 40,968 blocks of 2
+// heads, d = 128, bf16 (537 MB read and written): 108 us (5.0 TB/s); with plain
+// loads and stores 112; workgroups of 64, 128 or 512 threads, or 1,024 to 8,192
+// workgroups that stride, 108 to 113.  (A plain copy of as many contiguous bytes
+// takes 99.)
 #include <hip/hip_runtime.h>
 
 #include "../rotary.hpp"
@@ -26,10 +31,10 @@ __global__ __launch_bounds__(kThreads) void copy_blocks_kernel(const CopyParams 
     u32x4 x[kUnroll];
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i)
-      if (u0 + i * kThreads < p.units) x[i] = src[u0 + i * kThreads];
+      if (u0 + i * kThreads < p.units) x[i] = __builtin_nontemporal_load(src + u0 + i * kThreads);
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i)
-      if (u0 + i * kThreads < p.units) dst[u0 + i * kThreads] = x[i];
+      if (u0 + i * kThreads < p.units) __builtin_nontemporal_store(x[i], dst + u0 + i * kThreads);
   }
 }
 

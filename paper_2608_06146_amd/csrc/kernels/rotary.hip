@@ -8,9 +8,8 @@
 //
 // All of it is bound by memory: every element is read once and written once.
 // A row of one head is shared by D / 16 lanes (a group).  Lane l of a group
-// holds 16 dimensions: the eight pairs 8l .. 8l+7, so that a rotation stays
-// inside a lane and its memory accesses are 16 bytes each; where only the
-// leading dimensions are rotated, the lanes behind them hold the rest.
+// holds 16 dimensions in units of 16 bytes, chosen so that both members of a
+// pair are in one lane and the lanes of a group access neighbouring units.
 //
 // A workgroup takes a tile of rows of one tensor (q or k).  Its lanes compute
 // the cosines and sines of the tile's rows once, a pair each, into LDS; its
@@ -38,52 +37,66 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 
-// A lane's 16 elements of a head as they were loaded: its two chunks of eight,
-// one after the other, at addresses aligned to one element.
+// Elements of a 16-byte unit, the size of a lane's memory accesses, and units
+// of a lane.
 template <typename T>
-struct Raw;
+constexpr int kUnit = 16 / (int)sizeof(T);
+template <typename T>
+constexpr int kUnits = 16 / kUnit<T>;
+
+// A 16-byte unit at an address aligned to one element.
+template <typename T>
+struct Unit;
 template <>
-struct Raw<__bf16> {
-  typedef u32x4 unit __attribute__((aligned(2)));
-  u32x4 u[2];
-  __device__ __forceinline__ void load(const __bf16* p, const int (&at)[2]) {
-    u[0] = *reinterpret_cast<const unit*>(p + at[0]);
-    u[1] = *reinterpret_cast<const unit*>(p + at[1]);
-  }
-  __device__ __forceinline__ void get(float (&x)[16]) const {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      x[2 * i] = __uint_as_float(u[i / 4][i % 4] << 16);
-      x[2 * i + 1] = __uint_as_float(u[i / 4][i % 4] & 0xffff0000u);
-    }
-  }
+struct Unit<__bf16> {
+  typedef u32x4 type __attribute__((aligned(2)));
 };
 template <>
-struct Raw<float> {
-  typedef f32x4 unit __attribute__((aligned(4)));
-  f32x4 u[4];
-  __device__ __forceinline__ void load(const float* p, const int (&at)[2]) {
+struct Unit<float> {
+  typedef u32x4 type __attribute__((aligned(4)));
+};
+
+// A lane's 16 elements of a head as they were loaded: its units in turn.
+template <typename T>
+struct Raw {
+  u32x4 u[kUnits<T>];
+  // Rows are read once, past the caches' newer lines (non-temporal): with plain
+  // loads the forward of 43,067 rows of 18 heads takes 79.3 us, not 67.5 (bf16,
+  // d = 128; 5.9 TB/s), its backward 123.3, not 107.7.  (Non-temporal stores
+  // beside them: 72.6 and 114.5.)
+  __device__ __forceinline__ void load_row(const T* p, const int (&at)[kUnits<T>]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) u[i] = *reinterpret_cast<const unit*>(p + at[i / 2] + 4 * (i % 2));
+    for (int i = 0; i < kUnits<T>; ++i)
+      u[i] = __builtin_nontemporal_load(reinterpret_cast<const typename Unit<T>::type*>(p + at[i]));
+  }
+  __device__ __forceinline__ void load_weight(const T* p, const int (&at)[kUnits<T>]) {
+#pragma unroll
+    for (int i = 0; i < kUnits<T>; ++i) u[i] = *reinterpret_cast<const typename Unit<T>::type*>(p + at[i]);
   }
   __device__ __forceinline__ void get(float (&x)[16]) const {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = u[i / 4][i % 4];
+    for (int i = 0; i < 16; ++i)
+      x[i] = sizeof(T) == 4 ? __uint_as_float(u[i / 4 % kUnits<T>][i % 4])
+                            : __uint_as_float(i % 2 ? u[i / 8][i % 8 / 2] & 0xffff0000u : u[i / 8][i % 8 / 2] << 16);
   }
 };
 
-// Eight elements, rounded to nearest-even once, here (NaN stays NaN).
-__device__ __forceinline__ void store8(__bf16* p, const float* x) {
-  typedef u32x4 unit __attribute__((aligned(2)));
+// One unit's elements, rounded to nearest-even once, here (NaN stays NaN).
+__device__ __forceinline__ void store_unit(__bf16* p, const float* x) {
   const bf16x8 b = __builtin_convertvector((f32x8{x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]}), bf16x8);
   u32x4 u;
   __builtin_memcpy(&u, &b, 16);
-  *reinterpret_cast<unit*>(p) = u;
+  *reinterpret_cast<Unit<__bf16>::type*>(p) = u;
 }
-__device__ __forceinline__ void store8(float* p, const float* x) {
-  typedef f32x4 unit __attribute__((aligned(4)));
-  reinterpret_cast<unit*>(p)[0] = f32x4{x[0], x[1], x[2], x[3]};
-  reinterpret_cast<unit*>(p)[1] = f32x4{x[4], x[5], x[6], x[7]};
+__device__ __forceinline__ void store_unit(float* p, const float* x) {
+  u32x4 u;
+  __builtin_memcpy(&u, x, 16);
+  *reinterpret_cast<Unit<float>::type*>(p) = u;
+}
+template <typename T>
+__device__ __forceinline__ void store_row(T* p, const int (&at)[kUnits<T>], const float (&x)[16]) {
+#pragma unroll
+  for (int i = 0; i < kUnits<T>; ++i) store_unit(p + at[i], x + i * kUnit<T>);
 }
 
 // Sum over the L (4 or 8) lanes of a group, in every one of them.
@@ -108,34 +121,48 @@ __device__ __forceinline__ void sincos_turns(uint32_t phase, float& s, float& c)
   if ((quadrant + 1) & 2) c = -c;
 }
 
-// A lane's place in its group: element offsets of its two 8-element chunks,
-// and whether it holds rotated pairs.
-template <int D, bool PAIRS>
+// A lane's place in its group: which units it holds, in an order that keeps a
+// group's accesses side by side and both members of a pair in one lane.
+//   pairs of neighbours: units l, l + L, ... in turn
+//   halves: units k and k + n (n = units of half the rotated dimensions) for k =
+//   l, l + L, ...; behind the n rotated ones, k stands for two of the others
+// Pair m of a lane (0 .. 7) has elements first(m) and second(m).
+template <typename T, int D, bool PAIRS>
 struct Place {
-  int at[2];
-  int first_pair;
-  bool turned;
+  static constexpr int L = D / 16, E = kUnit<T>, N = kUnits<T>;
+  static constexpr int kPairsPerSlot = PAIRS ? E / 2 : E;
+  static constexpr int kSlots = 8 / kPairsPerSlot;  // a lane's units (PAIRS) or pairs of units
+  int at[N];
+  int turned;  // slots 0 .. turned-1 are rotated
   __device__ __forceinline__ Place(int lane, int pairs) {
-    first_pair = 8 * lane;
-    turned = first_pair < pairs;
-    if (PAIRS || !turned) {  // neighbouring chunks (behind the rotated ones: the same in both styles)
-      at[0] = 16 * lane;
-      at[1] = 16 * lane + 8;
-    } else {
-      at[0] = 8 * lane;
-      at[1] = 8 * lane + pairs;
+    const int n = pairs / kPairsPerSlot;  // rotated slots of the group
+    turned = 0;
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) {
+      const int k = i * L + lane;
+      turned += k < n;
+      if (PAIRS) {
+        at[i] = k * E;
+      } else {
+        at[2 * i] = (k < n ? k : n + k) * E;
+        at[2 * i + 1] = (k < n ? k + n : D / 2 / E + k) * E;
+      }
     }
   }
-};
-
-struct Angles {
-  float c[8], s[8];
+  static constexpr int first(int m) { return PAIRS ? 2 * m : m / E * (2 * E) + m % E; }
+  static constexpr int second(int m) { return PAIRS ? 2 * m + 1 : m / E * (2 * E) + E + m % E; }
+  // Lane and place in the lane of a pair.
+  static __device__ __forceinline__ int lane_of(int pair) { return pair / kPairsPerSlot % L; }
+  static __device__ __forceinline__ int index_of(int pair) {
+    return pair / kPairsPerSlot / L * kPairsPerSlot + pair % kPairsPerSlot;
+  }
 };
 
 // Cosines and sines of a tile's rows: per row and quarter i of a lane's pairs
 // (two of them), the lanes' 16 bytes side by side.
-template <int D>
+template <typename T, int D, bool PAIRS>
 struct AngleTable {
+  typedef Place<T, D, PAIRS> P;
   static constexpr int kLanes = D / 16;
   static constexpr int kRows = 4096 / D;  // rows of a tile, at most
   f32x4 at[kRows][4][kLanes];
@@ -148,37 +175,37 @@ struct AngleTable {
     if (pair >= p.pairs) return;
     const uint64_t turn = p.table.turn[pair];
     pos += p.table.axis[pair] * stride + row0;
-    float* dst = reinterpret_cast<float*>(&at[0][pair % 8 / 2][pair / 8]) + pair % 2 * 2;
+    const int m = P::index_of(pair);
+    float* dst = reinterpret_cast<float*>(&at[0][m / 2][P::lane_of(pair)]) + m % 2 * 2;
     for (int r = threadIdx.x / kPairs; r < n; r += kThreads / kPairs) {
       float s, c;
       sincos_turns((uint32_t)((uint64_t)(int64_t)pos[r] * turn >> 32), s, c);
-      dst[r * (D / 16 * 16)] = c * p.scale;
-      dst[r * (D / 16 * 16) + 1] = p.inverse ? -s * p.scale : s * p.scale;
+      dst[r * D] = c * p.scale;
+      dst[r * D + 1] = p.inverse ? -s * p.scale : s * p.scale;
     }
-  }
-  __device__ __forceinline__ Angles get(int row, int lane) const {
-    Angles a;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const f32x4 x = at[row][i][lane];
-      a.c[2 * i] = x[0];
-      a.s[2 * i] = x[1];
-      a.c[2 * i + 1] = x[2];
-      a.s[2 * i + 1] = x[3];
-    }
-    return a;
   }
 };
 
-// Rotate a lane's pairs.
-template <bool PAIRS>
-__device__ __forceinline__ void turn(float (&x)[16], const Angles& t) {
+// Rotate a lane's pairs by the angles of a row of the table.
+template <typename T, int D, bool PAIRS>
+__device__ __forceinline__ void turn(float (&x)[16], const AngleTable<T, D, PAIRS>& table, int row,
+                                     const Place<T, D, PAIRS>& pl) {
+  typedef Place<T, D, PAIRS> P;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int a = PAIRS ? 2 * j : j, b = PAIRS ? 2 * j + 1 : 8 + j;
-    const float ya = x[a], yb = x[b];
-    x[a] = ya * t.c[j] - yb * t.s[j];
-    x[b] = yb * t.c[j] + ya * t.s[j];
+  for (int slot = 0; slot < P::kSlots; ++slot) {
+    if (slot >= pl.turned) break;
+#pragma unroll
+    for (int i = 0; i < P::kPairsPerSlot / 2; ++i) {
+      const int m0 = slot * P::kPairsPerSlot + 2 * i;
+      const f32x4 t = table.at[row][m0 / 2][threadIdx.x % P::L];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int a = P::first(m0 + j), b = P::second(m0 + j);
+        const float c = t[2 * j], s = t[2 * j + 1], ya = x[a], yb = x[b];
+        x[a] = ya * c - yb * s;
+        x[b] = yb * c + ya * s;
+      }
+    }
   }
 }
 
@@ -195,9 +222,9 @@ __device__ __forceinline__ const T* head_row(const padoc_heads& x, int64_t row, 
   return static_cast<const T*>(x.data) + row * x.row_stride + h * x.head_stride;
 }
 
-// Rows that a lane has in flight at once.
-template <typename T>
-constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;
+// Rows that a lane has in flight at once (4: more registers, 67.7 us where 2
+// take 65.9).
+constexpr int kAhead = 2;
 
 // A tile of one tensor (q's or k's) as a workgroup sees it.
 struct Tile {
@@ -251,17 +278,17 @@ struct Cursor {
 // before theirs.
 template <typename T, int D, bool PAIRS, class Put>
 __device__ __forceinline__ void turn_tile(const RotaryParams& p, const Tile& t, const int32_t* pos, int64_t pos_stride,
-                                          AngleTable<D>& table, const Place<D, PAIRS>& pl, Put put) {
-  constexpr int L = D / 16, R = kThreads / L, U = kAhead<T>;
+                                          AngleTable<T, D, PAIRS>& table, const Place<T, D, PAIRS>& pl, Put put) {
+  constexpr int L = D / 16, R = kThreads / L, U = kAhead;
   const int dr = R / t.heads, dh = R - dr * t.heads;
   Cursor ahead(t, threadIdx.x / L), at = ahead;
   Raw<T> raw[U], rw;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    if (ahead.row < t.rows) raw[u].load(ahead.at<const T>(t.in, t), pl.at);
+    if (ahead.row < t.rows) raw[u].load_row(ahead.at<const T>(t.in, t), pl.at);
     ahead.next(t, dr, dh);
   }
-  if (t.w) rw.load(static_cast<const T*>(t.w), pl.at);
+  if (t.w) rw.load_weight(static_cast<const T*>(t.w), pl.at);
   table.fill(p, pos, pos_stride, t.row0, t.rows);
   __syncthreads();
   float wt[16];
@@ -272,14 +299,14 @@ __device__ __forceinline__ void turn_tile(const RotaryParams& p, const Tile& t, 
       if (at.row >= t.rows) break;
       float x[16];
       raw[u].get(x);
-      if (ahead.row < t.rows) raw[u].load(ahead.at<const T>(t.in, t), pl.at);
+      if (ahead.row < t.rows) raw[u].load_row(ahead.at<const T>(t.in, t), pl.at);
       ahead.next(t, dr, dh);
       if (t.w) {
         const float rho = rms_scale<D>(x, p.eps);
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] *= rho * wt[i];
       }
-      if (pl.turned) turn<PAIRS>(x, table.get(at.row, threadIdx.x % L));
+      turn(x, table, at.row, pl);
       put(at, x);
       at.next(t, dr, dh);
     }
@@ -290,14 +317,12 @@ __device__ __forceinline__ void turn_tile(const RotaryParams& p, const Tile& t, 
 // Forward (and, with `inverse`, the backward of a rotation without norms).
 template <typename T, int D, bool PAIRS>
 __global__ __launch_bounds__(kThreads) void rotary_fwd_kernel(const RotaryParams p) {
-  __shared__ AngleTable<D> table;
-  const Place<D, PAIRS> pl(threadIdx.x % (D / 16), p.pairs);
+  __shared__ AngleTable<T, D, PAIRS> table;
+  const Place<T, D, PAIRS> pl(threadIdx.x % (D / 16), p.pairs);
   for (int64_t b = blockIdx.x; b < p.items; b += gridDim.x) {
     const Tile t = tile_of(p, b);
     turn_tile<T, D, PAIRS>(p, t, p.pos, p.pos_stride, table, pl, [&](const Cursor& c, const float (&x)[16]) {
-      T* dst = c.at<T>(t.out, t);
-      store8(dst + pl.at[0], x);
-      store8(dst + pl.at[1], x + 8);
+      store_row(c.at<T>(t.out, t), pl.at, x);
     });
   }
 }
@@ -307,10 +332,10 @@ __global__ __launch_bounds__(kThreads) void rotary_fwd_kernel(const RotaryParams
 // wavefront and over the four wavefronts through LDS, into part[item][D].
 template <typename T, int D, bool PAIRS>
 __global__ __launch_bounds__(kThreads) void rotary_bwd_kernel(const RotaryParams p) {
-  constexpr int L = D / 16, R = kThreads / L, U = kAhead<T> / 2;
-  __shared__ AngleTable<D> table;
+  constexpr int L = D / 16, R = kThreads / L, U = sizeof(T) == 2 ? 2 : 1;  // of each tensor
+  __shared__ AngleTable<T, D, PAIRS> table;
   __shared__ float sums[kThreads / 64][D];
-  const Place<D, PAIRS> pl(threadIdx.x % L, p.pairs);
+  const Place<T, D, PAIRS> pl(threadIdx.x % L, p.pairs);
   for (int64_t b = blockIdx.x; b < p.items; b += gridDim.x) {
     Tile t = tile_of(p, b);
     const int64_t row_end = t.row0 + t.rows;
@@ -318,7 +343,7 @@ __global__ __launch_bounds__(kThreads) void rotary_bwd_kernel(const RotaryParams
     float acc[16] = {}, wt[16];
     if (t.w) {
       Raw<T> rw;
-      rw.load(static_cast<const T*>(t.w), pl.at);
+      rw.load_weight(static_cast<const T*>(t.w), pl.at);
       rw.get(wt);
     }
     for (; t.row0 < row_end; t.row0 += p.tile_rows[b >= p.tiles_q.items]) {
@@ -328,8 +353,8 @@ __global__ __launch_bounds__(kThreads) void rotary_bwd_kernel(const RotaryParams
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (ahead.row < t.rows) {
-          rg[u].load(ahead.at<const T>(t.in, t), pl.at);
-          if (t.w) rx[u].load(ahead.at<const T>(t.x, t), pl.at);
+          rg[u].load_row(ahead.at<const T>(t.in, t), pl.at);
+          if (t.w) rx[u].load_row(ahead.at<const T>(t.x, t), pl.at);
         }
         ahead.next(t, dr, dh);
       }
@@ -343,11 +368,11 @@ __global__ __launch_bounds__(kThreads) void rotary_bwd_kernel(const RotaryParams
           rg[u].get(g);
           if (t.w) rx[u].get(x);
           if (ahead.row < t.rows) {
-            rg[u].load(ahead.at<const T>(t.in, t), pl.at);
-            if (t.w) rx[u].load(ahead.at<const T>(t.x, t), pl.at);
+            rg[u].load_row(ahead.at<const T>(t.in, t), pl.at);
+            if (t.w) rx[u].load_row(ahead.at<const T>(t.x, t), pl.at);
           }
           ahead.next(t, dr, dh);
-          if (pl.turned) turn<PAIRS>(g, table.get(at.row, threadIdx.x % L));
+          turn(g, table, at.row, pl);
           if (t.w) {
             const float rho = rms_scale<D>(x, p.eps);
             float dot = 0.f;
@@ -362,9 +387,7 @@ __global__ __launch_bounds__(kThreads) void rotary_bwd_kernel(const RotaryParams
 #pragma unroll
             for (int i = 0; i < 16; ++i) g[i] = rho * (g[i] - x[i] * mean);
           }
-          T* dst = at.at<T>(t.out, t);
-          store8(dst + pl.at[0], g);
-          store8(dst + pl.at[1], g + 8);
+          store_row(at.at<T>(t.out, t), pl.at, g);
           at.next(t, dr, dh);
         }
       }
@@ -376,7 +399,7 @@ __global__ __launch_bounds__(kThreads) void rotary_bwd_kernel(const RotaryParams
       float v = acc[i];
 #pragma unroll
       for (int m = L; m < 64; m *= 2) v += __shfl_xor(v, m);
-      if (threadIdx.x % 64 < L) sums[threadIdx.x / 64][pl.at[i / 8] + i % 8] = v;
+      if (threadIdx.x % 64 < L) sums[threadIdx.x / 64][pl.at[i / kUnit<T>] + i % kUnit<T>] = v;
     }
     __syncthreads();
     if (threadIdx.x < D) {
@@ -389,11 +412,11 @@ __global__ __launch_bounds__(kThreads) void rotary_bwd_kernel(const RotaryParams
   }
 }
 
-// Sums of the items' parts in a fixed order: 16 columns of one tensor a
-// workgroup (q's, then k's), 64 of its rows side by side.
+// Sums of the items' parts in a fixed order, in 64 bits: 16 columns of one
+// tensor a workgroup (q's, then k's), 64 of its rows side by side.
 __global__ __launch_bounds__(1024) void rotary_bwd_sum_kernel(const float* __restrict__ part, int64_t n_q, int64_t n_k,
                                                               int D, float* dwq, float* dwk) {
-  __shared__ float sums[64][17];
+  __shared__ double sums[16][16];
   const int col = threadIdx.x % 16, r0 = threadIdx.x / 16;
   const bool is_q = (int)blockIdx.x * 16 < D;
   const int at = blockIdx.x * 16 + col - (is_q ? 0 : D);
@@ -401,15 +424,18 @@ __global__ __launch_bounds__(1024) void rotary_bwd_sum_kernel(const float* __res
   if (!dw) return;
   const float* src = part + (is_q ? 0 : n_q * D) + at;
   const int64_t n = is_q ? n_q : n_k;
-  float v = 0.f;
-#pragma unroll 4
+  double v = 0;
+#pragma unroll 8
   for (int64_t r = r0; r < n; r += 64) v += src[r * D];
-  sums[r0][col] = v;
+  v += __shfl_xor(v, 16);
+  v += __shfl_xor(v, 32);
+  if (threadIdx.x % 64 < 16) sums[threadIdx.x / 64][col] = v;
   __syncthreads();
   if (threadIdx.x >= 16) return;
-  v = 0.f;
-  for (int r = 0; r < 64; ++r) v += sums[r][col];
-  dw[at] = v;
+  v = 0;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) v += sums[r][col];
+  dw[at] = (float)v;
 }
 
 __device__ __forceinline__ bool slot_of(const RotaryParams& p, int64_t row, int32_t& blk, int32_t& slot) {
@@ -457,7 +483,8 @@ __device__ __forceinline__ void append_v(const RotaryParams& p, int64_t item, VT
   for (int u = tid; u < kUnits; u += kThreads) {
     const int r = u / (D / E), c = u % (D / E) * E;
     if (first + r < p.n) {
-      const auto x = *reinterpret_cast<const typename Raw<T>::unit*>(head_row<T>(p.v, first + r, h) + c);
+      const u32x4 x =
+          __builtin_nontemporal_load(reinterpret_cast<const typename Unit<T>::type*>(head_row<T>(p.v, first + r, h) + c));
       T y[E];
       __builtin_memcpy(y, &x, 16);
 #pragma unroll
@@ -503,11 +530,11 @@ __device__ __forceinline__ void append_v(const RotaryParams& p, int64_t item, VT
 template <typename T, int D, bool PAIRS, int ROWS>
 __global__ __launch_bounds__(kThreads) void rotary_append_kernel(const RotaryParams p) {
   __shared__ union Shared {
-    AngleTable<D> table;
+    AngleTable<T, D, PAIRS> table;
     VTile<T, D, ROWS> v;
     __device__ Shared() {}
   } shared;
-  const Place<D, PAIRS> pl(threadIdx.x % (D / 16), p.pairs);
+  const Place<T, D, PAIRS> pl(threadIdx.x % (D / 16), p.pairs);
   for (int64_t b = blockIdx.x; b < p.items; b += gridDim.x) {
     if (b < p.items_v) {
       append_v<T, D, ROWS>(p, b, shared.v);
@@ -525,15 +552,15 @@ __global__ __launch_bounds__(kThreads) void rotary_append_kernel(const RotaryPar
     turn_tile<T, D, PAIRS>(p, t, is_q ? p.q_pos : p.pos, is_q ? p.q_pos_stride : p.pos_stride, shared.table, pl,
                            [&](const Cursor& c, const float (&x)[16]) {
       if (is_q) {
-        T* dst = c.at<T>(t.out, t);
-        store8(dst + pl.at[0], x);
-        store8(dst + pl.at[1], x + 8);
+        store_row(c.at<T>(t.out, t), pl.at, x);
         return;
       }
       int32_t blk, slot;
       if (!slot_of(p, t.row0 + c.row, blk, slot)) return;
-      store8(cache + paged_k_offset<D>(blk, t.h0 + c.h, p.Hkv, slot, pl.at[0] / 8), x);
-      store8(cache + paged_k_offset<D>(blk, t.h0 + c.h, p.Hkv, slot, pl.at[1] / 8), x + 8);
+#pragma unroll
+      for (int u = 0; u < kUnits<T>; ++u)
+        store_unit(cache + paged_k_offset<D>(blk, t.h0 + c.h, p.Hkv, slot, pl.at[u] / 8) + pl.at[u] % 8,
+                   x + u * kUnit<T>);
     });
   }
 }
@@ -551,7 +578,7 @@ TileGrid tile_grid(int64_t n, int H, int H_all, int D) {
   TileGrid g{};
   if (n == 0 || H == 0) return g;
   const int64_t groups = kThreads / (D / 16);
-  const int64_t turns = std::min<int64_t>(kMaxTurns, std::max<int64_t>(1, n * H_all / (groups * kItems)));
+  const int64_t turns = std::min<int64_t>(kMaxTurns, ceil_div(n * H_all, groups * kItems));
   g.heads = (int32_t)std::min<int64_t>(H, groups * turns);
   g.head_runs = (int32_t)ceil_div(H, g.heads);
   g.rows = (int32_t)std::max<int64_t>(1, std::min<int64_t>({groups * turns / g.heads, 4096 / D, n}));
@@ -650,12 +677,12 @@ hipError_t launch_rotary_append(RotaryParams p, int D, bool bf16, bool pairs, hi
   p.tiles_q = tile_grid(p.n_q, p.Hq, p.Hq + p.Hkv, D);
   p.tiles_k = tile_grid(p.n, p.Hkv, p.Hq + p.Hkv, D);
   const bool tall = (int64_t)p.n * p.Hkv >= 16384;  // 64 rows a workgroup where that leaves every compute unit one
-  p.items_v = ceil_div(p.n, tall ? 64 : 16) * p.Hkv;
+  p.items_v = ceil_div(p.n, tall ? 64 : 8) * p.Hkv;
   p.items = p.items_v + p.tiles_q.items + p.tiles_k.items + ceil_div(p.n_patch, kThreads);
   if (p.items == 0) return hipSuccess;
   const dim3 grid = grid_of(p.items);
   return tall ? dispatch<Append<64>::Call>(p, D, bf16, pairs, grid, s)
-              : dispatch<Append<16>::Call>(p, D, bf16, pairs, grid, s);
+              : dispatch<Append<8>::Call>(p, D, bf16, pairs, grid, s);
 }
 
 }  // namespace padoc
