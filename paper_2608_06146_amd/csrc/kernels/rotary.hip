@@ -44,6 +44,14 @@ constexpr int kUnit = 16 / (int)sizeof(T);
 template <typename T>
 constexpr int kUnits = 16 / kUnit<T>;
 
+// Whether rows are loaded and stored past the caches (non-temporal): where an
+// access of a group covers whole 128-byte lines.  Measured, in turn over more
+// data than the caches hold (bf16): 43,067 rows of 18 heads of 128 70.1 us (5.7
+// TB/s) with, 78.8 without; 20,000 rows of 32 heads of 64, whose lines two
+// accesses share, 39.5 either way forward, 71.7 with and 69.4 without backward.
+template <int D>
+constexpr bool kStream = D == 128;
+
 // A 16-byte unit at an address aligned to one element.
 template <typename T>
 struct Unit;
@@ -60,18 +68,13 @@ struct Unit<float> {
 template <typename T>
 struct Raw {
   u32x4 u[kUnits<T>];
-  // Rows are read once, past the caches' newer lines (non-temporal): with plain
-  // loads the forward of 43,067 rows of 18 heads takes 79.3 us, not 67.5 (bf16,
-  // d = 128; 5.9 TB/s), its backward 123.3, not 107.7.  (Non-temporal stores
-  // beside them: 72.6 and 114.5.)
+  template <bool STREAM>
   __device__ __forceinline__ void load_row(const T* p, const int (&at)[kUnits<T>]) {
 #pragma unroll
-    for (int i = 0; i < kUnits<T>; ++i)
-      u[i] = __builtin_nontemporal_load(reinterpret_cast<const typename Unit<T>::type*>(p + at[i]));
-  }
-  __device__ __forceinline__ void load_weight(const T* p, const int (&at)[kUnits<T>]) {
-#pragma unroll
-    for (int i = 0; i < kUnits<T>; ++i) u[i] = *reinterpret_cast<const typename Unit<T>::type*>(p + at[i]);
+    for (int i = 0; i < kUnits<T>; ++i) {
+      const auto q = reinterpret_cast<const typename Unit<T>::type*>(p + at[i]);
+      u[i] = STREAM ? __builtin_nontemporal_load(q) : *q;
+    }
   }
   __device__ __forceinline__ void get(float (&x)[16]) const {
 #pragma unroll
@@ -82,21 +85,31 @@ struct Raw {
 };
 
 // One unit's elements, rounded to nearest-even once, here (NaN stays NaN).
+template <bool STREAM>
 __device__ __forceinline__ void store_unit(__bf16* p, const float* x) {
   const bf16x8 b = __builtin_convertvector((f32x8{x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]}), bf16x8);
   u32x4 u;
   __builtin_memcpy(&u, &b, 16);
-  *reinterpret_cast<Unit<__bf16>::type*>(p) = u;
+  const auto q = reinterpret_cast<Unit<__bf16>::type*>(p);
+  if (STREAM)
+    __builtin_nontemporal_store(u, q);
+  else
+    *q = u;
 }
+template <bool STREAM>
 __device__ __forceinline__ void store_unit(float* p, const float* x) {
   u32x4 u;
   __builtin_memcpy(&u, x, 16);
-  *reinterpret_cast<Unit<float>::type*>(p) = u;
+  const auto q = reinterpret_cast<Unit<float>::type*>(p);
+  if (STREAM)
+    __builtin_nontemporal_store(u, q);
+  else
+    *q = u;
 }
-template <typename T>
+template <bool STREAM, typename T>
 __device__ __forceinline__ void store_row(T* p, const int (&at)[kUnits<T>], const float (&x)[16]) {
 #pragma unroll
-  for (int i = 0; i < kUnits<T>; ++i) store_unit(p + at[i], x + i * kUnit<T>);
+  for (int i = 0; i < kUnits<T>; ++i) store_unit<STREAM>(p + at[i], x + i * kUnit<T>);
 }
 
 // Sum over the L (4 or 8) lanes of a group, in every one of them.
@@ -285,10 +298,10 @@ __device__ __forceinline__ void turn_tile(const RotaryParams& p, const Tile& t, 
   Raw<T> raw[U], rw;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    if (ahead.row < t.rows) raw[u].load_row(ahead.at<const T>(t.in, t), pl.at);
+    if (ahead.row < t.rows) raw[u].template load_row<kStream<D>>(ahead.at<const T>(t.in, t), pl.at);
     ahead.next(t, dr, dh);
   }
-  if (t.w) rw.load_weight(static_cast<const T*>(t.w), pl.at);
+  if (t.w) rw.template load_row<false>(static_cast<const T*>(t.w), pl.at);
   table.fill(p, pos, pos_stride, t.row0, t.rows);
   __syncthreads();
   float wt[16];
@@ -299,7 +312,7 @@ __device__ __forceinline__ void turn_tile(const RotaryParams& p, const Tile& t, 
       if (at.row >= t.rows) break;
       float x[16];
       raw[u].get(x);
-      if (ahead.row < t.rows) raw[u].load_row(ahead.at<const T>(t.in, t), pl.at);
+      if (ahead.row < t.rows) raw[u].template load_row<kStream<D>>(ahead.at<const T>(t.in, t), pl.at);
       ahead.next(t, dr, dh);
       if (t.w) {
         const float rho = rms_scale<D>(x, p.eps);
@@ -321,15 +334,17 @@ __global__ __launch_bounds__(kThreads) void rotary_fwd_kernel(const RotaryParams
   const Place<T, D, PAIRS> pl(threadIdx.x % (D / 16), p.pairs);
   for (int64_t b = blockIdx.x; b < p.items; b += gridDim.x) {
     const Tile t = tile_of(p, b);
-    turn_tile<T, D, PAIRS>(p, t, p.pos, p.pos_stride, table, pl, [&](const Cursor& c, const float (&x)[16]) {
-      store_row(c.at<T>(t.out, t), pl.at, x);
+    turn_tile(p, t, p.pos, p.pos_stride, table, pl, [&](const Cursor& c, const float (&x)[16]) {
+      store_row<kStream<D>>(c.at<T>(t.out, t), pl.at, x);
     });
   }
 }
 
-// Backward: dx of p.passes tiles one after the other, and the weight's gradient
-// over them (fp32): in acc, lane by lane, then over the lanes of equal l of a
-// wavefront and over the four wavefronts through LDS, into part[item][D].
+// Backward: dx of an item's tiles, and the weight's gradient over them (fp32):
+// in acc, lane by lane, then over the lanes that hold the same dimensions of a
+// wavefront and over the four wavefronts through LDS, into part[item][D].  The
+// tiles of an item lie as many rows apart as all items take at once, so that
+// what the chip reads at a time is one stretch of memory.
 template <typename T, int D, bool PAIRS>
 __global__ __launch_bounds__(kThreads) void rotary_bwd_kernel(const RotaryParams p) {
   constexpr int L = D / 16, R = kThreads / L, U = sizeof(T) == 2 ? 2 : 1;  // of each tensor
@@ -338,23 +353,24 @@ __global__ __launch_bounds__(kThreads) void rotary_bwd_kernel(const RotaryParams
   const Place<T, D, PAIRS> pl(threadIdx.x % L, p.pairs);
   for (int64_t b = blockIdx.x; b < p.items; b += gridDim.x) {
     Tile t = tile_of(p, b);
-    const int64_t row_end = t.row0 + t.rows;
     const int dr = R / t.heads, dh = R - dr * t.heads;
     float acc[16] = {}, wt[16];
     if (t.w) {
       Raw<T> rw;
-      rw.load_weight(static_cast<const T*>(t.w), pl.at);
+      rw.template load_row<false>(static_cast<const T*>(t.w), pl.at);
       rw.get(wt);
     }
-    for (; t.row0 < row_end; t.row0 += p.tile_rows[b >= p.tiles_q.items]) {
-      t.rows = (int)min((int64_t)p.tile_rows[b >= p.tiles_q.items], row_end - t.row0);
+    const TileGrid& grid = b < p.tiles_q.items ? p.tiles_q : p.tiles_k;
+    const int64_t apart = grid.items / grid.head_runs * grid.rows;
+    for (; t.row0 < p.n; t.row0 += apart) {
+      t.rows = (int)min((int64_t)grid.rows, p.n - t.row0);
       Cursor ahead(t, threadIdx.x / L), at = ahead;
       Raw<T> rg[U], rx[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (ahead.row < t.rows) {
-          rg[u].load_row(ahead.at<const T>(t.in, t), pl.at);
-          if (t.w) rx[u].load_row(ahead.at<const T>(t.x, t), pl.at);
+          rg[u].template load_row<kStream<D>>(ahead.at<const T>(t.in, t), pl.at);
+          if (t.w) rx[u].template load_row<kStream<D>>(ahead.at<const T>(t.x, t), pl.at);
         }
         ahead.next(t, dr, dh);
       }
@@ -368,8 +384,8 @@ __global__ __launch_bounds__(kThreads) void rotary_bwd_kernel(const RotaryParams
           rg[u].get(g);
           if (t.w) rx[u].get(x);
           if (ahead.row < t.rows) {
-            rg[u].load_row(ahead.at<const T>(t.in, t), pl.at);
-            if (t.w) rx[u].load_row(ahead.at<const T>(t.x, t), pl.at);
+            rg[u].template load_row<kStream<D>>(ahead.at<const T>(t.in, t), pl.at);
+            if (t.w) rx[u].template load_row<kStream<D>>(ahead.at<const T>(t.x, t), pl.at);
           }
           ahead.next(t, dr, dh);
           turn(g, table, at.row, pl);
@@ -387,7 +403,7 @@ __global__ __launch_bounds__(kThreads) void rotary_bwd_kernel(const RotaryParams
 #pragma unroll
             for (int i = 0; i < 16; ++i) g[i] = rho * (g[i] - x[i] * mean);
           }
-          store_row(at.at<T>(t.out, t), pl.at, g);
+          store_row<kStream<D>>(at.at<T>(t.out, t), pl.at, g);
           at.next(t, dr, dh);
         }
       }
@@ -549,17 +565,17 @@ __global__ __launch_bounds__(kThreads) void rotary_append_kernel(const RotaryPar
     const Tile t = tile_of(p, i);
     const bool is_q = i < n_q;
     T* cache = static_cast<T*>(p.k_cache);
-    turn_tile<T, D, PAIRS>(p, t, is_q ? p.q_pos : p.pos, is_q ? p.q_pos_stride : p.pos_stride, shared.table, pl,
+    turn_tile(p, t, is_q ? p.q_pos : p.pos, is_q ? p.q_pos_stride : p.pos_stride, shared.table, pl,
                            [&](const Cursor& c, const float (&x)[16]) {
       if (is_q) {
-        store_row(c.at<T>(t.out, t), pl.at, x);
+        store_row<kStream<D>>(c.at<T>(t.out, t), pl.at, x);
         return;
       }
       int32_t blk, slot;
       if (!slot_of(p, t.row0 + c.row, blk, slot)) return;
 #pragma unroll
       for (int u = 0; u < kUnits<T>; ++u)
-        store_unit(cache + paged_k_offset<D>(blk, t.h0 + c.h, p.Hkv, slot, pl.at[u] / 8) + pl.at[u] % 8,
+        store_unit<kStream<D>>(cache + paged_k_offset<D>(blk, t.h0 + c.h, p.Hkv, slot, pl.at[u] / 8) + pl.at[u] % 8,
                    x + u * kUnit<T>);
     });
   }
@@ -570,15 +586,14 @@ constexpr int64_t kMaxGrid = 1 << 20;  // workgroups of a launch: the rest by st
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Tiles of n rows of H heads (of H_all that the launch turns): as many turns a
-// group (up to kMaxTurns) as leave the chip about kItems workgroups, so that a
+// group (up to max_turns) as leave the chip about kItems workgroups, so that a
 // short call is spread over the chip.
 constexpr int64_t kItems = 1024;
-constexpr int kMaxTurns = 8;
-TileGrid tile_grid(int64_t n, int H, int H_all, int D) {
+TileGrid tile_grid(int64_t n, int H, int H_all, int D, int max_turns) {
   TileGrid g{};
   if (n == 0 || H == 0) return g;
   const int64_t groups = kThreads / (D / 16);
-  const int64_t turns = std::min<int64_t>(kMaxTurns, ceil_div(n * H_all, groups * kItems));
+  const int64_t turns = std::min<int64_t>(max_turns, ceil_div(n * H_all, groups * kItems));
   g.heads = (int32_t)std::min<int64_t>(H, groups * turns);
   g.head_runs = (int32_t)ceil_div(H, g.heads);
   g.rows = (int32_t)std::max<int64_t>(1, std::min<int64_t>({groups * turns / g.heads, 4096 / D, n}));
@@ -628,32 +643,26 @@ dim3 grid_of(int64_t items) { return dim3((unsigned)std::min(items, kMaxGrid)); 
 
 // The backward's items: some tiles each, so that about kItems of them leave
 // their D sums.
-void bwd_grids(int64_t n, int Hq, int Hkv, int D, TileGrid& q, TileGrid& k, int32_t (&tile_rows)[2]) {
-  q = tile_grid(n, Hq, Hq + Hkv, D);
-  k = tile_grid(n, Hkv, Hq + Hkv, D);
-  tile_rows[0] = q.rows;
-  tile_rows[1] = k.rows;
-  const int64_t passes = std::max<int64_t>(1, ceil_div(q.items + k.items, kItems));
-  for (TileGrid* g : {&q, &k}) {
-    if (g->items == 0) continue;
-    g->rows = (int32_t)std::min<int64_t>(g->rows * passes, n);
-    g->items = ceil_div(n, g->rows) * g->head_runs;
-  }
+void bwd_grids(int64_t n, int Hq, int Hkv, int D, TileGrid& q, TileGrid& k) {
+  q = tile_grid(n, Hq, Hq + Hkv, D, 8);
+  k = tile_grid(n, Hkv, Hq + Hkv, D, 8);
+  const int64_t passes = ceil_div(q.items + k.items, kItems);
+  for (TileGrid* g : {&q, &k})
+    if (g->items > 0) g->items = ceil_div(g->items / g->head_runs, passes) * g->head_runs;
 }
 
 }  // namespace
 
 size_t rotary_bwd_parts(int64_t n, int Hq, int Hkv, int D) {
   TileGrid q, k;
-  int32_t tile_rows[2];
-  bwd_grids(n, Hq, Hkv, D, q, k, tile_rows);
+  bwd_grids(n, Hq, Hkv, D, q, k);
   return (size_t)(q.items + k.items);
 }
 
 hipError_t launch_rotary_fwd(RotaryParams p, int D, bool bf16, bool pairs, hipStream_t s) {
   p.n_q = p.n;
-  p.tiles_q = tile_grid(p.n, p.Hq, p.Hq + p.Hkv, D);
-  p.tiles_k = tile_grid(p.n, p.Hkv, p.Hq + p.Hkv, D);
+  p.tiles_q = tile_grid(p.n, p.Hq, p.Hq + p.Hkv, D, 4);
+  p.tiles_k = tile_grid(p.n, p.Hkv, p.Hq + p.Hkv, D, 4);
   p.items = p.tiles_q.items + p.tiles_k.items;
   if (p.items == 0) return hipSuccess;
   return dispatch<Fwd>(p, D, bf16, pairs, grid_of(p.items), s);
@@ -661,7 +670,7 @@ hipError_t launch_rotary_fwd(RotaryParams p, int D, bool bf16, bool pairs, hipSt
 
 hipError_t launch_rotary_bwd(RotaryParams p, int D, bool bf16, bool pairs, float* dwq, float* dwk, hipStream_t s) {
   p.n_q = p.n;
-  bwd_grids(p.n, p.Hq, p.Hkv, D, p.tiles_q, p.tiles_k, p.tile_rows);
+  bwd_grids(p.n, p.Hq, p.Hkv, D, p.tiles_q, p.tiles_k);
   p.items = p.tiles_q.items + p.tiles_k.items;
   if (p.items > 0) {
     const hipError_t e = dispatch<Bwd>(p, D, bf16, pairs, grid_of(p.items), s);
@@ -674,8 +683,8 @@ hipError_t launch_rotary_bwd(RotaryParams p, int D, bool bf16, bool pairs, float
 }
 
 hipError_t launch_rotary_append(RotaryParams p, int D, bool bf16, bool pairs, hipStream_t s) {
-  p.tiles_q = tile_grid(p.n_q, p.Hq, p.Hq + p.Hkv, D);
-  p.tiles_k = tile_grid(p.n, p.Hkv, p.Hq + p.Hkv, D);
+  p.tiles_q = tile_grid(p.n_q, p.Hq, p.Hq + p.Hkv, D, 4);
+  p.tiles_k = tile_grid(p.n, p.Hkv, p.Hq + p.Hkv, D, 4);
   const bool tall = (int64_t)p.n * p.Hkv >= 16384;  // 64 rows a workgroup where that leaves every compute unit one
   p.items_v = ceil_div(p.n, tall ? 64 : 8) * p.Hkv;
   p.items = p.items_v + p.tiles_q.items + p.tiles_k.items + ceil_div(p.n_patch, kThreads);

@@ -25,7 +25,7 @@ struct TileGrid {
   int32_t rows;       // rows of a tile
   int32_t heads;      // heads of a tile
   int32_t head_runs;  // tiles side by side over the heads
-  int64_t items;
+  int64_t items;      // workgroups (backward: each takes every (items / head_runs)-th tile)
 };
 
 struct RotaryParams {
@@ -38,7 +38,6 @@ struct RotaryParams {
   int32_t n, n_q;   // rows of k (and v), of q
   int32_t Hq, Hkv;
   TileGrid tiles_q, tiles_k;
-  int32_t tile_rows[2];  // backward: rows of a tile of q, of k (the grids' rows: of an item)
   int64_t items;       // workgroup items of all kinds
   padoc_heads q, k;    // in: rows, or (inverse, backward) gradients of the outputs
   padoc_heads qo, ko;  // out
