@@ -459,6 +459,7 @@ class Rotary:
         _lib.check(_lib.lib().padoc_rotary_create(C.byref(desc), C.byref(h)))
         self._h = h
         self.torch_dtype = _torch_dtype(self)
+        self._rows = _lib.rows(h, self.head_dim, self.n_axes, _DTYPES[dtype] == _lib.BF16)
 
     @property
     def handle(self):
@@ -468,6 +469,7 @@ class Rotary:
 
     def close(self):
         if getattr(self, "_h", None) is not None:
+            self._rows = None
             _lib.lib().padoc_rotary_destroy(self._h)
             self._h = None
 
@@ -568,6 +570,10 @@ def rotary_fwd(q, k, positions, rotary: Rotary, q_weight=None, k_weight=None, q_
     n]``; ``padoc_rotary_fwd``).  Rows and heads may be strided, as in slices
     of a fused projection; q or k may be None, and q_out / k_out may be q / k.
     Returns ``(q_out, k_out)``."""
+    if stream is None and rotary._rows is not None:
+        done = rotary._rows.fwd(q, k, positions, q_weight, k_weight, q_out, k_out)
+        if done is not None:
+            return done if type(done) is tuple else _lib.check(done)
     like = k if q is None else q
     device, dt = _rows_of(rotary, like)
     n, d = like.shape[0], rotary.head_dim
@@ -608,6 +614,10 @@ def rotary_bwd(dq_out, dk_out, positions, rotary: Rotary, q=None, k=None, q_weig
     weight).  Returns ``(dq, dk, dq_weight, dk_weight)``; the weights'
     gradients are float32 ``[d]``, None without a weight or with
     ``weight_grads=False``."""
+    if stream is None and rotary._rows is not None:
+        done = rotary._rows.bwd(dq_out, dk_out, positions, q, k, q_weight, k_weight, dq, dk, weight_grads)
+        if done is not None:
+            return done if type(done) is tuple else _lib.check(done)
     import torch
     like = dk_out if dq_out is None else dq_out
     device, dt = _rows_of(rotary, like)
@@ -701,6 +711,10 @@ def rotary_append(q, k, v, positions, slots, k_cache, v_cache, rotary: Rotary, q
     caches (k normed and rotated) at ``slots`` (int32 ``[n_new, 2]``: block id
     and slot; a block id of -1 leaves the row out).  ``q_positions`` may be
     left out when query row i is new row i; q may be None.  Returns q_out."""
+    if stream is None and rotary._rows is not None:
+        done = rotary._rows.append(q, k, v, positions, slots, k_cache, v_cache, q_weight, k_weight, q_positions, q_out)
+        if done is not None:
+            return done[0] if type(done) is tuple else _lib.check(done)
     import torch
     if k is None or v is None:
         raise ValueError("rotary_append needs k and v (rotary_fwd rotates q alone)")
@@ -718,11 +732,24 @@ def rotary_append(q, k, v, positions, slots, k_cache, v_cache, rotary: Rotary, q
     return q_out
 
 
+def _copy_blocks(k_cache, v_cache, pairs):
+    """The native call; its first use finds it."""
+    global _copy_blocks
+    _copy_blocks = _lib.native_copy_blocks()
+    return _copy_blocks(k_cache, v_cache, pairs)
+
+
 def cache_copy_blocks(k_cache, v_cache, pairs, k_dst=None, v_dst=None, pairs_host=None, stream=None):
     """Copy blocks ``pairs[i, 0]`` of the paged caches to blocks ``pairs[i,
     1]`` of the same caches, or of ``k_dst`` / ``v_dst``
     (``padoc_cache_copy_blocks``; int32 ``[n, 2]`` on the device, with an
     optional host copy that is only checked).  Returns the caches written."""
+    if stream is None and k_dst is None and v_dst is None and pairs_host is None:
+        done = _copy_blocks(k_cache, v_cache, pairs)
+        if done is not None:
+            if done:
+                _lib.check(done)
+            return k_cache, v_cache
     import torch
     if (k_dst is None) != (v_dst is None):
         raise ValueError("pass k_dst and v_dst together (or neither)")

@@ -225,6 +225,38 @@ def streams(handle):
                   C.cast(L.padoc_session_close, C.c_void_p).value)
 
 
+def native_rows():
+    """The module ``_rows``, or None where it is not built for this interpreter
+    and this PyTorch."""
+    try:
+        import torch  # noqa: F401  (whose libraries the module needs)
+        from . import _rows
+    except ImportError:
+        return None
+    return _rows
+
+
+def rows(handle, head_dim: int, n_axes: int, bf16: bool):
+    """The native calls of rotary ``handle``, or None."""
+    m = native_rows()
+    if m is None:
+        return None
+    L = lib()
+    at = [C.cast(getattr(L, f), C.c_void_p).value
+          for f in ("padoc_rotary_fwd", "padoc_rotary_bwd", "padoc_rotary_bwd_workspace_bytes", "padoc_rotary_append")]
+    return m.Rows(handle.value, *at, head_dim, n_axes, bf16)
+
+
+def native_copy_blocks():
+    """``copy_blocks(k_cache, v_cache, pairs)`` of the native module, or a
+    function that leaves every call to the caller."""
+    m = native_rows()
+    if m is None:
+        return lambda k_cache, v_cache, pairs: None
+    f, address = m.copy_blocks, C.cast(lib().padoc_cache_copy_blocks, C.c_void_p).value
+    return lambda k_cache, v_cache, pairs: f(address, k_cache, v_cache, pairs)
+
+
 def check(status: int) -> None:
     if status != OK:
         raise PadocError(status, lib().padoc_last_error().decode(errors="replace"))

@@ -1,6 +1,7 @@
-"""Build ``libpadoc_attn.so`` in-tree with hipcc for gfx950, and the small
-CPython module ``_streams`` beside it (where Python's headers are; the package
-calls the library through ctypes without it).
+"""Build ``libpadoc_attn.so`` in-tree with hipcc for gfx950, and beside it the
+small CPython modules ``_streams`` (where Python's headers are) and ``_rows``
+(where PyTorch's are too); without them the package calls the library through
+ctypes.
 
     python -m paper_2608_06146_amd.build            # incremental
     python -m paper_2608_06146_amd.build --force    # rebuild everything
@@ -13,6 +14,7 @@ from __future__ import annotations
 import argparse
 import concurrent.futures as cf
 import hashlib
+import importlib.util
 import os
 import shutil
 import subprocess
@@ -27,6 +29,7 @@ STREAMS = os.path.join(PKG, "_streams" + (sysconfig.get_config_var("EXT_SUFFIX")
 ARCH = os.environ.get("PADOC_OFFLOAD_ARCH", "gfx950")
 
 STREAMS_SOURCE = "csrc/python/streams.cpp"
+ROWS_SOURCE = "csrc/python/rows.cpp"
 SOURCES = [
     "csrc/host/plan.cpp",
     "csrc/host/session.cpp",
@@ -100,13 +103,45 @@ def _compile_streams(cc: str, out: str) -> bool:
     return True
 
 
+def _compile_rows(cc: str, out: str, force: bool) -> bool:
+    """``_rows`` into file `out`; False where there are no Python or PyTorch
+    headers."""
+    inc = sysconfig.get_paths()["include"]
+    spec = importlib.util.find_spec("torch")
+    torch_dir = spec.submodule_search_locations[0] if spec and spec.submodule_search_locations else ""
+    if not os.path.exists(os.path.join(inc, "Python.h")) or \
+            not os.path.exists(os.path.join(torch_dir, "include", "torch", "csrc", "autograd", "python_variable.h")):
+        return False
+    src = os.path.join(PKG, ROWS_SOURCE)
+    paths = [inc, os.path.join(ROOT, "include"), os.path.join(torch_dir, "include"),
+             os.path.join(torch_dir, "include", "torch", "csrc", "api", "include")]
+    cmd = [cc, "-O2", "-std=c++17", "-fPIC", "-Wall", "-shared", "-no-hip-rt", "-DUSE_ROCM", "-D__HIP_PLATFORM_AMD__"]
+    cmd += [x for i in paths for x in ("-isystem", i)]
+    libs = ["-L", os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"]
+    with open(os.path.join(torch_dir, "version.py"), "rb") as f:
+        version = f.read()
+    tag = hashlib.sha256(version + " ".join(cmd + libs).encode() +
+                         _digest([src, os.path.join(ROOT, "include", "padoc_attn.h")]).encode()).hexdigest()[:16]
+    kept = os.path.join(BUILD, f"rows.{tag}.so")
+    if force or not os.path.exists(kept):
+        r = subprocess.run(cmd + ["-o", kept + ".tmp", src] + libs, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+        os.replace(kept + ".tmp", kept)
+    shutil.copyfile(kept, out)
+    return True
+
+
 def build(force: bool = True, verbose: bool = False) -> str:
     """Compile every source and link the shared library; returns its path.
     What was built before is replaced only once everything has compiled."""
     cc = hipcc()
     os.makedirs(BUILD, exist_ok=True)
-    with cf.ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
+    rows = os.path.join(os.path.dirname(STREAMS), "_rows" + STREAMS[STREAMS.index("_streams") + len("_streams"):])
+    with cf.ThreadPoolExecutor(max_workers=min(8, len(SOURCES) + 1)) as ex:
+        rows_built = ex.submit(_compile_rows, cc, rows + ".tmp", force)
         objs = list(ex.map(lambda s: _compile(cc, s, force), SOURCES))
+        have_rows = rows_built.result()
     tmp = LIB + ".tmp"
     cmd = [cc, "-shared", "-fPIC", f"--offload-arch={ARCH}", "-o", tmp] + objs
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -114,10 +149,11 @@ def build(force: bool = True, verbose: bool = False) -> str:
         raise RuntimeError(f"link failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
     have_streams = _compile_streams(cc, STREAMS + ".tmp")
     os.replace(tmp, LIB)
-    if have_streams:
-        os.replace(STREAMS + ".tmp", STREAMS)
-    elif os.path.exists(STREAMS):
-        os.remove(STREAMS)  # of other sources
+    for have, path in ((have_streams, STREAMS), (have_rows, rows)):
+        if have:
+            os.replace(path + ".tmp", path)
+        elif os.path.exists(path):
+            os.remove(path)  # of other sources
     if verbose:
         print(f"built {LIB}")
     return LIB

@@ -10,6 +10,12 @@ from _rotary import normal
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True, params=["native", "python"])
+def binding(request, monkeypatch):
+    if request.param == "python":
+        monkeypatch.setattr(pa, "_copy_blocks", lambda *a: None)
+
+
 def _caches(nb, hkv, d, dtype, seed):
     return normal((nb, hkv, d // 8, 16, 8), seed, dtype), normal((nb, hkv, d, 16), seed + 1, dtype)
 
@@ -29,6 +35,25 @@ def test_within_a_cache(dtype, d, hkv, n):
     out = pa.cache_copy_blocks(kc, vc, torch.from_numpy(ids).cuda(), pairs_host=ids)
     assert out[0] is kc and out[1] is vc
     assert torch.equal(kc, want[0]) and torch.equal(vc, want[1])
+    back = torch.from_numpy(ids[n // 2:, ::-1].copy()[:1]).cuda()  # one back, without the host's copy
+    pa.cache_copy_blocks(kc, vc, back)
+    assert torch.equal(kc, want[0]) and torch.equal(vc, want[1])
+
+
+def test_refusals():
+    kc, vc = _caches(4, 2, 64, "bf16", 1)
+    pairs = torch.tensor([[0, 1]], dtype=torch.int32, device="cuda")
+    for k, v, p in ((kc.float(), vc, pairs), (kc, vc[:3], pairs), (kc, vc, pairs.long()), (kc, vc, pairs[0]), (kc, vc, pairs.cpu()),
+                    (kc.transpose(2, 3), vc, pairs), (kc.half(), vc.half(), pairs), (kc, vc.transpose(2, 3).contiguous(), pairs),
+                    (vc, kc, pairs), (kc.cpu(), vc, pairs)):
+        with pytest.raises((ValueError, TypeError)):
+            pa.cache_copy_blocks(k, v, p)
+    with pytest.raises(ValueError):
+        pa.cache_copy_blocks(kc, vc, pairs, k_dst=kc)
+    with pytest.raises(ValueError):
+        pa.cache_copy_blocks(kc, vc, pairs, *_caches(4, 1, 64, "bf16", 1))
+    with pytest.raises(ValueError):
+        pa.cache_copy_blocks(kc, vc, pairs, pairs_host=np.zeros((2, 2), np.int32))
 
 
 def test_to_another_cache_with_ids_outside():

@@ -5,9 +5,21 @@ import pytest
 import torch
 
 import paper_2608_06146_amd as pa
+from paper_2608_06146_amd import _lib
 from _rotary import Setup, check, f64, k_block_view, normal, positions, torch_dtype, v_block_view
 
 pytestmark = pytest.mark.gpu
+
+@pytest.fixture(autouse=True, params=["native", "python"])
+def binding(request, monkeypatch):
+    """Every test through the native module and without it."""
+    if request.param == "python":
+        monkeypatch.setattr(_lib, "native_rows", lambda: None)
+        monkeypatch.setattr(pa, "_copy_blocks", lambda *a: None)
+    else:
+        assert _lib.native_rows() is not None, "the native module is not built"
+    return request.param
+
 
 HEADS = {"gqa": (16, 2), "seven": (28, 4), "odd": (5, 3)}
 
@@ -380,3 +392,76 @@ def test_a_stream_of_the_callers():
         junk = [torch.full((256, 1024), 3.0, device="cuda") for _ in range(4)]  # memory the calls let go of is not theirs yet
         torch.cuda.current_stream().wait_stream(side)
         assert all(a is None and b is None or torch.equal(a, b) for a, b in zip(got, want)) and len(junk) == 4
+
+
+# ---------------------------------------------------------------- refusals
+
+def _call(what="fwd", **kw):
+    st, n, d = kw.pop("st", None) or Setup(64, "bf16"), 6, 64
+    a = {"q": normal((n, 4, d), 1, "bf16"), "k": normal((n, 2, d), 2, "bf16"), "v": normal((n, 2, d), 3, "bf16"),
+         "positions": positions(3, n, 4), "q_weight": normal((d,), 5, "bf16"), "k_weight": normal((d,), 6, "bf16"),
+         "gq": normal((n, 4, d), 7, "bf16"), "gk": normal((n, 2, d), 8, "bf16"), "q_out": None,
+         "slots": torch.from_numpy(_slots(n, 3, 1)).cuda(), "q_positions": None,
+         "kc": torch.zeros((3, 2, 8, 16, 8), dtype=torch.bfloat16, device="cuda"),
+         "vc": torch.zeros((3, 2, d, 16), dtype=torch.bfloat16, device="cuda")}
+    a.update(kw)
+    if what == "fwd":
+        return pa.rotary_fwd(a["q"], a["k"], a["positions"], st.handle, a["q_weight"], a["k_weight"], a["q_out"])
+    if what == "bwd":
+        return pa.rotary_bwd(a["gq"], a["gk"], a["positions"], st.handle, a["q"], a["k"], a["q_weight"], a["k_weight"], dq=a["q_out"])
+    return pa.rotary_append(a["q"], a["k"], a["v"], a["positions"], a["slots"], a["kc"], a["vc"], st.handle, a["q_weight"],
+                            a["k_weight"], a["q_positions"], a["q_out"])
+
+
+BAD = {  # argument: values that no call takes
+    "q": [lambda t: t.float(), lambda t: t.cpu(), lambda t: t[:, :, :32], lambda t: t[:5], lambda t: t[0],
+          lambda t: torch.empty((64, 4, 6), dtype=t.dtype, device="cuda").permute(2, 1, 0)],
+    "k": [lambda t: t.float(), lambda t: t.cpu(), lambda t: t[:5]],
+    "positions": [lambda t: t.long(), lambda t: t.cpu(), lambda t: t[:2], lambda t: t[:, :5], lambda t: t[0],
+                  lambda t: torch.stack([t, t], -1)[..., 0]],
+    "q_weight": [lambda t: t.float(), lambda t: t.cpu(), lambda t: t[:32], lambda t: torch.stack([t, t], -1)[:, 0]],
+    "q_out": [lambda t: torch.empty((6, 4, 64), device="cuda"), lambda t: torch.empty((6, 3, 64), dtype=torch.bfloat16, device="cuda"),
+              lambda t: torch.empty((6, 1, 64), dtype=torch.bfloat16, device="cuda").expand(6, 4, 64)],
+    "gq": [lambda t: t.float(), lambda t: t[:5]],
+    "v": [lambda t: t.float(), lambda t: t[:5], lambda t: t[:, :1]],
+    "slots": [lambda t: t.long(), lambda t: t[:5], lambda t: t.t().contiguous(), lambda t: t.cpu()],
+    "kc": [lambda t: t.float(), lambda t: t[:2], lambda t: t.transpose(2, 3)],
+    "vc": [lambda t: t.float(), lambda t: t[:, :1], lambda t: t.transpose(2, 3).contiguous()],
+    "q_positions": [lambda t: positions(3, 5, 1)],
+}
+USED = {"fwd": ("q", "k", "positions", "q_weight", "q_out"), "bwd": ("q", "k", "positions", "q_weight", "q_out", "gq"),
+        "append": ("q", "k", "positions", "q_weight", "q_out", "v", "slots", "kc", "vc", "q_positions")}
+
+
+@pytest.mark.parametrize("what", USED)
+def test_refusals(what):
+    st = Setup(64, "bf16")
+    _call(what, st=st)
+    for name in USED[what]:
+        for i, spoil in enumerate(BAD[name]):
+            if what == "append" and name == "q" and i == 3:
+                continue  # fewer queries than new rows: refused for its positions below
+            base = {"q": normal((6, 4, 64), 1, "bf16"), "k": normal((6, 2, 64), 2, "bf16"), "v": normal((6, 2, 64), 2, "bf16"),
+                    "positions": positions(3, 6, 4), "q_weight": normal((64,), 5, "bf16"), "gq": normal((6, 4, 64), 7, "bf16"),
+                    "slots": torch.from_numpy(_slots(6, 3, 1)).cuda(), "kc": torch.zeros((3, 2, 8, 16, 8), dtype=torch.bfloat16, device="cuda"),
+                    "vc": torch.zeros((3, 2, 64, 16), dtype=torch.bfloat16, device="cuda")}.get(name)
+            with pytest.raises((ValueError, TypeError, pa.PadocError)):
+                _call(what, st=st, **{name: spoil(base)})
+                print("taken:", what, name, i, flush=True)
+    if what == "append":
+        with pytest.raises(pa.PadocError, match="q_pos"):
+            _call(what, st=st, q=normal((5, 4, 64), 1, "bf16"))
+        with pytest.raises((ValueError, AttributeError)):
+            _call(what, st=st, v=None)
+    with pytest.raises(ValueError, match="stream"):
+        class Elsewhere:
+            device, cuda_stream = torch.device("cuda", 7), 0
+        pa.rotary_fwd(normal((6, 4, 64), 1, "bf16"), None, positions(3, 6, 4), st.handle, stream=Elsewhere)
+
+
+def test_a_closed_handle_is_refused():
+    st = Setup(64, "bf16")
+    st.handle.close()
+    for what in USED:
+        with pytest.raises(ValueError, match="closed"):
+            _call(what, st=st)
