@@ -71,6 +71,6 @@ struct CopyParams {
 };
 
 // Items of a backward: each leaves D sums in the workspace.
-size_t rotary_bwd_parts(int64_t n, int Hq, int Hkv, int D);
+size_t rotary_bwd_parts(int64_t n, int Hq, int Hkv, int D, bool bf16);
 
 }  // namespace padoc
