@@ -7,9 +7,11 @@
 //   dx = rho (g - x rho^2 mean(g x)),  rho = 1 / sqrt(mean x^2 + eps)
 //
 // All of it is bound by memory: every element is read once and written once.
-// A row of one head is shared by D / 16 lanes (a group).  Lane l of a group
-// holds 16 dimensions in units of 16 bytes, chosen so that both members of a
-// pair are in one lane and the lanes of a group access neighbouring units.
+// A row of one head is shared by eight lanes (a group).  A lane holds D / 8
+// dimensions in units of 16 bytes, chosen so that the lanes of a group access
+// neighbouring units (whole 128-byte lines) and both members of a pair are in
+// one lane; only where a lane has a single unit (bf16, D = 64, halves) the
+// members are in lanes four apart, which exchange their values.
 //
 // A workgroup takes a tile of rows of one tensor (q or k).  Its lanes compute
 // the cosines and sines of the tile's rows once, a pair each, into LDS; its
@@ -37,20 +39,16 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 
+constexpr int kLanes = 8;                    // of a group
+constexpr int kGroups = kThreads / kLanes;   // of a workgroup, and rows of a tile at most
+template <int D>
+constexpr int kElems = D / kLanes;           // elements of a lane
 // Elements of a 16-byte unit, the size of a lane's memory accesses, and units
 // of a lane.
 template <typename T>
 constexpr int kUnit = 16 / (int)sizeof(T);
-template <typename T>
-constexpr int kUnits = 16 / kUnit<T>;
-
-// Whether rows are loaded and stored past the caches (non-temporal): where an
-// access of a group covers whole 128-byte lines.  Measured, in turn over more
-// data than the caches hold (bf16): 43,067 rows of 18 heads of 128 70.1 us (5.7
-// TB/s) with, 78.8 without; 20,000 rows of 32 heads of 64, whose lines two
-// accesses share, 39.5 either way forward, 71.7 with and 69.4 without backward.
-template <int D>
-constexpr bool kStream = D == 128;
+template <typename T, int D>
+constexpr int kUnits = kElems<D> / kUnit<T>;
 
 // A 16-byte unit at an address aligned to one element.
 template <typename T>
@@ -64,61 +62,69 @@ struct Unit<float> {
   typedef u32x4 type __attribute__((aligned(4)));
 };
 
-// A lane's 16 elements of a head as they were loaded: its units in turn.
+// Rows are loaded and stored past the caches (non-temporal).  Measured, in turn
+// over more data than the caches hold: 43,067 rows of 18 heads of 128 (bf16) 70.1
+// us (5.7 TB/s) with, 78.8 without.
 template <typename T>
+__device__ __forceinline__ u32x4 load_unit(const T* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const typename Unit<T>::type*>(p));
+}
+
+// A lane's elements of a head as they were loaded: its units in turn.
+template <typename T, int D>
 struct Raw {
-  u32x4 u[kUnits<T>];
-  template <bool STREAM>
-  __device__ __forceinline__ void load_row(const T* p, const int (&at)[kUnits<T>]) {
+  u32x4 u[kUnits<T, D>];
+  __device__ __forceinline__ void load_row(const T* p, const int (&at)[kUnits<T, D>]) {
 #pragma unroll
-    for (int i = 0; i < kUnits<T>; ++i) {
-      const auto q = reinterpret_cast<const typename Unit<T>::type*>(p + at[i]);
-      u[i] = STREAM ? __builtin_nontemporal_load(q) : *q;
-    }
+    for (int i = 0; i < kUnits<T, D>; ++i) u[i] = load_unit(p + at[i]);
   }
-  __device__ __forceinline__ void get(float (&x)[16]) const {
+  __device__ __forceinline__ void load_weight(const T* p, const int (&at)[kUnits<T, D>]) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      x[i] = sizeof(T) == 4 ? __uint_as_float(u[i / 4 % kUnits<T>][i % 4])
-                            : __uint_as_float(i % 2 ? u[i / 8][i % 8 / 2] & 0xffff0000u : u[i / 8][i % 8 / 2] << 16);
+    for (int i = 0; i < kUnits<T, D>; ++i) u[i] = *reinterpret_cast<const typename Unit<T>::type*>(p + at[i]);
+  }
+  __device__ __forceinline__ void get(float (&x)[kElems<D>]) const {
+#pragma unroll
+    for (int i = 0; i < kElems<D>; ++i) {
+      const uint32_t w = u[i / kUnit<T>][i % kUnit<T> * (int)sizeof(T) / 4];
+      x[i] = __uint_as_float(sizeof(T) == 4 ? w : i % 2 ? w & 0xffff0000u : w << 16);
+    }
   }
 };
 
 // One unit's elements, rounded to nearest-even once, here (NaN stays NaN).
-template <bool STREAM>
-__device__ __forceinline__ void store_unit(__bf16* p, const float* x) {
+__device__ __forceinline__ u32x4 pack_unit(const __bf16*, const float* x) {
   const bf16x8 b = __builtin_convertvector((f32x8{x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]}), bf16x8);
   u32x4 u;
   __builtin_memcpy(&u, &b, 16);
-  const auto q = reinterpret_cast<Unit<__bf16>::type*>(p);
-  if (STREAM)
-    __builtin_nontemporal_store(u, q);
-  else
-    *q = u;
+  return u;
 }
-template <bool STREAM>
-__device__ __forceinline__ void store_unit(float* p, const float* x) {
+__device__ __forceinline__ u32x4 pack_unit(const float*, const float* x) {
   u32x4 u;
   __builtin_memcpy(&u, x, 16);
-  const auto q = reinterpret_cast<Unit<float>::type*>(p);
-  if (STREAM)
-    __builtin_nontemporal_store(u, q);
-  else
-    *q = u;
+  return u;
 }
-template <bool STREAM, typename T>
-__device__ __forceinline__ void store_row(T* p, const int (&at)[kUnits<T>], const float (&x)[16]) {
+template <typename T, int N, int E>
+__device__ __forceinline__ void store_row(T* p, const int (&at)[N], const float (&x)[E]) {
 #pragma unroll
-  for (int i = 0; i < kUnits<T>; ++i) store_unit<STREAM>(p + at[i], x + i * kUnit<T>);
+  for (int i = 0; i < N; ++i)
+    __builtin_nontemporal_store(pack_unit(p, x + i * kUnit<T>), reinterpret_cast<typename Unit<T>::type*>(p + at[i]));
 }
 
-// Sum over the L (4 or 8) lanes of a group, in every one of them.
-template <int L>
+// Sum over the eight lanes of a group, in every one of them.
 __device__ __forceinline__ float group_sum(float v) {
-  v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0xB1, 0xf, 0xf, true));  // lane ^ 1
-  v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4E, 0xf, 0xf, true));  // lane ^ 2
-  if (L == 8) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x141, 0xf, 0xf, true));  // 7 - lane
+  v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0xB1, 0xf, 0xf, true));   // lane ^ 1
+  v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4E, 0xf, 0xf, true));   // lane ^ 2
+  v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x141, 0xf, 0xf, true));  // 7 - lane
   return v;
+}
+
+// The value of lane ^ 4: from four lanes on for the lower half of a group (banks
+// 0 and 2 of a row of 16 lanes), from four lanes back for the upper.
+__device__ __forceinline__ float other_half(float v) {
+  const int x = __float_as_int(v);
+  int r = __builtin_amdgcn_update_dpp(0, x, 0x104, 0xf, 0x5, false);
+  r = __builtin_amdgcn_update_dpp(r, x, 0x114, 0xf, 0xa, false);
+  return __int_as_float(r);
 }
 
 // Sine and cosine of `phase` turns / 2^32.
@@ -134,51 +140,58 @@ __device__ __forceinline__ void sincos_turns(uint32_t phase, float& s, float& c)
   if ((quadrant + 1) & 2) c = -c;
 }
 
-// A lane's place in its group: which units it holds, in an order that keeps a
-// group's accesses side by side and both members of a pair in one lane.
-//   pairs of neighbours: units l, l + L, ... in turn
-//   halves: units k and k + n (n = units of half the rotated dimensions) for k =
-//   l, l + L, ...; behind the n rotated ones, k stands for two of the others
-// Pair m of a lane (0 .. 7) has elements first(m) and second(m).
+// A lane's place in its group: which units it holds.  A slot is what holds whole
+// pairs: a unit (pairs of neighbours), or units k and k + n (halves; n = units
+// of half the rotated dimensions), where behind the n rotated slots k stands for
+// two of the other units.  Lane l has slots l, l + 8, ... (split: lanes l and l + 4
+// share slot l, a unit each).  Pair m of a lane has elements first(m) and
+// second(m).
 template <typename T, int D, bool PAIRS>
 struct Place {
-  static constexpr int L = D / 16, E = kUnit<T>, N = kUnits<T>;
+  static constexpr int E = kUnit<T>, N = kUnits<T, D>;
+  static constexpr bool kSplit = !PAIRS && N == 1;
+  static constexpr int kSlotLanes = kSplit ? kLanes / 2 : kLanes;
   static constexpr int kPairsPerSlot = PAIRS ? E / 2 : E;
-  static constexpr int kSlots = 8 / kPairsPerSlot;  // a lane's units (PAIRS) or pairs of units
+  static constexpr int kSlots = PAIRS ? N : kSplit ? 1 : N / 2;
   int at[N];
   int turned;  // slots 0 .. turned-1 are rotated
-  __device__ __forceinline__ Place(int lane, int pairs) {
+  __device__ __forceinline__ Place(int pairs) {
+    const int lane = threadIdx.x % kLanes;
     const int n = pairs / kPairsPerSlot;  // rotated slots of the group
     turned = 0;
 #pragma unroll
     for (int i = 0; i < kSlots; ++i) {
-      const int k = i * L + lane;
+      const int k = i * kSlotLanes + lane % kSlotLanes;
       turned += k < n;
       if (PAIRS) {
         at[i] = k * E;
       } else {
-        at[2 * i] = (k < n ? k : n + k) * E;
-        at[2 * i + 1] = (k < n ? k + n : D / 2 / E + k) * E;
+        const int a = (k < n ? k : n + k) * E, b = (k < n ? k + n : D / 2 / E + k) * E;
+        if (kSplit) {
+          at[0] = lane < kSlotLanes ? a : b;
+        } else {
+          at[2 * i % N] = a;
+          at[(2 * i + 1) % N] = b;
+        }
       }
     }
   }
-  static constexpr int first(int m) { return PAIRS ? 2 * m : m / E * (2 * E) + m % E; }
+  static constexpr int first(int m) { return PAIRS ? 2 * m : kSplit ? m : m / E * (2 * E) + m % E; }
   static constexpr int second(int m) { return PAIRS ? 2 * m + 1 : m / E * (2 * E) + E + m % E; }
-  // Lane and place in the lane of a pair.
-  static __device__ __forceinline__ int lane_of(int pair) { return pair / kPairsPerSlot % L; }
+  // (Slot) lane and place in the lane of a pair.
+  static __device__ __forceinline__ int lane_of(int pair) { return pair / kPairsPerSlot % kSlotLanes; }
   static __device__ __forceinline__ int index_of(int pair) {
-    return pair / kPairsPerSlot / L * kPairsPerSlot + pair % kPairsPerSlot;
+    return pair / kPairsPerSlot / kSlotLanes * kPairsPerSlot + pair % kPairsPerSlot;
   }
 };
 
-// Cosines and sines of a tile's rows: per row and quarter i of a lane's pairs
-// (two of them), the lanes' 16 bytes side by side.
+// Cosines and sines of a tile's rows: per row and two pairs of a lane, the lanes'
+// 16 bytes side by side.
 template <typename T, int D, bool PAIRS>
 struct AngleTable {
   typedef Place<T, D, PAIRS> P;
-  static constexpr int kLanes = D / 16;
-  static constexpr int kRows = 4096 / D;  // rows of a tile, at most
-  f32x4 at[kRows][4][kLanes];
+  f32x4 at[kGroups][P::kSlots * P::kPairsPerSlot / 2][P::kSlotLanes];
+  static_assert(sizeof(at) == kGroups * D * sizeof(float), "D / 2 pairs a row");
 
   // Fill rows [0, n): thread t takes pair t % (D / 2) of rows t / (D / 2), ...;
   // scaled, the sine negated for the inverse rotation.
@@ -199,35 +212,47 @@ struct AngleTable {
   }
 };
 
-// Rotate a lane's pairs by the angles of a row of the table.
+// Rotate a lane's pairs by the angles of a row of the table.  (Split: every lane
+// of the group calls it with its one unit.)
 template <typename T, int D, bool PAIRS>
-__device__ __forceinline__ void turn(float (&x)[16], const AngleTable<T, D, PAIRS>& table, int row,
+__device__ __forceinline__ void turn(float (&x)[kElems<D>], const AngleTable<T, D, PAIRS>& table, int row,
                                      const Place<T, D, PAIRS>& pl) {
   typedef Place<T, D, PAIRS> P;
+  float y[kElems<D>];
+  if (P::kSplit) {
+#pragma unroll
+    for (int i = 0; i < kElems<D>; ++i) y[i] = other_half(x[i]);
+  }
 #pragma unroll
   for (int slot = 0; slot < P::kSlots; ++slot) {
     if (slot >= pl.turned) break;
 #pragma unroll
     for (int i = 0; i < P::kPairsPerSlot / 2; ++i) {
       const int m0 = slot * P::kPairsPerSlot + 2 * i;
-      const f32x4 t = table.at[row][m0 / 2][threadIdx.x % P::L];
+      const f32x4 t = table.at[row][m0 / 2][threadIdx.x % P::kSlotLanes];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const int a = P::first(m0 + j), b = P::second(m0 + j);
-        const float c = t[2 * j], s = t[2 * j + 1], ya = x[a], yb = x[b];
-        x[a] = ya * c - yb * s;
-        x[b] = yb * c + ya * s;
+        const int a = P::first(m0 + j);
+        const float c = t[2 * j], s = t[2 * j + 1], ya = x[a];
+        if (P::kSplit) {
+          x[a] = ya * c + y[a] * (threadIdx.x % kLanes < P::kSlotLanes ? -s : s);
+        } else {
+          const int b = P::second(m0 + j) % kElems<D>;
+          const float yb = x[b];
+          x[a] = ya * c - yb * s;
+          x[b] = yb * c + ya * s;
+        }
       }
     }
   }
 }
 
 template <int D>
-__device__ __forceinline__ float rms_scale(const float (&x)[16], float eps) {
+__device__ __forceinline__ float rms_scale(const float (&x)[kElems<D>], float eps) {
   float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) s += x[i] * x[i];
-  return __builtin_amdgcn_rsqf(group_sum<D / 16>(s) * (1.f / D) + eps);
+  for (int i = 0; i < kElems<D>; ++i) s += x[i] * x[i];
+  return __builtin_amdgcn_rsqf(group_sum(s) * (1.f / D) + eps);
 }
 
 template <typename T>
@@ -292,32 +317,32 @@ struct Cursor {
 template <typename T, int D, bool PAIRS, class Put>
 __device__ __forceinline__ void turn_tile(const RotaryParams& p, const Tile& t, const int32_t* pos, int64_t pos_stride,
                                           AngleTable<T, D, PAIRS>& table, const Place<T, D, PAIRS>& pl, Put put) {
-  constexpr int L = D / 16, R = kThreads / L, U = kAhead;
-  const int dr = R / t.heads, dh = R - dr * t.heads;
-  Cursor ahead(t, threadIdx.x / L), at = ahead;
-  Raw<T> raw[U], rw;
+  constexpr int U = kAhead;
+  const int dr = kGroups / t.heads, dh = kGroups - dr * t.heads;
+  Cursor ahead(t, threadIdx.x / kLanes), at = ahead;
+  Raw<T, D> raw[U], rw;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    if (ahead.row < t.rows) raw[u].template load_row<kStream<D>>(ahead.at<const T>(t.in, t), pl.at);
+    if (ahead.row < t.rows) raw[u].load_row(ahead.at<const T>(t.in, t), pl.at);
     ahead.next(t, dr, dh);
   }
-  if (t.w) rw.template load_row<false>(static_cast<const T*>(t.w), pl.at);
+  if (t.w) rw.load_weight(static_cast<const T*>(t.w), pl.at);
   table.fill(p, pos, pos_stride, t.row0, t.rows);
   __syncthreads();
-  float wt[16];
+  float wt[kElems<D>];
   if (t.w) rw.get(wt);
   while (at.row < t.rows) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (at.row >= t.rows) break;
-      float x[16];
+      float x[kElems<D>];
       raw[u].get(x);
-      if (ahead.row < t.rows) raw[u].template load_row<kStream<D>>(ahead.at<const T>(t.in, t), pl.at);
+      if (ahead.row < t.rows) raw[u].load_row(ahead.at<const T>(t.in, t), pl.at);
       ahead.next(t, dr, dh);
       if (t.w) {
         const float rho = rms_scale<D>(x, p.eps);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] *= rho * wt[i];
+        for (int i = 0; i < kElems<D>; ++i) x[i] *= rho * wt[i];
       }
       turn(x, table, at.row, pl);
       put(at, x);
@@ -331,18 +356,17 @@ __device__ __forceinline__ void turn_tile(const RotaryParams& p, const Tile& t, 
 template <typename T, int D, bool PAIRS>
 __global__ __launch_bounds__(kThreads) void rotary_fwd_kernel(const RotaryParams p) {
   __shared__ AngleTable<T, D, PAIRS> table;
-  const Place<T, D, PAIRS> pl(threadIdx.x % (D / 16), p.pairs);
+  const Place<T, D, PAIRS> pl(p.pairs);
   for (int64_t b = blockIdx.x; b < p.items; b += gridDim.x) {
     const Tile t = tile_of(p, b);
-    turn_tile(p, t, p.pos, p.pos_stride, table, pl, [&](const Cursor& c, const float (&x)[16]) {
-      store_row<kStream<D>>(c.at<T>(t.out, t), pl.at, x);
+    turn_tile(p, t, p.pos, p.pos_stride, table, pl, [&](const Cursor& c, const float (&x)[kElems<D>]) {
+      store_row(c.at<T>(t.out, t), pl.at, x);
     });
   }
 }
 
 // Workgroups of the backward that a compute unit holds (by their registers).
-template <typename T>
-constexpr int kBwdPerUnit = sizeof(T) == 2 ? 3 : 2;
+constexpr int bwd_per_unit(int D, bool bf16) { return D == 64 ? 4 : bf16 ? 3 : 2; }
 
 // Backward: dx of an item's tiles, and the weight's gradient over them (fp32):
 // in acc, lane by lane, then over the lanes that hold the same dimensions of a
@@ -350,31 +374,31 @@ constexpr int kBwdPerUnit = sizeof(T) == 2 ? 3 : 2;
 // tiles of an item lie as many rows apart as all items take at once, so that
 // what the chip reads at a time is one stretch of memory.
 template <typename T, int D, bool PAIRS>
-__global__ __launch_bounds__(kThreads, kBwdPerUnit<T>) void rotary_bwd_kernel(const RotaryParams p) {
-  constexpr int L = D / 16, R = kThreads / L, U = sizeof(T) == 2 ? 2 : 1;  // of each tensor
+__global__ __launch_bounds__(kThreads, bwd_per_unit(D, sizeof(T) == 2)) void rotary_bwd_kernel(const RotaryParams p) {
+  constexpr int U = sizeof(T) == 2 ? 2 : 1;  // rows of each tensor in flight
   __shared__ AngleTable<T, D, PAIRS> table;
   __shared__ float sums[kThreads / 64][D];
-  const Place<T, D, PAIRS> pl(threadIdx.x % L, p.pairs);
+  const Place<T, D, PAIRS> pl(p.pairs);
   for (int64_t b = blockIdx.x; b < p.items; b += gridDim.x) {
     Tile t = tile_of(p, b);
-    const int dr = R / t.heads, dh = R - dr * t.heads;
-    float acc[16] = {}, wt[16];
+    const int dr = kGroups / t.heads, dh = kGroups - dr * t.heads;
+    float acc[kElems<D>] = {}, wt[kElems<D>];
     if (t.w) {
-      Raw<T> rw;
-      rw.template load_row<false>(static_cast<const T*>(t.w), pl.at);
+      Raw<T, D> rw;
+      rw.load_weight(static_cast<const T*>(t.w), pl.at);
       rw.get(wt);
     }
     const TileGrid& grid = b < p.tiles_q.items ? p.tiles_q : p.tiles_k;
     const int64_t apart = grid.items / grid.head_runs * grid.rows;
     for (; t.row0 < p.n; t.row0 += apart) {
       t.rows = (int)min((int64_t)grid.rows, p.n - t.row0);
-      Cursor ahead(t, threadIdx.x / L), at = ahead;
-      Raw<T> rg[U], rx[U];
+      Cursor ahead(t, threadIdx.x / kLanes), at = ahead;
+      Raw<T, D> rg[U], rx[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (ahead.row < t.rows) {
-          rg[u].template load_row<kStream<D>>(ahead.at<const T>(t.in, t), pl.at);
-          if (t.w) rx[u].template load_row<kStream<D>>(ahead.at<const T>(t.x, t), pl.at);
+          rg[u].load_row(ahead.at<const T>(t.in, t), pl.at);
+          if (t.w) rx[u].load_row(ahead.at<const T>(t.x, t), pl.at);
         }
         ahead.next(t, dr, dh);
       }
@@ -384,12 +408,12 @@ __global__ __launch_bounds__(kThreads, kBwdPerUnit<T>) void rotary_bwd_kernel(co
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           if (at.row >= t.rows) break;
-          float g[16], x[16];
+          float g[kElems<D>], x[kElems<D>];
           rg[u].get(g);
           if (t.w) rx[u].get(x);
           if (ahead.row < t.rows) {
-            rg[u].template load_row<kStream<D>>(ahead.at<const T>(t.in, t), pl.at);
-            if (t.w) rx[u].template load_row<kStream<D>>(ahead.at<const T>(t.x, t), pl.at);
+            rg[u].load_row(ahead.at<const T>(t.in, t), pl.at);
+            if (t.w) rx[u].load_row(ahead.at<const T>(t.x, t), pl.at);
           }
           ahead.next(t, dr, dh);
           turn(g, table, at.row, pl);
@@ -397,17 +421,17 @@ __global__ __launch_bounds__(kThreads, kBwdPerUnit<T>) void rotary_bwd_kernel(co
             const float rho = rms_scale<D>(x, p.eps);
             float dot = 0.f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
+            for (int i = 0; i < kElems<D>; ++i) {
               x[i] *= rho;
               acc[i] += g[i] * x[i];
               g[i] *= wt[i];
               dot += g[i] * x[i];
             }
-            const float mean = group_sum<D / 16>(dot) * (1.f / D);
+            const float mean = group_sum(dot) * (1.f / D);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) g[i] = rho * (g[i] - x[i] * mean);
+            for (int i = 0; i < kElems<D>; ++i) g[i] = rho * (g[i] - x[i] * mean);
           }
-          store_row<kStream<D>>(at.at<T>(t.out, t), pl.at, g);
+          store_row(at.at<T>(t.out, t), pl.at, g);
           at.next(t, dr, dh);
         }
       }
@@ -415,11 +439,11 @@ __global__ __launch_bounds__(kThreads, kBwdPerUnit<T>) void rotary_bwd_kernel(co
     }
     if (!p.part) continue;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < kElems<D>; ++i) {
       float v = acc[i];
 #pragma unroll
-      for (int m = L; m < 64; m *= 2) v += __shfl_xor(v, m);
-      if (threadIdx.x % 64 < L) sums[threadIdx.x / 64][pl.at[i / kUnit<T>] + i % kUnit<T>] = v;
+      for (int m = kLanes; m < 64; m *= 2) v += __shfl_xor(v, m);
+      if (threadIdx.x % 64 < kLanes) sums[threadIdx.x / 64][pl.at[i / kUnit<T>] + i % kUnit<T>] = v;
     }
     __syncthreads();
     if (threadIdx.x < D) {
@@ -484,7 +508,7 @@ struct VTile {
 template <typename T, int D, int ROWS>
 __device__ __forceinline__ void append_v(const RotaryParams& p, int64_t item, VTile<T, D, ROWS>& m) {
   constexpr int kRows = VTile<T, D, ROWS>::kRows, kStride = VTile<T, D, ROWS>::kStride;
-  constexpr int E = 16 / (int)sizeof(T);  // elements per 16-byte unit
+  constexpr int E = kUnit<T>;
   T* tile = m.tile;
   int64_t* place = m.place;
   int32_t* runs = m.runs;
@@ -498,13 +522,11 @@ __device__ __forceinline__ void append_v(const RotaryParams& p, int64_t item, VT
     const bool ok = row >= 0 && row < p.n && slot_of(p, row, blk, slot);
     place[tid] = ok ? (int64_t)blk * kBlock + slot : -2;
   }
-  constexpr int kUnits = kRows * D / E;
 #pragma unroll 4
-  for (int u = tid; u < kUnits; u += kThreads) {
+  for (int u = tid; u < kRows * D / E; u += kThreads) {
     const int r = u / (D / E), c = u % (D / E) * E;
     if (first + r < p.n) {
-      const u32x4 x =
-          __builtin_nontemporal_load(reinterpret_cast<const typename Unit<T>::type*>(head_row<T>(p.v, first + r, h) + c));
+      const u32x4 x = load_unit(head_row<T>(p.v, first + r, h) + c);
       T y[E];
       __builtin_memcpy(y, &x, 16);
 #pragma unroll
@@ -554,7 +576,7 @@ __global__ __launch_bounds__(kThreads) void rotary_append_kernel(const RotaryPar
     VTile<T, D, ROWS> v;
     __device__ Shared() {}
   } shared;
-  const Place<T, D, PAIRS> pl(threadIdx.x % (D / 16), p.pairs);
+  const Place<T, D, PAIRS> pl(p.pairs);
   for (int64_t b = blockIdx.x; b < p.items; b += gridDim.x) {
     if (b < p.items_v) {
       append_v<T, D, ROWS>(p, b, shared.v);
@@ -570,17 +592,19 @@ __global__ __launch_bounds__(kThreads) void rotary_append_kernel(const RotaryPar
     const bool is_q = i < n_q;
     T* cache = static_cast<T*>(p.k_cache);
     turn_tile(p, t, is_q ? p.q_pos : p.pos, is_q ? p.q_pos_stride : p.pos_stride, shared.table, pl,
-                           [&](const Cursor& c, const float (&x)[16]) {
+              [&](const Cursor& c, const float (&x)[kElems<D>]) {
       if (is_q) {
-        store_row<kStream<D>>(c.at<T>(t.out, t), pl.at, x);
+        store_row(c.at<T>(t.out, t), pl.at, x);
         return;
       }
       int32_t blk, slot;
       if (!slot_of(p, t.row0 + c.row, blk, slot)) return;
+      // (16 bytes of a line each: plain stores, which the L2 puts together)
 #pragma unroll
-      for (int u = 0; u < kUnits<T>; ++u)
-        store_unit<kStream<D>>(cache + paged_k_offset<D>(blk, t.h0 + c.h, p.Hkv, slot, pl.at[u] / 8) + pl.at[u] % 8,
-                   x + u * kUnit<T>);
+      for (int u = 0; u < kUnits<T, D>; ++u) {
+        T* dst = cache + paged_k_offset<D>(blk, t.h0 + c.h, p.Hkv, slot, pl.at[u] / 8) + pl.at[u] % 8;
+        *reinterpret_cast<u32x4*>(dst) = pack_unit(dst, x + u * kUnit<T>);
+      }
     });
   }
 }
@@ -592,14 +616,13 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Tiles of n rows of H heads (of H_all that the launch turns): as many turns a
 // group (up to max_turns) as leave the chip about that many workgroups, so that
 // a short call is spread over the chip.
-TileGrid tile_grid(int64_t n, int H, int H_all, int D, int max_turns, int64_t workgroups) {
+TileGrid tile_grid(int64_t n, int H, int H_all, int max_turns, int64_t workgroups) {
   TileGrid g{};
   if (n == 0 || H == 0) return g;
-  const int64_t groups = kThreads / (D / 16);
-  const int64_t turns = std::min<int64_t>(max_turns, ceil_div(n * H_all, groups * workgroups));
-  g.heads = (int32_t)std::min<int64_t>(H, groups * turns);
+  const int64_t turns = std::min<int64_t>(max_turns, ceil_div(n * H_all, kGroups * workgroups));
+  g.heads = (int32_t)std::min<int64_t>(H, kGroups * turns);
   g.head_runs = (int32_t)ceil_div(H, g.heads);
-  g.rows = (int32_t)std::max<int64_t>(1, std::min<int64_t>({groups * turns / g.heads, 4096 / D, n}));
+  g.rows = (int32_t)std::max<int64_t>(1, std::min<int64_t>({kGroups * turns / g.heads, kGroups, n}));
   g.items = ceil_div(n, g.rows) * g.head_runs;
   return g;
 }
@@ -650,9 +673,9 @@ dim3 grid_of(int64_t items) { return dim3((unsigned)std::min(items, kMaxGrid)); 
 // of them some tiles, with their D sums left once.
 constexpr int kComputeUnits = 256;
 void bwd_grids(int64_t n, int Hq, int Hkv, int D, bool bf16, TileGrid& q, TileGrid& k) {
-  q = tile_grid(n, Hq, Hq + Hkv, D, 8, kComputeUnits * 3 / 2);
-  k = tile_grid(n, Hkv, Hq + Hkv, D, 8, kComputeUnits * 3 / 2);
-  const int64_t held = kComputeUnits * (bf16 ? kBwdPerUnit<__bf16> : kBwdPerUnit<float>);
+  q = tile_grid(n, Hq, Hq + Hkv, 8, kComputeUnits * 3 / 2);
+  k = tile_grid(n, Hkv, Hq + Hkv, 8, kComputeUnits * 3 / 2);
+  const int64_t held = kComputeUnits * bwd_per_unit(D, bf16);
   const int64_t passes = ceil_div(q.items + k.items, held);
   for (TileGrid* g : {&q, &k})
     if (g->items > 0) g->items = ceil_div(g->items / g->head_runs, passes) * g->head_runs;
@@ -668,8 +691,8 @@ size_t rotary_bwd_parts(int64_t n, int Hq, int Hkv, int D, bool bf16) {
 
 hipError_t launch_rotary_fwd(RotaryParams p, int D, bool bf16, bool pairs, hipStream_t s) {
   p.n_q = p.n;
-  p.tiles_q = tile_grid(p.n, p.Hq, p.Hq + p.Hkv, D, 4, 4 * kComputeUnits);
-  p.tiles_k = tile_grid(p.n, p.Hkv, p.Hq + p.Hkv, D, 4, 4 * kComputeUnits);
+  p.tiles_q = tile_grid(p.n, p.Hq, p.Hq + p.Hkv, 4, 4 * kComputeUnits);
+  p.tiles_k = tile_grid(p.n, p.Hkv, p.Hq + p.Hkv, 4, 4 * kComputeUnits);
   p.items = p.tiles_q.items + p.tiles_k.items;
   if (p.items == 0) return hipSuccess;
   return dispatch<Fwd>(p, D, bf16, pairs, grid_of(p.items), s);
@@ -690,9 +713,13 @@ hipError_t launch_rotary_bwd(RotaryParams p, int D, bool bf16, bool pairs, float
 }
 
 hipError_t launch_rotary_append(RotaryParams p, int D, bool bf16, bool pairs, hipStream_t s) {
-  p.tiles_q = tile_grid(p.n_q, p.Hq, p.Hq + p.Hkv, D, 4, 4 * kComputeUnits);
-  p.tiles_k = tile_grid(p.n, p.Hkv, p.Hq + p.Hkv, D, 4, 4 * kComputeUnits);
-  const bool tall = (int64_t)p.n * p.Hkv >= 16384;  // 64 rows a workgroup where that leaves every compute unit one
+  p.tiles_q = tile_grid(p.n_q, p.Hq, p.Hq + p.Hkv, 4, 4 * kComputeUnits);
+  p.tiles_k = tile_grid(p.n, p.Hkv, p.Hq + p.Hkv, 4, 4 * kComputeUnits);
+  // V rows of a workgroup: 64 of many (whole runs of a prefill together), 8 of
+  // few (a decode step's scattered rows).  Measured, bf16, d = 128, 2 KV heads:
+  // 4,000 rows in runs 12.0 us a call (15.8 in eights), 20,000 42.5; 3,200
+  // scattered rows 20.4 us (17.7 in eights), 1,600 11.6, 5,000 25.3 either way.
+  const bool tall = (int64_t)p.n * p.Hkv >= 6144;
   p.items_v = ceil_div(p.n, tall ? 64 : 8) * p.Hkv;
   p.items = p.items_v + p.tiles_q.items + p.tiles_k.items + ceil_div(p.n_patch, kThreads);
   if (p.items == 0) return hipSuccess;
