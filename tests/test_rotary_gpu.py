@@ -21,7 +21,7 @@ def binding(request, monkeypatch):
     return request.param
 
 
-HEADS = {"gqa": (16, 2), "seven": (28, 4), "odd": (5, 3)}
+HEADS = {"gqa": (16, 2), "seven": (28, 4), "odd": (5, 3), "many": (70, 33)}
 
 
 def _say(*a):
@@ -146,6 +146,58 @@ def test_in_place_and_other_orders(dtype):
     dq, dk, dwq, dwk = pa.rotary_bwd(g, None, pos, st.handle, qt, None, wq, None, dq=g)
     assert dk is None and dwk is None and dwq is not None
     check("dq in place", g, want, tol)
+
+
+def test_the_forwards_rows_become_their_gradients():
+    st, n, d = Setup(64, "bf16"), 50, 64
+    x, g, w, pos = normal((n, 3, d), 1, "bf16"), normal((n, 3, d), 2, "bf16"), normal((d,), 3, "bf16"), positions(3, n, 4)
+    want, tol, dw, dtol = st.backward(g, x, pos, w)
+    out = pa.rotary_bwd(g, None, pos, st.handle, x, None, w, dq=x)
+    assert out[0].data_ptr() == x.data_ptr()
+    check("dq", x, want, tol)
+    check("dw", out[2], dw, dtol)
+
+
+def test_one_position_for_every_axis():
+    st, n, d = Setup(64, "f32"), 33, 64
+    x, pos = normal((n, 2, d), 1, "f32"), positions(1, n, 2).expand(3, n)
+    z, _ = pa.rotary_fwd(x, None, pos, st.handle)
+    check("z", z, *st.forward(x, pos))
+
+
+def test_two_streams_at_once():
+    st, n, d = Setup(128, "bf16"), 9000, 128
+    w, pos = normal((d,), 1, "bf16"), positions(3, n, 2)
+    rows = [(normal((n, 4, d), 10 + i, "bf16"), normal((n, 4, d), 20 + i, "bf16")) for i in range(2)]
+    run = lambda x, g: (pa.rotary_fwd(x, None, pos, st.handle, w)[0], *pa.rotary_bwd(g, None, pos, st.handle, x, None, w)[::2])  # noqa: E731
+    want = [run(*r) for r in rows]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in rows]
+    for _ in range(5):
+        got = []
+        for s, r in zip(streams, rows):
+            with torch.cuda.stream(s):
+                got.append(run(*r))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y))
+
+
+def test_more_rows_than_32_bits_address(binding):
+    """Rows behind 2^33 elements, in more tiles than a launch has workgroups."""
+    if binding == "python" or torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("once, and where there is room")
+    st, part, times, d = Setup(64, "bf16", n_axes=1), 1 << 20, 135, 64
+    n = part * times
+    base, pos = normal((part, 1, d), 1, "bf16"), torch.arange(n, dtype=torch.int32, device="cuda")
+    x = base.repeat(times, 1, 1)
+    z, _ = pa.rotary_fwd(x, None, pos, st.handle)
+    at = torch.cat([torch.arange(40), torch.arange(n - 40, n), torch.randint(0, n, (300,), generator=torch.Generator().manual_seed(2))]).cuda()
+    check("rows", z[at], *st.forward(x[at], pos[at][None]))
+    back = pa.rotary_bwd(z, None, pos, st.handle, dq=z)[0]  # turned back, in place: the rows, rounded twice
+    # z is off by 2^-8 of itself, so the rows turned back by 2^-8 (|z_a| + |z_b|) <= 2^-8 sqrt(2) (|a| + |b|) and 2^-8 |a|
+    for i in range(0, times, 15):
+        err = (back[i * part:(i + 1) * part].float() - base.float()).abs()
+        assert bool((err <= 2.0 ** -7 * 1.5 * (base.float().abs() + base.float().roll(32, -1).abs())).all()), i
 
 
 @pytest.mark.parametrize("which", ["q", "k"])
@@ -327,6 +379,19 @@ def test_append_long():
     _say("long")
     lengths, firsts = (2557, 1031, 700), (0, 3, 8)
     _check_append(Setup(128, "bf16"), 4, 2, 128, "bf16", _runs(lengths, firsts, 300, 1), 300, True)
+
+
+def test_append_many_heads_and_queries_in_place():
+    _say("many heads")
+    _check_append(Setup(64, "bf16"), 70, 33, 64, "bf16", _runs((9, 30), (3, 0), 5, 1), 5, True)
+    st, n, d = Setup(128, "bf16", style="pairs"), 20, 128
+    buf, q, k, v = _fused(n, 4, 2, d, "bf16", 1)
+    pos, w, s = positions(3, n, 2), normal((d,), 3, "bf16"), torch.from_numpy(_slots(n, 4, 4)).cuda()
+    kc, vc = torch.zeros((4, 2, 16, 16, 8), dtype=torch.bfloat16, device="cuda"), torch.zeros((4, 2, d, 16), dtype=torch.bfloat16, device="cuda")
+    want, k0 = st.forward(q, pos, w), k.clone()
+    out = pa.rotary_append(q, k, v, pos, s, kc, vc, st.handle, w, w, q_out=q)
+    assert out.data_ptr() == q.data_ptr() and torch.equal(k, k0)
+    check("q", q, *want)
 
 
 def test_append_keys_alone():

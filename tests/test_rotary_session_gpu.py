@@ -190,6 +190,21 @@ def test_copies_run_before_a_plain_launch_too():
         compare(f"stream {(a, b)[i]}", o[i:i + 1], lse[i:i + 1], O, L, "bf16")
 
 
+def test_queries_rotated_in_place_on_a_stream():
+    s = Server(8, 2, 128, "bf16", 20, "halves")
+    s.open()
+    s.s.prepare([21], [21])
+    q, k, v, pos = normal((21, 8, 128), 1, "bf16"), normal((21, 2, 128), 2, "bf16"), normal((21, 2, 128), 3, "bf16"), positions(3, 21, 4)
+    (zq, tol), (zk, _) = (s.st.forward(x, pos, w) for x, w in ((q, s.wq), (k, s.wk)))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    o, lse = s.s.launch_rotary(q, k, v, pos, s.st.handle, s.wq, s.wk, q_rot=q, stream=side)
+    side.synchronize()
+    check("q", q, zq, tol)
+    O, L = oracle.tree_attention([(-1, 0, 21, 21)], torch.from_numpy(zq).bfloat16(), torch.from_numpy(zk).bfloat16(), v, 1 / math.sqrt(128), 8, 2)
+    compare("in place", o, lse, O, L, "bf16")
+
+
 def test_session_refusals():
     s = Server(8, 2, 128, "bf16", 20, "halves")
     s.open()
