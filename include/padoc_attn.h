@@ -326,7 +326,8 @@ padoc_status padoc_cache_from_rows(const void* k_rows, const void* v_rows, void*
  *     z_a = scale * (y_a cos t - y_b sin t),  z_b = scale * (y_b cos t + y_a sin t)
  *   every other dimension: z = y
  *
- * Computed in fp32 and rounded once.  Positions are int32, negative ones and
+ * Computed in fp32 (mean squares too: rows whose squares leave its normal range
+ * lose precision) and rounded once.  Positions are int32, negative ones and
  * ones of any size included: angles are reduced in 64-bit fixed-point turns,
  * so they stay exact to about 1e-7 radians at every position.
  * ------------------------------------------------------------------------- */
@@ -371,9 +372,10 @@ typedef struct {
 
 /* z of n_rows rows of q (num_heads_q heads) and k (num_heads_kv), one kernel.
    Either head count may be 0 (its pointers are not read then).  pos: device
-   int32, position of row r on axis a at pos[a * pos_stride + r].  q_weight /
-   k_weight: device, head_dim elements, or NULL.  n_rows <= 2^31-1, head counts
-   <= 4096.  Nothing is allocated; the launch may be captured. */
+   int32, position of row r on axis a at pos[a * pos_stride + r] (pos_stride 0,
+   or at least n_rows).  q_weight / k_weight: device, head_dim elements, or
+   NULL.  n_rows <= 2^31-1, head counts <= 4096.  Nothing is allocated; the
+   launch may be captured. */
 typedef struct {
   int64_t n_rows;
   int32_t num_heads_q, num_heads_kv;

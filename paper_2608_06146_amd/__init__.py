@@ -427,15 +427,16 @@ class Rotary:
     """Head norms and rotary positions of a decoder layer (``padoc_rotary``):
     the first ``rotary_dim`` dimensions (default: all) of every head are
     rotated by the positions of up to four axes.  ``axis[i]`` is the axis of
-    pair i, or ``sections`` counts the pairs of each axis in order; neither:
-    one axis.  ``inv_freq`` (radians per position of each pair) replaces
+    pair i (of ``n_axes``; default: as many as it names), or ``sections`` counts
+    the pairs of each axis in order; neither: one axis.  ``inv_freq`` (radians per position of each pair) replaces
     ``base ** (-2 i / rotary_dim)``.  ``style``: "halves" pairs dimensions i
     and i + rotary_dim/2, "pairs" 2i and 2i + 1.  ``scale`` multiplies the
     cosines and sines; ``eps`` belongs to the norms (used where a call passes
     weights).  Host memory only."""
 
     def __init__(self, head_dim: int, dtype: str = "bf16", rotary_dim: Optional[int] = None, sections=None, axis=None,
-                 base: float = 10000.0, inv_freq=None, style: str = "halves", scale: float = 1.0, eps: float = 1e-6):
+                 base: float = 10000.0, inv_freq=None, style: str = "halves", scale: float = 1.0, eps: float = 1e-6,
+                 n_axes: Optional[int] = None):
         self.head_dim, self.dtype = int(head_dim), dtype
         self.rotary_dim = self.head_dim if rotary_dim is None else int(rotary_dim)
         if style not in _STYLES:
@@ -450,7 +451,9 @@ class Rotary:
         for name, a in (("axis / sections", ax), ("inv_freq", fr)):
             if a is not None and a.shape != (pairs,):
                 raise ValueError(f"{name} must cover the {pairs} rotated pairs, got shape {a.shape}")
-        self.n_axes = 1 if ax is None else len(sections) if sections is not None else int(ax.max(initial=0)) + 1
+        if n_axes is None:
+            n_axes = 1 if ax is None else len(sections) if sections is not None else int(ax.max(initial=0)) + 1
+        self.n_axes = int(n_axes)
         desc = _lib.RotaryDesc(self.head_dim, self.rotary_dim, self.n_axes, _STYLES[style],
                                ax.ctypes.data if ax is not None else None,
                                fr.ctypes.data if fr is not None else None, float(base), float(scale), float(eps),

@@ -62,25 +62,28 @@ struct Unit<float> {
   typedef u32x4 type __attribute__((aligned(4)));
 };
 
-// Rows are loaded and stored past the caches (non-temporal).  Measured, in turn
-// over more data than the caches hold: 43,067 rows of 18 heads of 128 (bf16) 70.1
-// us (5.7 TB/s) with, 78.8 without.
-template <typename T>
+// Rows are stored past the caches (non-temporal), and loaded so (STREAM) by
+// calls that read and write more than 128 MiB, half of what the last-level cache
+// holds; of shorter calls the producer's rows are likely still there.  Measured
+// with inputs and outputs in turn: 43,067 rows of 18 heads of 128 (bf16) 69.3 us
+// (5.7 TB/s), with plain loads 72.0, plain stores 74.0, both plain 78.2; their
+// backward 111.4, 116.2, 119.1 and 120.6; 5,437 rows of 32 heads of 64 (fp32, 89
+// MB) 15.0 with plain loads, 17.2 past the caches.
+constexpr int64_t kStreamBytes = 128 << 20;
+template <bool STREAM, typename T>
 __device__ __forceinline__ u32x4 load_unit(const T* p) {
-  return __builtin_nontemporal_load(reinterpret_cast<const typename Unit<T>::type*>(p));
+  const auto q = reinterpret_cast<const typename Unit<T>::type*>(p);
+  return STREAM ? __builtin_nontemporal_load(q) : *q;
 }
 
 // A lane's elements of a head as they were loaded: its units in turn.
 template <typename T, int D>
 struct Raw {
   u32x4 u[kUnits<T, D>];
-  __device__ __forceinline__ void load_row(const T* p, const int (&at)[kUnits<T, D>]) {
+  template <bool STREAM>
+  __device__ __forceinline__ void load(const T* p, const int (&at)[kUnits<T, D>]) {
 #pragma unroll
-    for (int i = 0; i < kUnits<T, D>; ++i) u[i] = load_unit(p + at[i]);
-  }
-  __device__ __forceinline__ void load_weight(const T* p, const int (&at)[kUnits<T, D>]) {
-#pragma unroll
-    for (int i = 0; i < kUnits<T, D>; ++i) u[i] = *reinterpret_cast<const typename Unit<T>::type*>(p + at[i]);
+    for (int i = 0; i < kUnits<T, D>; ++i) u[i] = load_unit<STREAM>(p + at[i]);
   }
   __device__ __forceinline__ void get(float (&x)[kElems<D>]) const {
 #pragma unroll
@@ -314,7 +317,7 @@ struct Cursor {
 // Rows of a tile: norm, rotation, and `put(row, head, values)`.  The first
 // rows are asked for before the angles are computed, the others kAhead turns
 // before theirs.
-template <typename T, int D, bool PAIRS, class Put>
+template <bool STREAM, typename T, int D, bool PAIRS, class Put>
 __device__ __forceinline__ void turn_tile(const RotaryParams& p, const Tile& t, const int32_t* pos, int64_t pos_stride,
                                           AngleTable<T, D, PAIRS>& table, const Place<T, D, PAIRS>& pl, Put put) {
   constexpr int U = kAhead;
@@ -323,10 +326,10 @@ __device__ __forceinline__ void turn_tile(const RotaryParams& p, const Tile& t, 
   Raw<T, D> raw[U], rw;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    if (ahead.row < t.rows) raw[u].load_row(ahead.at<const T>(t.in, t), pl.at);
+    if (ahead.row < t.rows) raw[u].template load<STREAM>(ahead.at<const T>(t.in, t), pl.at);
     ahead.next(t, dr, dh);
   }
-  if (t.w) rw.load_weight(static_cast<const T*>(t.w), pl.at);
+  if (t.w) rw.template load<false>(static_cast<const T*>(t.w), pl.at);
   table.fill(p, pos, pos_stride, t.row0, t.rows);
   __syncthreads();
   float wt[kElems<D>];
@@ -337,7 +340,7 @@ __device__ __forceinline__ void turn_tile(const RotaryParams& p, const Tile& t, 
       if (at.row >= t.rows) break;
       float x[kElems<D>];
       raw[u].get(x);
-      if (ahead.row < t.rows) raw[u].load_row(ahead.at<const T>(t.in, t), pl.at);
+      if (ahead.row < t.rows) raw[u].template load<STREAM>(ahead.at<const T>(t.in, t), pl.at);
       ahead.next(t, dr, dh);
       if (t.w) {
         const float rho = rms_scale<D>(x, p.eps);
@@ -353,13 +356,13 @@ __device__ __forceinline__ void turn_tile(const RotaryParams& p, const Tile& t, 
 }
 
 // Forward (and, with `inverse`, the backward of a rotation without norms).
-template <typename T, int D, bool PAIRS>
+template <typename T, int D, bool PAIRS, bool STREAM>
 __global__ __launch_bounds__(kThreads) void rotary_fwd_kernel(const RotaryParams p) {
   __shared__ AngleTable<T, D, PAIRS> table;
   const Place<T, D, PAIRS> pl(p.pairs);
   for (int64_t b = blockIdx.x; b < p.items; b += gridDim.x) {
     const Tile t = tile_of(p, b);
-    turn_tile(p, t, p.pos, p.pos_stride, table, pl, [&](const Cursor& c, const float (&x)[kElems<D>]) {
+    turn_tile<STREAM>(p, t, p.pos, p.pos_stride, table, pl, [&](const Cursor& c, const float (&x)[kElems<D>]) {
       store_row(c.at<T>(t.out, t), pl.at, x);
     });
   }
@@ -373,7 +376,7 @@ constexpr int bwd_per_unit(int D, bool bf16) { return D == 64 ? 4 : bf16 ? 3 : 2
 // wavefront and over the four wavefronts through LDS, into part[item][D].  The
 // tiles of an item lie as many rows apart as all items take at once, so that
 // what the chip reads at a time is one stretch of memory.
-template <typename T, int D, bool PAIRS>
+template <typename T, int D, bool PAIRS, bool STREAM>
 __global__ __launch_bounds__(kThreads, bwd_per_unit(D, sizeof(T) == 2)) void rotary_bwd_kernel(const RotaryParams p) {
   constexpr int U = sizeof(T) == 2 ? 2 : 1;  // rows of each tensor in flight
   __shared__ AngleTable<T, D, PAIRS> table;
@@ -385,7 +388,7 @@ __global__ __launch_bounds__(kThreads, bwd_per_unit(D, sizeof(T) == 2)) void rot
     float acc[kElems<D>] = {}, wt[kElems<D>];
     if (t.w) {
       Raw<T, D> rw;
-      rw.load_weight(static_cast<const T*>(t.w), pl.at);
+      rw.template load<false>(static_cast<const T*>(t.w), pl.at);
       rw.get(wt);
     }
     const TileGrid& grid = b < p.tiles_q.items ? p.tiles_q : p.tiles_k;
@@ -397,8 +400,8 @@ __global__ __launch_bounds__(kThreads, bwd_per_unit(D, sizeof(T) == 2)) void rot
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (ahead.row < t.rows) {
-          rg[u].load_row(ahead.at<const T>(t.in, t), pl.at);
-          if (t.w) rx[u].load_row(ahead.at<const T>(t.x, t), pl.at);
+          rg[u].template load<STREAM>(ahead.at<const T>(t.in, t), pl.at);
+          if (t.w) rx[u].template load<STREAM>(ahead.at<const T>(t.x, t), pl.at);
         }
         ahead.next(t, dr, dh);
       }
@@ -412,8 +415,8 @@ __global__ __launch_bounds__(kThreads, bwd_per_unit(D, sizeof(T) == 2)) void rot
           rg[u].get(g);
           if (t.w) rx[u].get(x);
           if (ahead.row < t.rows) {
-            rg[u].load_row(ahead.at<const T>(t.in, t), pl.at);
-            if (t.w) rx[u].load_row(ahead.at<const T>(t.x, t), pl.at);
+            rg[u].template load<STREAM>(ahead.at<const T>(t.in, t), pl.at);
+            if (t.w) rx[u].template load<STREAM>(ahead.at<const T>(t.x, t), pl.at);
           }
           ahead.next(t, dr, dh);
           turn(g, table, at.row, pl);
@@ -505,7 +508,7 @@ struct VTile {
   int32_t n_runs;
 };
 
-template <typename T, int D, int ROWS>
+template <bool STREAM, typename T, int D, int ROWS>
 __device__ __forceinline__ void append_v(const RotaryParams& p, int64_t item, VTile<T, D, ROWS>& m) {
   constexpr int kRows = VTile<T, D, ROWS>::kRows, kStride = VTile<T, D, ROWS>::kStride;
   constexpr int E = kUnit<T>;
@@ -526,7 +529,7 @@ __device__ __forceinline__ void append_v(const RotaryParams& p, int64_t item, VT
   for (int u = tid; u < kRows * D / E; u += kThreads) {
     const int r = u / (D / E), c = u % (D / E) * E;
     if (first + r < p.n) {
-      const u32x4 x = load_unit(head_row<T>(p.v, first + r, h) + c);
+      const u32x4 x = load_unit<STREAM>(head_row<T>(p.v, first + r, h) + c);
       T y[E];
       __builtin_memcpy(y, &x, 16);
 #pragma unroll
@@ -569,7 +572,7 @@ __device__ __forceinline__ void append_v(const RotaryParams& p, int64_t item, VT
 // Append: items of four roles, one after the other: v's rows into the V cache,
 // tiles of q's rows into q_out, tiles of k's rows into their slots of the K
 // cache, block-table patches.
-template <typename T, int D, bool PAIRS, int ROWS>
+template <typename T, int D, bool PAIRS, int ROWS, bool STREAM>
 __global__ __launch_bounds__(kThreads) void rotary_append_kernel(const RotaryParams p) {
   __shared__ union Shared {
     AngleTable<T, D, PAIRS> table;
@@ -579,7 +582,7 @@ __global__ __launch_bounds__(kThreads) void rotary_append_kernel(const RotaryPar
   const Place<T, D, PAIRS> pl(p.pairs);
   for (int64_t b = blockIdx.x; b < p.items; b += gridDim.x) {
     if (b < p.items_v) {
-      append_v<T, D, ROWS>(p, b, shared.v);
+      append_v<STREAM>(p, b, shared.v);
       continue;
     }
     const int64_t i = b - p.items_v, n_q = p.tiles_q.items, n_turned = n_q + p.tiles_k.items;
@@ -591,7 +594,7 @@ __global__ __launch_bounds__(kThreads) void rotary_append_kernel(const RotaryPar
     const Tile t = tile_of(p, i);
     const bool is_q = i < n_q;
     T* cache = static_cast<T*>(p.k_cache);
-    turn_tile(p, t, is_q ? p.q_pos : p.pos, is_q ? p.q_pos_stride : p.pos_stride, shared.table, pl,
+    turn_tile<STREAM>(p, t, is_q ? p.q_pos : p.pos, is_q ? p.q_pos_stride : p.pos_stride, shared.table, pl,
               [&](const Cursor& c, const float (&x)[kElems<D>]) {
       if (is_q) {
         store_row(c.at<T>(t.out, t), pl.at, x);
@@ -643,27 +646,36 @@ hipError_t dispatch(const RotaryParams& p, int D, bool bf16, bool pairs, dim3 gr
   return hipGetLastError();
 }
 
-template <typename T, int D, bool PAIRS>
+template <bool STREAM>
 struct Fwd {
-  static void go(const RotaryParams& p, dim3 grid, hipStream_t s) {
-    hipLaunchKernelGGL((rotary_fwd_kernel<T, D, PAIRS>), grid, dim3(kThreads), 0, s, p);
-  }
+  template <typename T, int D, bool PAIRS>
+  struct Call {
+    static void go(const RotaryParams& p, dim3 grid, hipStream_t s) {
+      hipLaunchKernelGGL((rotary_fwd_kernel<T, D, PAIRS, STREAM>), grid, dim3(kThreads), 0, s, p);
+    }
+  };
 };
-template <typename T, int D, bool PAIRS>
+template <bool STREAM>
 struct Bwd {
-  static void go(const RotaryParams& p, dim3 grid, hipStream_t s) {
-    hipLaunchKernelGGL((rotary_bwd_kernel<T, D, PAIRS>), grid, dim3(kThreads), 0, s, p);
-  }
+  template <typename T, int D, bool PAIRS>
+  struct Call {
+    static void go(const RotaryParams& p, dim3 grid, hipStream_t s) {
+      hipLaunchKernelGGL((rotary_bwd_kernel<T, D, PAIRS, STREAM>), grid, dim3(kThreads), 0, s, p);
+    }
+  };
 };
-template <int ROWS>
+template <int ROWS, bool STREAM>
 struct Append {
   template <typename T, int D, bool PAIRS>
   struct Call {
     static void go(const RotaryParams& p, dim3 grid, hipStream_t s) {
-      hipLaunchKernelGGL((rotary_append_kernel<T, D, PAIRS, ROWS>), grid, dim3(kThreads), 0, s, p);
+      hipLaunchKernelGGL((rotary_append_kernel<T, D, PAIRS, ROWS, STREAM>), grid, dim3(kThreads), 0, s, p);
     }
   };
 };
+
+// Whether a call that moves `rows` rows of a head goes past the caches.
+bool streams(int64_t rows, int D, bool bf16) { return rows * D * (bf16 ? 2 : 4) > kStreamBytes; }
 
 dim3 grid_of(int64_t items) { return dim3((unsigned)std::min(items, kMaxGrid)); }
 
@@ -695,7 +707,9 @@ hipError_t launch_rotary_fwd(RotaryParams p, int D, bool bf16, bool pairs, hipSt
   p.tiles_k = tile_grid(p.n, p.Hkv, p.Hq + p.Hkv, 4, 4 * kComputeUnits);
   p.items = p.tiles_q.items + p.tiles_k.items;
   if (p.items == 0) return hipSuccess;
-  return dispatch<Fwd>(p, D, bf16, pairs, grid_of(p.items), s);
+  return streams((int64_t)p.n * (p.Hq + p.Hkv) * 2, D, bf16)
+             ? dispatch<Fwd<true>::Call>(p, D, bf16, pairs, grid_of(p.items), s)
+             : dispatch<Fwd<false>::Call>(p, D, bf16, pairs, grid_of(p.items), s);
 }
 
 hipError_t launch_rotary_bwd(RotaryParams p, int D, bool bf16, bool pairs, float* dwq, float* dwk, hipStream_t s) {
@@ -703,7 +717,9 @@ hipError_t launch_rotary_bwd(RotaryParams p, int D, bool bf16, bool pairs, float
   bwd_grids(p.n, p.Hq, p.Hkv, D, bf16, p.tiles_q, p.tiles_k);
   p.items = p.tiles_q.items + p.tiles_k.items;
   if (p.items > 0) {
-    const hipError_t e = dispatch<Bwd>(p, D, bf16, pairs, grid_of(p.items), s);
+    const hipError_t e = streams((int64_t)p.n * (p.Hq + p.Hkv) * 3, D, bf16)
+                             ? dispatch<Bwd<true>::Call>(p, D, bf16, pairs, grid_of(p.items), s)
+                             : dispatch<Bwd<false>::Call>(p, D, bf16, pairs, grid_of(p.items), s);
     if (e != hipSuccess) return e;
   }
   if (dwq || dwk)
@@ -724,8 +740,10 @@ hipError_t launch_rotary_append(RotaryParams p, int D, bool bf16, bool pairs, hi
   p.items = p.items_v + p.tiles_q.items + p.tiles_k.items + ceil_div(p.n_patch, kThreads);
   if (p.items == 0) return hipSuccess;
   const dim3 grid = grid_of(p.items);
-  return tall ? dispatch<Append<64>::Call>(p, D, bf16, pairs, grid, s)
-              : dispatch<Append<8>::Call>(p, D, bf16, pairs, grid, s);
+  if (!tall) return dispatch<Append<8, false>::Call>(p, D, bf16, pairs, grid, s);
+  return streams(((int64_t)p.n_q * p.Hq + (int64_t)p.n * p.Hkv * 2) * 2, D, bf16)
+             ? dispatch<Append<64, true>::Call>(p, D, bf16, pairs, grid, s)
+             : dispatch<Append<64, false>::Call>(p, D, bf16, pairs, grid, s);
 }
 
 }  // namespace padoc

@@ -66,7 +66,8 @@ def test_argument_sizes():
     (dict(base=float("nan")), _lib.ERR_ARG), (dict(base=1e-322), _lib.ERR_ARG), (dict(scale=float("nan")), _lib.ERR_ARG),
     (dict(eps=-1.0), _lib.ERR_ARG), (dict(eps=float("inf")), _lib.ERR_ARG),
     (dict(axis=[0] * 63 + [4]), _lib.ERR_SHAPE), (dict(axis=[0] * 63 + [-1]), _lib.ERR_BOUNDS),
-    (dict(sections=(10, 10, 10, 10, 24)), _lib.ERR_SHAPE), (dict(inv_freq=[0.0] * 63 + [float("inf")]), _lib.ERR_ARG)])
+    (dict(sections=(10, 10, 10, 10, 24)), _lib.ERR_SHAPE), (dict(n_axes=0), _lib.ERR_SHAPE),
+    (dict(axis=[2] * 64, n_axes=2), _lib.ERR_BOUNDS), (dict(inv_freq=[0.0] * 63 + [float("inf")]), _lib.ERR_ARG)])
 def test_handles_refused(kw, status):
     with pytest.raises(_lib.PadocError) as e:
         pa.Rotary(**{"head_dim": 128, **kw})
@@ -88,6 +89,7 @@ def test_handles_refused_in_python():
     d = _lib.RotaryDesc(128, 128, 1, 2, None, None, 1e4, 1.0, 1e-6, 0)
     assert L.padoc_rotary_create(C.byref(d), C.byref(h)) == _lib.ERR_ARG
     assert L.padoc_rotary_create(C.byref(d), None) == _lib.ERR_ARG
+    assert pa.Rotary(64, axis=[0] * 32, n_axes=3).n_axes == 3 and pa.Rotary(64, sections=(20, 12, 0)).n_axes == 3
     r = pa.Rotary(64)
     r.close()
     r.close()

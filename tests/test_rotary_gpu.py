@@ -68,6 +68,17 @@ def test_long_runs_of_heads(d, n):
     _fwd_bwd(Setup(d, "bf16"), n, 4, 1, d, "bf16", True)
 
 
+@pytest.mark.parametrize("style", ["halves", "pairs"])
+def test_calls_past_the_caches(style, binding):
+    """More than 128 MiB: forward, backward, append."""
+    if binding == "python":
+        pytest.skip("once")
+    _say(style)
+    st = Setup(128, "bf16", style=style)
+    _fwd_bwd(st, 26500, 8, 2, 128, "bf16", True)
+    _check_append(st, 16, 2, 128, "bf16", _runs((13300, 37), (5, 0), 850, 1), 850, True)
+
+
 @pytest.mark.parametrize("far", [10 ** 6, 2 ** 31 - 5001, -2 ** 31, -77])
 def test_far_positions(far):
     _say(far)
