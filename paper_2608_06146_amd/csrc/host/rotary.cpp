@@ -5,6 +5,7 @@
 #include <cmath>
 #include <limits>
 #include <new>
+#include <numeric>
 #include <vector>
 
 using padoc::clear_error;
@@ -47,24 +48,49 @@ padoc_status check_heads(const char* name, const padoc_heads& x, int64_t n, int3
   return PADOC_OK;
 }
 
-// Whether `out` may be written while `in` is read: the same rows, or apart.
-padoc_status check_apart(const char* name, const padoc_heads& in, const char* out_name, const padoc_heads& out,
-                         int64_t n, int32_t H, int32_t D, size_t esz) {
-  if (n == 0 || H == 0) return PADOC_OK;
-  const bool same_rows = n == 1 || in.row_stride == out.row_stride;
-  if (in.data == out.data && same_rows && (H == 1 || in.head_stride == out.head_stride)) return PADOC_OK;
-  const uintptr_t a = (uintptr_t)in.data, b = (uintptr_t)out.data;
-  const uintptr_t an = (uintptr_t)extent(in, n, H, D) * esz, bn = (uintptr_t)extent(out, n, H, D) * esz;
+// Rows of a call's tensor: n rows of H heads.
+struct Rows {
+  const char* name;
+  const padoc_heads& at;
+  int64_t n;
+  int32_t H;
+};
+
+// Whether `out` may be written while `in` is read or written: apart, or (where
+// `same` allows it) the same rows, which their one reader writes.
+padoc_status check_apart(const Rows& in, const Rows& out, int32_t D, size_t esz, bool same) {
+  if (in.n == 0 || in.H == 0 || out.n == 0 || out.H == 0) return PADOC_OK;
+  const bool strides = in.n == 1 || in.at.row_stride == out.at.row_stride;
+  if (same && in.at.data == out.at.data && strides && (in.H == 1 || in.at.head_stride == out.at.head_stride))
+    return PADOC_OK;
+  const uintptr_t a = (uintptr_t)in.at.data, b = (uintptr_t)out.at.data;
+  const uintptr_t an = (uintptr_t)extent(in.at, in.n, in.H, D) * esz;
+  const uintptr_t bn = (uintptr_t)extent(out.at, out.n, out.H, D) * esz;
   if (a + an <= b || b + bn <= a) return PADOC_OK;
-  // slices of the same rows side by side
-  const int64_t rs = in.row_stride * (int64_t)esz;
-  const int64_t sa = ((H - 1) * in.head_stride + D) * (int64_t)esz, sb = ((H - 1) * out.head_stride + D) * (int64_t)esz;
-  if (same_rows && n > 1 && sa <= rs && sb <= rs) {
-    int64_t delta = (int64_t)(b - a) % rs;
-    if (delta < 0) delta += rs;
-    if (delta >= sa && delta + sb <= rs) return PADOC_OK;
+  const auto clear = [&](int64_t step, int64_t in_span, int64_t out_span) {  // each within a step, beside the other
+    const int64_t delta = ((int64_t)(b - a) % step + step) % step;
+    return in_span <= delta && delta + out_span <= step;
+  };
+  // slices of the same rows side by side, or of the same heads where rows lie within heads
+  for (int by_head = 0; by_head < 2; ++by_head) {
+    const auto count = [&](const Rows& x) { return by_head ? (int64_t)x.H : x.n; };
+    const auto stride = [&](const Rows& x) { return (by_head ? x.at.head_stride : x.at.row_stride) * (int64_t)esz; };
+    const auto span = [&](const Rows& x) {
+      return (by_head ? (x.n - 1) * x.at.row_stride : (x.H - 1) * x.at.head_stride) * (int64_t)esz + D * (int64_t)esz;
+    };
+    if (count(in) > 1 && count(out) > 1 && stride(in) == stride(out) && stride(in) > 0 &&
+        clear(stride(in), span(in), span(out)))
+      return PADOC_OK;
   }
-  return set_error(PADOC_ERR_ARG, "%s overlaps %s without being the same rows", out_name, name);
+  // heads side by side ([n, H, 3, D] with q, k and v of a head together): every
+  // row and head lies a multiple of `step` elements from its tensor's start
+  int64_t step = 0;
+  for (const Rows* x : {&in, &out}) {
+    if (x->n > 1) step = std::gcd(step, x->at.row_stride);
+    if (x->H > 1) step = std::gcd(step, x->at.head_stride);
+  }
+  if (step > 0 && clear(step * (int64_t)esz, D * (int64_t)esz, D * (int64_t)esz)) return PADOC_OK;
+  return set_error(PADOC_ERR_ARG, "%s overlaps %s%s", out.name, in.name, same ? " without being the same rows" : "");
 }
 
 padoc_status check_pos(const char* name, const padoc_rotary* r, const int32_t* pos, int64_t stride, int64_t n) {
@@ -110,8 +136,12 @@ padoc_status check_rotary_fwd(const padoc_rotary* r, const padoc_rotary_fwd_args
   PADOC_TRY(check_heads("k", a->k, n, Hkv, r->D, e, false));
   PADOC_TRY(check_heads("q_out", a->q_out, n, Hq, r->D, e, true));
   PADOC_TRY(check_heads("k_out", a->k_out, n, Hkv, r->D, e, true));
-  PADOC_TRY(check_apart("q", a->q, "q_out", a->q_out, n, Hq, r->D, e));
-  PADOC_TRY(check_apart("k", a->k, "k_out", a->k_out, n, Hkv, r->D, e));
+  const Rows q{"q", a->q, n, Hq}, k{"k", a->k, n, Hkv}, q_out{"q_out", a->q_out, n, Hq}, k_out{"k_out", a->k_out, n, Hkv};
+  PADOC_TRY(check_apart(q, q_out, r->D, e, true));
+  PADOC_TRY(check_apart(k, k_out, r->D, e, true));
+  PADOC_TRY(check_apart(k, q_out, r->D, e, false));
+  PADOC_TRY(check_apart(q, k_out, r->D, e, false));
+  PADOC_TRY(check_apart(q_out, k_out, r->D, e, false));
   PADOC_TRY(check_weight("q_weight", a->q_weight, e));
   PADOC_TRY(check_weight("k_weight", a->k_weight, e));
   return PADOC_OK;
@@ -135,15 +165,24 @@ padoc_status check_rotary_bwd(const padoc_rotary* r, const padoc_rotary_bwd_args
   PADOC_TRY(check_heads("dk_out", a->dk_out, n, Hkv, r->D, e, false));
   PADOC_TRY(check_heads("dq", a->dq, n, Hq, r->D, e, true));
   PADOC_TRY(check_heads("dk", a->dk, n, Hkv, r->D, e, true));
-  PADOC_TRY(check_apart("dq_out", a->dq_out, "dq", a->dq, n, Hq, r->D, e));
-  PADOC_TRY(check_apart("dk_out", a->dk_out, "dk", a->dk, n, Hkv, r->D, e));
+  const Rows dq_out{"dq_out", a->dq_out, n, Hq}, dk_out{"dk_out", a->dk_out, n, Hkv};
+  const Rows dq{"dq", a->dq, n, Hq}, dk{"dk", a->dk, n, Hkv};
+  PADOC_TRY(check_apart(dq_out, dq, r->D, e, true));
+  PADOC_TRY(check_apart(dk_out, dk, r->D, e, true));
+  PADOC_TRY(check_apart(dk_out, dq, r->D, e, false));
+  PADOC_TRY(check_apart(dq_out, dk, r->D, e, false));
+  PADOC_TRY(check_apart(dq, dk, r->D, e, false));
   if (a->q_weight) {
+    const Rows q{"q", a->q, n, Hq};
     PADOC_TRY(check_heads("q", a->q, n, Hq, r->D, e, false));
-    PADOC_TRY(check_apart("q", a->q, "dq", a->dq, n, Hq, r->D, e));
+    PADOC_TRY(check_apart(q, dq, r->D, e, true));
+    PADOC_TRY(check_apart(q, dk, r->D, e, false));
   }
   if (a->k_weight) {
+    const Rows k{"k", a->k, n, Hkv};
     PADOC_TRY(check_heads("k", a->k, n, Hkv, r->D, e, false));
-    PADOC_TRY(check_apart("k", a->k, "dk", a->dk, n, Hkv, r->D, e));
+    PADOC_TRY(check_apart(k, dk, r->D, e, true));
+    PADOC_TRY(check_apart(k, dq, r->D, e, false));
   }
   PADOC_TRY(check_weight("q_weight", a->q_weight, e));
   PADOC_TRY(check_weight("k_weight", a->k_weight, e));
@@ -165,9 +204,12 @@ padoc_status check_rotary_append(const padoc_rotary* r, const padoc_rotary_appen
                      (long long)a->n_new);
   PADOC_TRY(check_heads("q", a->q, a->n_q, Hq, r->D, e, false));
   PADOC_TRY(check_heads("q_out", a->q_out, a->n_q, Hq, r->D, e, true));
-  PADOC_TRY(check_apart("q", a->q, "q_out", a->q_out, a->n_q, Hq, r->D, e));
   PADOC_TRY(check_heads("k", a->k, a->n_new, Hkv, r->D, e, false));
   PADOC_TRY(check_heads("v", a->v, a->n_new, Hkv, r->D, e, false));
+  const Rows q_out{"q_out", a->q_out, a->n_q, Hq};
+  PADOC_TRY(check_apart(Rows{"q", a->q, a->n_q, Hq}, q_out, r->D, e, true));
+  PADOC_TRY(check_apart(Rows{"k", a->k, a->n_new, Hkv}, q_out, r->D, e, false));
+  PADOC_TRY(check_apart(Rows{"v", a->v, a->n_new, Hkv}, q_out, r->D, e, false));
   PADOC_TRY(check_weight("q_weight", a->q_weight, e));
   PADOC_TRY(check_weight("k_weight", a->k_weight, e));
   if (session) {

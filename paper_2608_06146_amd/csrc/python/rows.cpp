@@ -158,6 +158,7 @@ PyObject* rows_fwd(PyObject* self, PyObject* const* a, Py_ssize_t count) {
     const Rows* r = reinterpret_cast<Rows*>(self);
     const at::Tensor *q = tensor(a[0]), *k = tensor(a[1]);
     need(q || k);
+    need((q ? *q : *k).dim() == 3);
     const Where w(q ? *q : *k);
     padoc_rotary_fwd_args p{};
     p.n_rows = (q ? *q : *k).size(0);
@@ -190,6 +191,7 @@ PyObject* rows_bwd(PyObject* self, PyObject* const* a, Py_ssize_t count) {
     const at::Tensor* g[2] = {tensor(a[0]), tensor(a[1])};
     need(g[0] || g[1]);
     const at::Tensor& like = g[0] ? *g[0] : *g[1];
+    need(like.dim() == 3);
     const Where w(like);
     const bool grads = PyObject_IsTrue(a[9]) == 1;
     const int64_t n = like.size(0);

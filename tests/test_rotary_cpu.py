@@ -113,6 +113,9 @@ def test_forward_refused(rot, rot3):
     for qo in (heads(A + 2, 256, 64), heads(A, 128, 64), heads(A + 300, 256, 64), heads(A + 64, 256, 64), heads(A + 6, 64, 256)):
         assert fwd(rot, qo=qo) == _lib.ERR_ARG, qo
         assert "overlaps" in message()
+    # q_out in k, or in k_out
+    for kw in (dict(qo=heads(2 * A)), dict(ko=heads(A)), dict(ko=heads(3 * A + 64)), dict(n=1, qo=heads(2 * A, 0, 64))):
+        assert fwd(rot, **kw) == _lib.ERR_ARG and "overlaps" in message(), kw
     # axes: one after the other, at least the rows apart, or all the same
     assert fwd(rot3, pos_stride=3) == _lib.ERR_BOUNDS
     assert fwd(rot3, pos_stride=-4) == _lib.ERR_BOUNDS
@@ -126,7 +129,8 @@ def test_backward_refused(rot):
                        (dict(dk=heads(0)), _lib.ERR_ARG), (dict(dwq=A), _lib.ERR_ARG), (dict(wq=A, q=heads(0)), _lib.ERR_ARG),
                        (dict(wq=A, wk=A, dwq=A, dwk=A), _lib.ERR_ARG), (dict(wq=A, dwq=A + 2), _lib.ERR_ARG),
                        (dict(dq=heads(3 * A, 0, 64)), _lib.ERR_BOUNDS), (dict(dq=heads(5 * A + 2)), _lib.ERR_ARG),
-                       (dict(wq=A, dq=heads(A + 2)), _lib.ERR_ARG),
+                       (dict(wq=A, dq=heads(A + 2)), _lib.ERR_ARG), (dict(dq=heads(4 * A)), _lib.ERR_ARG),
+                       (dict(dk=heads(5 * A)), _lib.ERR_ARG), (dict(wk=A, dq=heads(2 * A)), _lib.ERR_ARG),
                        (dict(wq=A, dwq=A), _lib.ERR_WORKSPACE), (dict(wq=A, dwq=A, ws=256, nb=8), _lib.ERR_WORKSPACE),
                        (dict(wq=A, dwq=A, ws=128, nb=1 << 20), _lib.ERR_WORKSPACE)]:
         assert bwd(rot, **kw) == status, (kw, message())
@@ -147,7 +151,8 @@ def test_append_refused(rot):
                        (dict(v=heads(0)), _lib.ERR_ARG), (dict(qo=heads(0)), _lib.ERR_ARG), (dict(slots=0), _lib.ERR_ARG),
                        (dict(slots=A + 1), _lib.ERR_ARG), (dict(kc=0), _lib.ERR_ARG), (dict(vc=A + 8), _lib.ERR_ARG),
                        (dict(kc=2 * A), _lib.ERR_ARG), (dict(nb=-1), _lib.ERR_ARG), (dict(nb=2 ** 31), _lib.ERR_ARG),
-                       (dict(qo=heads(A + 2)), _lib.ERR_ARG), (dict(n_q=3, q_pos=A + 1), _lib.ERR_ARG)]:
+                       (dict(qo=heads(A + 2)), _lib.ERR_ARG), (dict(n_q=3, q_pos=A + 1), _lib.ERR_ARG),
+                       (dict(qo=heads(2 * A)), _lib.ERR_ARG), (dict(qo=heads(3 * A + 8)), _lib.ERR_ARG)]:
         assert append(rot, **kw) == status, (kw, message())
     assert append(rot, n=0, n_q=0, pos=0, slots=0, kc=0, vc=0, nb=0) == _lib.OK
 

@@ -159,6 +159,27 @@ def test_in_place_and_other_orders(dtype):
     check("dq in place", g, want, tol)
 
 
+@pytest.mark.parametrize("order", ["rows", "heads"])
+def test_in_place_beside_other_heads(order):
+    """q, k and v of a head side by side, rotated where they lie: the row and
+    head strides are the same for all three, and their extents overlap."""
+    st, n, h, d = Setup(64, "bf16"), 37, 5, 64
+    pos, wq, wk = positions(3, n, 1), normal((d,), 3, "bf16"), normal((d,), 4, "bf16")
+    buf = normal((n, h, 3, d) if order == "rows" else (h, 3, n, d), 5, "bf16")
+    q, k, v = (buf[:, :, i] for i in range(3)) if order == "rows" else (buf[:, i].transpose(0, 1) for i in range(3))
+    want, v0 = [st.forward(q, pos, wq), st.forward(k, pos, wk)], v.clone()
+    pa.rotary_fwd(q, k, pos, st.handle, wq, wk, q_out=q, k_out=k)
+    check("q", q, *want[0])
+    check("k", k, *want[1])
+    assert torch.equal(v, v0)
+    gq, gk = normal((n, h, d), 6, "bf16"), normal((n, h, d), 7, "bf16")
+    want = [st.backward(gq, q, pos, wq)[:2], st.backward(gk, k, pos, wk)[:2]]
+    pa.rotary_bwd(gq, gk, pos, st.handle, q, k, wq, wk, dq=q, dk=k)
+    check("dq", q, *want[0])
+    check("dk", k, *want[1])
+    assert torch.equal(v, v0)
+
+
 def test_the_forwards_rows_become_their_gradients():
     st, n, d = Setup(64, "bf16"), 50, 64
     x, g, w, pos = normal((n, 3, d), 1, "bf16"), normal((n, 3, d), 2, "bf16"), normal((d,), 3, "bf16"), positions(3, n, 4)
@@ -491,14 +512,14 @@ def _call(what="fwd", **kw):
 
 BAD = {  # argument: values that no call takes
     "q": [lambda t: t.float(), lambda t: t.cpu(), lambda t: t[:, :, :32], lambda t: t[:5], lambda t: t[0],
-          lambda t: torch.empty((64, 4, 6), dtype=t.dtype, device="cuda").permute(2, 1, 0)],
+          lambda t: torch.empty((64, 4, 6), dtype=t.dtype, device="cuda").permute(2, 1, 0), lambda t: t[0, 0, 0]],
     "k": [lambda t: t.float(), lambda t: t.cpu(), lambda t: t[:5]],
     "positions": [lambda t: t.long(), lambda t: t.cpu(), lambda t: t[:2], lambda t: t[:, :5], lambda t: t[0],
                   lambda t: torch.stack([t, t], -1)[..., 0]],
     "q_weight": [lambda t: t.float(), lambda t: t.cpu(), lambda t: t[:32], lambda t: torch.stack([t, t], -1)[:, 0]],
     "q_out": [lambda t: torch.empty((6, 4, 64), device="cuda"), lambda t: torch.empty((6, 3, 64), dtype=torch.bfloat16, device="cuda"),
               lambda t: torch.empty((6, 1, 64), dtype=torch.bfloat16, device="cuda").expand(6, 4, 64)],
-    "gq": [lambda t: t.float(), lambda t: t[:5]],
+    "gq": [lambda t: t.float(), lambda t: t[:5], lambda t: t[0, 0, 0]],
     "v": [lambda t: t.float(), lambda t: t[:5], lambda t: t[:, :1]],
     "slots": [lambda t: t.long(), lambda t: t[:5], lambda t: t.t().contiguous(), lambda t: t.cpu()],
     "kc": [lambda t: t.float(), lambda t: t[:2], lambda t: t.transpose(2, 3)],
