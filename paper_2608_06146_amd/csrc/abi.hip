@@ -429,7 +429,8 @@ extern "C" padoc_status padoc_rotary_bwd_workspace_bytes(const padoc_rotary* r, 
   if (n_rows < 0 || n_rows > INT32_MAX)
     return set_error(n_rows < 0 ? PADOC_ERR_ARG : PADOC_ERR_BOUNDS, "n_rows=%lld must be in [0, 2^31-1]",
                      (long long)n_rows);
-  *bytes = std::max<size_t>(256, rotary_bwd_parts(n_rows, num_heads_q, num_heads_kv, r->D, r->dtype == PADOC_BF16) * r->D * sizeof(float));
+  const size_t parts = rotary_bwd_parts(n_rows, num_heads_q, num_heads_kv, r->D, r->dtype == PADOC_BF16);
+  *bytes = std::max<size_t>(256, parts * r->D * sizeof(float));
   return PADOC_OK;
 }
 
@@ -440,7 +441,9 @@ extern "C" padoc_status padoc_rotary_bwd(const padoc_rotary* r, const padoc_rota
   if (st != PADOC_OK) return st;
   const bool sums = a->dq_weight || a->dk_weight;
   if (sums) {
-    const size_t need = rotary_bwd_parts(a->n_rows, a->num_heads_q, a->num_heads_kv, r->D, r->dtype == PADOC_BF16) * r->D * sizeof(float);
+    const size_t parts =
+        rotary_bwd_parts(a->n_rows, a->num_heads_q, a->num_heads_kv, r->D, r->dtype == PADOC_BF16);
+    const size_t need = parts * r->D * sizeof(float);
     if (!workspace) return set_error(PADOC_ERR_WORKSPACE, "workspace is null");
     if (((uintptr_t)workspace) & 255) return set_error(PADOC_ERR_WORKSPACE, "workspace must be 256-byte aligned");
     if (workspace_bytes < need)

@@ -136,7 +136,8 @@ padoc_status check_rotary_fwd(const padoc_rotary* r, const padoc_rotary_fwd_args
   PADOC_TRY(check_heads("k", a->k, n, Hkv, r->D, e, false));
   PADOC_TRY(check_heads("q_out", a->q_out, n, Hq, r->D, e, true));
   PADOC_TRY(check_heads("k_out", a->k_out, n, Hkv, r->D, e, true));
-  const Rows q{"q", a->q, n, Hq}, k{"k", a->k, n, Hkv}, q_out{"q_out", a->q_out, n, Hq}, k_out{"k_out", a->k_out, n, Hkv};
+  const Rows q{"q", a->q, n, Hq}, k{"k", a->k, n, Hkv};
+  const Rows q_out{"q_out", a->q_out, n, Hq}, k_out{"k_out", a->k_out, n, Hkv};
   PADOC_TRY(check_apart(q, q_out, r->D, e, true));
   PADOC_TRY(check_apart(k, k_out, r->D, e, true));
   PADOC_TRY(check_apart(k, q_out, r->D, e, false));
