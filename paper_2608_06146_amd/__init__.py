@@ -547,19 +547,27 @@ def _positions(name, pos, rotary, n, device):
     return pos.data_ptr(), rs if axes > 1 else 0
 
 
-def _launch(f, device, stream, made, *args):
-    """``f(*args, stream)`` on GPU ``device`` and ``stream`` (None: its current
-    one); tensors that the call ``made`` stay while a stream of the caller's
-    reads them."""
+def _on_stream(stream, device, call, *args):
+    """``call(*args)`` on ``stream`` of GPU ``device``.  What it allocates comes
+    from that stream's memory (a block that another stream let go of may still
+    be in use by the work queued there); what it returns also belongs to the
+    stream that was current, on which the caller reads it after a wait."""
     import torch
-    if stream is None:
-        s = torch._C._cuda_getCurrentRawStream(device)  # current_stream().cuda_stream, 1.7 us sooner
-    else:
-        if stream.device.index != device:
-            raise ValueError(f"the stream is on {stream.device}, the tensors on cuda:{device}")
-        for t in made:
-            t.record_stream(stream)
-        s = stream.cuda_stream
+    if stream.device.index != device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on cuda:{device}")
+    current = torch.cuda.current_stream(device)
+    with torch.cuda.stream(stream):
+        out = call(*args)
+    for t in out if isinstance(out, tuple) else (out,):
+        if t is not None and not any(t is a for a in args):
+            t.record_stream(current)
+    return out
+
+
+def _launch(f, device, *args):
+    """``f(*args, stream)`` on GPU ``device`` and its current stream."""
+    import torch
+    s = torch._C._cuda_getCurrentRawStream(device)  # current_stream().cuda_stream, 1.7 us sooner
     if device == torch._C._cuda_getDevice():
         _lib.check(f(*args, s))
     else:
@@ -573,7 +581,10 @@ def rotary_fwd(q, k, positions, rotary: Rotary, q_weight=None, k_weight=None, q_
     n]``; ``padoc_rotary_fwd``).  Rows and heads may be strided, as in slices
     of a fused projection; q or k may be None, and q_out / k_out may be q / k.
     Returns ``(q_out, k_out)``."""
-    if stream is None and rotary._rows is not None:
+    if stream is not None:
+        return _on_stream(stream, _rows_of(rotary, k if q is None else q)[0], rotary_fwd, q, k, positions, rotary, q_weight,
+                          k_weight, q_out, k_out)
+    if rotary._rows is not None:
         done = rotary._rows.fwd(q, k, positions, q_weight, k_weight, q_out, k_out)
         if done is not None:
             return done if type(done) is tuple else _lib.check(done)
@@ -582,14 +593,12 @@ def rotary_fwd(q, k, positions, rotary: Rotary, q_weight=None, k_weight=None, q_
     n, d = like.shape[0], rotary.head_dim
     hq = hk = 0
     q_in = q_to = k_in = k_to = _NO_HEADS
-    made = []
     if q is not None:
         hq = q.shape[1]
         shape = (n, hq, d)
         q_in = _heads("q", q, dt, device, shape)
         if q_out is None:
             q_out = q.new_empty(shape)
-            made.append(q_out)
             q_to = q_out.data_ptr(), hq * d, d
         else:
             q_to = _heads("q_out", q_out, dt, device, shape)
@@ -599,14 +608,13 @@ def rotary_fwd(q, k, positions, rotary: Rotary, q_weight=None, k_weight=None, q_
         k_in = _heads("k", k, dt, device, shape)
         if k_out is None:
             k_out = k.new_empty(shape)
-            made.append(k_out)
             k_to = k_out.data_ptr(), hk * d, d
         else:
             k_to = _heads("k_out", k_out, dt, device, shape)
     args = _lib.ROTARY_FWD_ARGS.pack(n, hq, hk, *_positions("positions", positions, rotary, n, device), *q_in, *k_in,
                                      *q_to, *k_to, _weight("q_weight", q_weight, dt, device, d),
                                      _weight("k_weight", k_weight, dt, device, d))
-    _launch(_lib.lib().padoc_rotary_fwd, device, stream, made, rotary.handle, args)
+    _launch(_lib.lib().padoc_rotary_fwd, device, rotary.handle, args)
     return (None if q is None else q_out), (None if k is None else k_out)
 
 
@@ -617,7 +625,10 @@ def rotary_bwd(dq_out, dk_out, positions, rotary: Rotary, q=None, k=None, q_weig
     weight).  Returns ``(dq, dk, dq_weight, dk_weight)``; the weights'
     gradients are float32 ``[d]``, None without a weight or with
     ``weight_grads=False``."""
-    if stream is None and rotary._rows is not None:
+    if stream is not None:
+        return _on_stream(stream, _rows_of(rotary, dk_out if dq_out is None else dq_out)[0], rotary_bwd, dq_out, dk_out,
+                          positions, rotary, q, k, q_weight, k_weight, dq, dk, weight_grads)
+    if rotary._rows is not None:
         done = rotary._rows.bwd(dq_out, dk_out, positions, q, k, q_weight, k_weight, dq, dk, weight_grads)
         if done is not None:
             return done if type(done) is tuple else _lib.check(done)
@@ -625,7 +636,7 @@ def rotary_bwd(dq_out, dk_out, positions, rotary: Rotary, q=None, k=None, q_weig
     like = dk_out if dq_out is None else dq_out
     device, dt = _rows_of(rotary, like)
     n, d = like.shape[0], rotary.head_dim
-    made, heads, counts, outs, ws, dws = [], [], [], [], [], []
+    heads, counts, outs, ws, dws = [], [], [], [], []
     for name, g, x, w, out in (("q", dq_out, q, q_weight, dq), ("k", dk_out, k, k_weight, dk)):
         if g is None:
             heads.append((_NO_HEADS,) * 3), counts.append(0), outs.append(None), ws.append(0), dws.append(None)
@@ -639,7 +650,6 @@ def rotary_bwd(dq_out, dk_out, positions, rotary: Rotary, q=None, k=None, q_weig
             x_in = _heads(name, x, dt, device, shape)
         if out is None:
             out = g.new_empty(shape)
-            made.append(out)
             to = out.data_ptr(), h * d, d
         else:
             to = _heads("d" + name, out, dt, device, shape)
@@ -653,16 +663,15 @@ def rotary_bwd(dq_out, dk_out, positions, rotary: Rotary, q=None, k=None, q_weig
         nb = C.c_size_t(0)
         _lib.check(L.padoc_rotary_bwd_workspace_bytes(handle, n, hq, hk, C.byref(nb)))
         work = like.new_empty(nb.value, dtype=torch.uint8)  # the allocator's blocks are 512-byte aligned
-        made.extend(t for t in (work, *dws) if t is not None)
         wptr, wbytes = work.data_ptr(), nb.value
     (xq, gq, oq), (xk, gk, ok) = heads
     args = _lib.ROTARY_BWD_ARGS.pack(n, hq, hk, *_positions("positions", positions, rotary, n, device), *xq, *xk, *gq,
                                      *gk, *oq, *ok, *ws, *(0 if t is None else t.data_ptr() for t in dws))
-    _launch(L.padoc_rotary_bwd, device, stream, made, handle, args, wptr, wbytes)
+    _launch(L.padoc_rotary_bwd, device, handle, args, wptr, wbytes)
     return outs[0], outs[1], dws[0], dws[1]
 
 
-def _append_args(rotary, q, k, v, positions, q_weight, k_weight, q_positions, q_out, made, slots=0, k_cache=0, v_cache=0,
+def _append_args(rotary, q, k, v, positions, q_weight, k_weight, q_positions, q_out, slots=0, k_cache=0, v_cache=0,
                  num_blocks=0):
     """The packed arguments of an append, its q_out and the GPU's index."""
     device, dt = _rows_of(rotary, q if k is None else k)
@@ -682,7 +691,6 @@ def _append_args(rotary, q, k, v, positions, q_weight, k_weight, q_positions, q_
         q_in = _heads("q", q, dt, device, shape)
         if q_out is None:
             q_out = q.new_empty(shape)
-            made.append(q_out)
             q_to = q_out.data_ptr(), hq * d, d
         else:
             q_to = _heads("q_out", q_out, dt, device, shape)
@@ -714,7 +722,10 @@ def rotary_append(q, k, v, positions, slots, k_cache, v_cache, rotary: Rotary, q
     caches (k normed and rotated) at ``slots`` (int32 ``[n_new, 2]``: block id
     and slot; a block id of -1 leaves the row out).  ``q_positions`` may be
     left out when query row i is new row i; q may be None.  Returns q_out."""
-    if stream is None and rotary._rows is not None:
+    if stream is not None:
+        return _on_stream(stream, _rows_of(rotary, q if k is None else k)[0], rotary_append, q, k, v, positions, slots,
+                          k_cache, v_cache, rotary, q_weight, k_weight, q_positions, q_out)
+    if rotary._rows is not None:
         done = rotary._rows.append(q, k, v, positions, slots, k_cache, v_cache, q_weight, k_weight, q_positions, q_out)
         if done is not None:
             return done[0] if type(done) is tuple else _lib.check(done)
@@ -728,10 +739,9 @@ def rotary_append(q, k, v, positions, slots, k_cache, v_cache, rotary: Rotary, q
     _check_tensor("slots", slots, torch.int32, dev)
     if slots.shape != (k.shape[0], 2):
         raise ValueError(f"slots has shape {tuple(slots.shape)}, expected {(k.shape[0], 2)}")
-    made = []
-    args, q_out, device = _append_args(rotary, q, k, v, positions, q_weight, k_weight, q_positions, q_out, made,
+    args, q_out, device = _append_args(rotary, q, k, v, positions, q_weight, k_weight, q_positions, q_out,
                                        slots.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), nb)
-    _launch(_lib.lib().padoc_rotary_append, device, stream, made, rotary.handle, args)
+    _launch(_lib.lib().padoc_rotary_append, device, rotary.handle, args)
     return q_out
 
 
@@ -747,7 +757,11 @@ def cache_copy_blocks(k_cache, v_cache, pairs, k_dst=None, v_dst=None, pairs_hos
     1]`` of the same caches, or of ``k_dst`` / ``v_dst``
     (``padoc_cache_copy_blocks``; int32 ``[n, 2]`` on the device, with an
     optional host copy that is only checked).  Returns the caches written."""
-    if stream is None and k_dst is None and v_dst is None and pairs_host is None:
+    if stream is not None:
+        if not k_cache.is_cuda:
+            raise ValueError(f"k_cache is on {k_cache.device}, expected a GPU")
+        return _on_stream(stream, k_cache.get_device(), cache_copy_blocks, k_cache, v_cache, pairs, k_dst, v_dst, pairs_host)
+    if k_dst is None and v_dst is None and pairs_host is None:
         done = _copy_blocks(k_cache, v_cache, pairs)
         if done is not None:
             if done:
@@ -776,7 +790,7 @@ def cache_copy_blocks(k_cache, v_cache, pairs, k_dst=None, v_dst=None, pairs_hos
         host = np.ascontiguousarray(pairs_host, dtype=np.int32)
         if host.shape != pairs.shape:
             raise ValueError(f"pairs_host has shape {host.shape}, expected {tuple(pairs.shape)}")
-    _launch(_lib.lib().padoc_cache_copy_blocks, dev.index, stream, (), k_cache.data_ptr(), v_cache.data_ptr(), nb,
+    _launch(_lib.lib().padoc_cache_copy_blocks, dev.index, k_cache.data_ptr(), v_cache.data_ptr(), nb,
             k_dst.data_ptr(), v_dst.data_ptr(), nd, pairs.data_ptr(), pairs.shape[0],
             None if host is None else host.ctypes.data, hkv, d, _lib.BF16 if dt == torch.bfloat16 else _lib.F32)
     return k_dst, v_dst
@@ -1033,6 +1047,9 @@ class DecodeSession:
         import torch
         if self.device is None:
             raise RuntimeError("host-only session: use commit()")
+        if stream is not None:
+            return _on_stream(stream, self.device.index, self.launch_rotary, q, k_new, v_new, positions, rotary, q_weight,
+                              k_weight, q_positions, q_rot, out, lse, workspace)
         n_q, n_kv = self.n_q_rows, self.n_kv_rows
         dt, dev = self.k_cache.dtype, self.device
         if _torch_dtype(rotary) != dt:
@@ -1050,13 +1067,10 @@ class DecodeSession:
                 raise TypeError("q must be a torch tensor")
             if tuple(q.shape) != (n_q, self.num_heads_q, self.head_dim):
                 raise ValueError(f"q must be [{n_q}, {self.num_heads_q}, {self.head_dim}]")
-        made = []
         if out is None:
             out = torch.empty(n_q, self.num_heads_q, self.head_dim, dtype=dt, device=dev)
-            made.append(out)
         if lse is None:
             lse = torch.empty(n_q, self.num_heads_q, dtype=torch.float32, device=dev)
-            made.append(lse)
         if n_q:
             _check_tensor("out", out, dt, dev)
             _check_tensor("lse", lse, torch.float32, dev)
@@ -1068,7 +1082,7 @@ class DecodeSession:
             raise ValueError(f"{n_q} query rows of {n_kv} new ones need q_positions")
         if n_q or n_kv:
             args, _, device = _append_args(rotary, q if n_q else None, k_new if n_kv else None, v_new, positions,
-                                             q_weight, k_weight, q_positions, q_rot, made)
+                                             q_weight, k_weight, q_positions, q_rot)
             if device != dev.index:
                 raise ValueError(f"rows are on cuda:{device}, expected {dev}")
         else:
@@ -1076,7 +1090,7 @@ class DecodeSession:
         # head counts are the session's also where a step has no rows of a kind
         args = args[:16] + struct.pack("=ii", self.num_heads_q, self.num_heads_kv) + args[24:]
         ws = self.workspace() if workspace is None else workspace
-        _launch(_lib.lib().padoc_session_launch_rotary, dev.index, stream, made, self.handle, rotary.handle, args,
+        _launch(_lib.lib().padoc_session_launch_rotary, dev.index, self.handle, rotary.handle, args,
                 out.data_ptr() if n_q else None, lse.data_ptr() if n_q else None, ws.data_ptr(), ws.numel())
         return out, lse
 

@@ -1,0 +1,55 @@
+"""Calls on a caller's stream while the current stream still works on memory that
+the program let go of: outputs and workspaces must not lie there."""
+import pytest
+import torch
+
+import paper_2608_06146_amd as pa
+from _rotary import Setup, normal, positions
+
+pytestmark = pytest.mark.gpu
+
+
+def leave(shapes, dtype):
+    """Tensors that the current stream writes some milliseconds from now, let go
+    of; returns their addresses."""
+    ts = [torch.empty(s, dtype=t, device="cuda") for s, t in zip(shapes, dtype)]
+    torch.cuda._sleep(2_000_000)
+    for t in ts:
+        t.fill_(7)
+    return {t.data_ptr() for t in ts}
+
+
+def rotary_calls():
+    st, n, hq, hkv, d = Setup(64, "bf16"), 3000, 8, 2, 64
+    q, k, v = normal((n, hq, d), 1, "bf16"), normal((n, hkv, d), 2, "bf16"), normal((n, hkv, d), 3, "bf16")
+    w, pos = normal((d,), 4, "bf16"), positions(3, n, 5)
+    nb = -(-n // 16)
+    t = torch.arange(n, dtype=torch.int32)
+    slots = torch.stack([t // 16, t % 16], 1).cuda()
+    kc, vc = torch.zeros((nb, hkv, d // 8, 16, 8), dtype=q.dtype, device="cuda"), torch.zeros((nb, hkv, d, 16), dtype=q.dtype, device="cuda")
+    return {"fwd": lambda s: pa.rotary_fwd(q, k, pos, st.handle, w, w, stream=s),
+            "bwd": lambda s: pa.rotary_bwd(q, k, pos, st.handle, q, k, w, w, stream=s),
+            "append": lambda s: (pa.rotary_append(q, k, v, pos, slots, kc, vc, st.handle, w, w, stream=s), kc, vc)}
+
+
+def on_a_busy_device(call):
+    """``call(side)`` beside queued work on memory of its outputs' sizes gives
+    what ``call(None)`` gives."""
+    want = [t.clone() for t in call(None)]
+    side = torch.cuda.Stream()
+    shapes, types = [t.shape for t in want], [t.dtype for t in want]
+    torch.cuda.synchronize()
+    for i in range(3):
+        print("[case] run", i, flush=True)
+        left = leave(shapes, types)
+        got = call(side)
+        assert not left & {t.data_ptr() for t in got}
+        side.synchronize()
+        torch.cuda.synchronize()  # the queued writes too
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        del got
+
+
+@pytest.mark.parametrize("what", ["fwd", "bwd", "append"])
+def test_rotary_calls(what):
+    on_a_busy_device(rotary_calls()[what])
