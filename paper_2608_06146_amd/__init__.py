@@ -855,6 +855,7 @@ class DecodeSession:
         self.n_kv_rows = self.n_q_rows = 0
         self.workspace_bytes = 0
         self._ws = None
+        self._users = set()  # streams of _keep
 
     @property
     def handle(self):
@@ -940,6 +941,7 @@ class DecodeSession:
                                                    None if k_cache is None else k_cache.data_ptr(),
                                                    None if v_cache is None else v_cache.data_ptr()))
         self.k_cache, self.v_cache, self.num_blocks = k_cache, v_cache, int(num_blocks)
+        self._users = set()
 
     def copies(self):
         """The prepared step's block copies: one ``[n, 2]`` array of (source,
@@ -998,7 +1000,21 @@ class DecodeSession:
             raw = torch.empty(cap + 256, dtype=torch.uint8, device=self.device)
             off = (-raw.data_ptr()) % 256
             self._ws = (self.device, raw, raw[off: off + cap])
+            self._users = set()
         return self._ws[2]
+
+    def _keep(self):
+        """What the session holds belongs to the current stream, too, on which a
+        step is about to use it: a workspace that the session outgrows, or caches
+        that it is moved from, stay until the steps queued there are done."""
+        import torch
+        raw = torch._C._cuda_getCurrentRawStream(self.device.index)
+        if raw in self._users:
+            return
+        s = torch.cuda.current_stream(self.device)
+        for t in (self.k_cache, self.v_cache, self.block_table) + (() if self._ws is None else (self._ws[1],)):
+            t.record_stream(s)
+        self._users.add(raw)
 
     def launch(self, q, k_new, v_new, out=None, lse=None, workspace=None, stream=None):
         """Run the prepared step; q ``[n_q_rows, Hq, d]``, k_new / v_new
@@ -1006,6 +1022,8 @@ class DecodeSession:
         import torch
         if self.device is None:
             raise RuntimeError("host-only session: use commit()")
+        if stream is not None:
+            return _on_stream(stream, self.device.index, self.launch, q, k_new, v_new, out, lse, workspace)
         dt = self.k_cache.dtype
         dev = self.device
         if self.n_kv_rows:
@@ -1026,7 +1044,8 @@ class DecodeSession:
             if tuple(out.shape) != tuple(q.shape) or tuple(lse.shape) != tuple(q.shape[:2]):
                 raise ValueError("out / lse shape does not match q")
         ws = self.workspace() if workspace is None else workspace
-        s = torch.cuda.current_stream(dev) if stream is None else stream
+        self._keep()
+        s = torch.cuda.current_stream(dev)
 
         def p(t, n):
             return _ptr(t) if n else None
@@ -1090,6 +1109,7 @@ class DecodeSession:
         # head counts are the session's also where a step has no rows of a kind
         args = args[:16] + struct.pack("=ii", self.num_heads_q, self.num_heads_kv) + args[24:]
         ws = self.workspace() if workspace is None else workspace
+        self._keep()
         _launch(_lib.lib().padoc_session_launch_rotary, dev.index, self.handle, rotary.handle, args,
                 out.data_ptr() if n_q else None, lse.data_ptr() if n_q else None, ws.data_ptr(), ws.numel())
         return out, lse

@@ -96,3 +96,41 @@ def test_a_sessions_rotary_launch_allocates_on_the_callers_stream(monkeypatch):
     out, made = sv.step("rotary", 5, sv.gpu.side)
     assert len(made) == 4 and all(t.allocated is sv.gpu.side for t in made)  # out, lse, rotated queries, workspace
     assert all(sv.gpu.first in t.recorded for t in out)
+
+
+@pytest.mark.parametrize("form", ["plain", "rotary"])
+def test_a_session_keeps_its_memory_for_the_steps_queued(monkeypatch, form):
+    """Steps on two streams, growing: whatever the session holds was allocated
+    on, or recorded for, every stream that a step ran on."""
+    sv = Serving(monkeypatch)
+    for _ in range(4):
+        sv.s.open()
+    held = []
+    for n, stream in ((1, None), (1, sv.gpu.side), (60, sv.gpu.side), (1, None), (80, None)):
+        sv.step(form, n, stream)
+        s = stream or sv.gpu.first
+        address = sv.seen[-1][5 if form == "rotary" else 6]
+        workspace = sv.gpu.holder(getattr(address, "value", address))
+        if not any(workspace is t for t in held):
+            held.append(workspace)
+        for t in (workspace, *sv.caches):
+            assert t.allocated is s or s in t.recorded
+    assert len(held) >= 2  # outgrown and replaced
+
+
+def test_caches_that_a_session_is_moved_from(monkeypatch):
+    sv = Serving(monkeypatch)
+    sv.s.open()
+    sv.step("rotary", 5, sv.gpu.side)
+    new = sv.t(50, 2, 8, 16, 8), sv.t(50, 2, 64, 16)
+    sv.s.resize(50, *new)
+    sv.step("rotary", 5, sv.gpu.side)
+    assert all(sv.gpu.side in t.recorded for t in (*sv.caches, *new))
+
+
+def test_a_plain_launch_allocates_on_the_callers_stream(monkeypatch):
+    sv = Serving(monkeypatch)
+    sv.s.open()
+    out, made = sv.step("plain", 5, sv.gpu.side)
+    assert len(made) == 3 and all(t.allocated is sv.gpu.side for t in made)  # out, lse, workspace
+    assert all(sv.gpu.first in t.recorded for t in out)

@@ -53,3 +53,41 @@ def on_a_busy_device(call):
 @pytest.mark.parametrize("what", ["fwd", "bwd", "append"])
 def test_rotary_calls(what):
     on_a_busy_device(rotary_calls()[what])
+
+
+@pytest.mark.parametrize("form", ["plain", "rotary"])
+def test_a_growing_session(form):
+    """Steps that outgrow the session's workspace on a stream of the caller's;
+    between them the current stream allocates and writes as much memory.  The
+    results are those of a twin that runs alone."""
+    hq, hkv, d, nb = 8, 2, 64, 700
+    st, w = Setup(d, "bf16"), normal((d,), 1, "bf16")
+
+    def session():
+        kc, vc = torch.zeros((nb, hkv, d // 8, 16, 8), dtype=torch.bfloat16, device="cuda"), torch.zeros((nb, hkv, d, 16), dtype=torch.bfloat16, device="cuda")
+        return pa.DecodeSession(hq, hkv, d, nb, "bf16", kc, vc, torch.zeros(4096, dtype=torch.int32, device="cuda"))
+
+    steps = [(1, 40), (3, 5), (20, 9), (64, 3), (64, 30)]  # streams, tokens of each
+    rows = [(normal((s * t, hq, d), i, "bf16"), normal((s * t, hkv, d), i + 20, "bf16"), positions(3, s * t, i)) for i, (s, t) in enumerate(steps)]
+
+    def run(stream):
+        s, out, sizes = session(), [], []
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream())
+        for (n, t), (q, k, pos) in zip(steps, rows):
+            while s.n_open < n:
+                s.open()
+            s.prepare([t] * n, [t] * n)
+            print("[case]", form, n, t, s.workspace_bytes, flush=True)
+            sizes.append(s.workspace_bytes)
+            out.append(s.launch_rotary(q, k, k, pos, st.handle, w, w, stream=stream) if form == "rotary" else s.launch(q, k, k, stream=stream))
+            if stream is not None:
+                for z in sizes:
+                    torch.full((z + z // 4 + 256,), 255, dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        assert max(sizes) > 2 * sizes[0]
+        return [t for o in out for t in o] + [s.k_cache, s.v_cache]
+
+    want = run(None)
+    got = run(torch.cuda.Stream())
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
