@@ -107,12 +107,31 @@ def tree_remaining(segments: np.ndarray, progress=None) -> np.ndarray:
     return out
 
 
+def _on_stream(stream, device, call, *args):
+    """``call(*args)`` on ``stream`` of GPU ``device``.  What it allocates comes
+    from that stream's memory (a block that another stream let go of may still
+    be in use by the work queued there); what it returns also belongs to the
+    stream that was current, on which the caller reads it after a wait."""
+    import torch
+    if stream.device.index != device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on cuda:{device}")
+    current = torch.cuda.current_stream(device)
+    with torch.cuda.stream(stream):
+        out = call(*args)
+    for t in out if isinstance(out, tuple) else (out,):
+        if t is not None and not any(t is a for a in args):
+            t.record_stream(current)
+    return out
+
+
 def cache_from_rows(k_rows, v_rows, k_cache=None, v_cache=None, stream=None):
     """Paged K/V blocks in row layout ``[num_blocks, Hkv, 16, d]`` rewritten
     into the library's paged layouts (``padoc_cache_from_rows``): K
     ``[num_blocks, Hkv, d/8, 16, 8]``, V ``[num_blocks, Hkv, d, 16]``, block
     for block.  Returns ``(k_cache, v_cache)`` (allocated when not given)."""
     import torch
+    if stream is not None:
+        return _on_stream(stream, k_rows.get_device(), cache_from_rows, k_rows, v_rows, k_cache, v_cache)
     if k_rows.dim() != 4 or k_rows.shape[2] != 16 or tuple(v_rows.shape) != tuple(k_rows.shape):
         raise ValueError("k_rows / v_rows must both be [num_blocks, Hkv, 16, d]")
     nb, hkv, _, d = k_rows.shape
@@ -130,7 +149,7 @@ def cache_from_rows(k_rows, v_rows, k_cache=None, v_cache=None, stream=None):
         _check_tensor(name, t, dt, dev)
         if tuple(t.shape) != shape:
             raise ValueError(f"{name} must be {shape}")
-    s = torch.cuda.current_stream(dev) if stream is None else stream
+    s = torch.cuda.current_stream(dev)
     _lib.check(_lib.lib().padoc_cache_from_rows(_ptr(k_rows), _ptr(v_rows), _ptr(k_cache), _ptr(v_cache), int(nb),
                                                 int(hkv), int(d), _lib.BF16 if dt == torch.bfloat16 else _lib.F32,
                                                 C.c_void_p(s.cuda_stream)))
@@ -202,22 +221,30 @@ class TreePlan:
 
     def backward_workspace(self, device):
         """A cached device workspace for the backward (256-byte aligned)."""
-        import torch
-        if getattr(self, "_bws", None) is None or self._bws[0] != torch.device(device):
-            nb = self.backward_workspace_bytes()
-            raw = torch.empty(nb + 256, dtype=torch.uint8, device=device)
-            off = (-raw.data_ptr()) % 256
-            self._bws = (torch.device(device), raw, raw[off: off + nb])
+        self._bws = _workspace(getattr(self, "_bws", None), self.backward_workspace_bytes(), device)
         return self._bws[2]
 
     def workspace(self, device):
         """A cached device workspace of the plan's size (256-byte aligned)."""
-        import torch
-        if self._ws is None or self._ws[0] != torch.device(device):
-            raw = torch.empty(self.workspace_bytes + 256, dtype=torch.uint8, device=device)
-            off = (-raw.data_ptr()) % 256
-            self._ws = (torch.device(device), raw, raw[off: off + self.workspace_bytes])
+        self._ws = _workspace(self._ws, self.workspace_bytes, device)
         return self._ws[2]
+
+
+def _workspace(held, nbytes, device):
+    """``(device, allocation, workspace, streams)``: ``held`` where it is on
+    ``device``, else a new one.  It belongs to the streams that were current when
+    it was asked for: a plan may go while work is queued on any of them."""
+    import torch
+    dev = torch.device(device)
+    if held is None or held[0] != dev:
+        raw = torch.empty(nbytes + 256, dtype=torch.uint8, device=dev)
+        off = (-raw.data_ptr()) % 256
+        held = (dev, raw, raw[off: off + nbytes], set())
+    s = torch._C._cuda_getCurrentRawStream(held[1].get_device()) if held[1].is_cuda else None
+    if s is not None and s not in held[3]:
+        held[1].record_stream(torch.cuda.current_stream(dev))  # (nothing, on the stream it was allocated on)
+        held[3].add(s)
+    return held
 
 
 def _carray(ptr, n, dt):
@@ -283,13 +310,15 @@ def tree_attn_fwd(q, k, v, plan: TreePlan, out=None, lse=None, workspace=None, s
     """Packed forward (``padoc_tree_attn_fwd``).  q ``[n_q, Hq, d]``; k, v
     ``[T, Hkv, d]``; returns ``(O [n_q, Hq, d], LSE [n_q, Hq] float32)``."""
     import torch
+    if stream is not None:
+        return _on_stream(stream, q.get_device(), tree_attn_fwd, q, k, v, plan, out, lse, workspace)
     dt = _torch_dtype(plan)
     dev = q.device
     for name, t in (("q", q), ("k", k), ("v", v)):
         _check_tensor(name, t, dt, dev)
     out, lse = _outputs(plan, q, out, lse)
     ws = plan.workspace(dev) if workspace is None else workspace
-    s = torch.cuda.current_stream(dev) if stream is None else stream
+    s = torch.cuda.current_stream(dev)
     _lib.check(_lib.lib().padoc_tree_attn_fwd(plan.handle, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse),
                                               _ptr(ws), ws.numel(), C.c_void_p(s.cuda_stream)))
     return out, lse
@@ -319,6 +348,8 @@ def branch_decode(q, k_cache, v_cache, block_table, plan: TreePlan, out=None, ls
         if args is not None:
             _lib.check(_lib.lib().padoc_branch_decode(*args))
             return out, lse
+    elif stream is not None:
+        return _on_stream(stream, q.get_device(), branch_decode, q, k_cache, v_cache, block_table, plan, out, lse, workspace)
     dt = _torch_dtype(plan)
     dev = q.device
     for name, t in (("q", q), ("k_cache", k_cache), ("v_cache", v_cache)):
@@ -400,6 +431,8 @@ def tree_attn_bwd(q, k, v, o, lse, dout, plan: TreePlan, dq=None, dk=None, dv=No
     q, o, dout ``[n_q, Hq, d]``; k, v ``[T, Hkv, d]``; lse float32 ``[n_q,
     Hq]`` (the forward's outputs); returns ``(dQ, dK, dV)``."""
     import torch
+    if stream is not None:
+        return _on_stream(stream, q.get_device(), tree_attn_bwd, q, k, v, o, lse, dout, plan, dq, dk, dv, workspace)
     dt = _torch_dtype(plan)
     dev = q.device
     for name, t in (("q", q), ("k", k), ("v", v), ("o", o), ("dout", dout)):
@@ -413,7 +446,7 @@ def tree_attn_bwd(q, k, v, o, lse, dout, plan: TreePlan, dq=None, dk=None, dv=No
         if t.shape != ref.shape:
             raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(ref.shape)}")
     ws = plan.backward_workspace(dev) if workspace is None else workspace
-    s = torch.cuda.current_stream(dev) if stream is None else stream
+    s = torch.cuda.current_stream(dev)
     _lib.check(_lib.lib().padoc_tree_attn_bwd(plan.handle, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(dout),
                                               _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws), ws.numel(),
                                               C.c_void_p(s.cuda_stream)))
@@ -545,23 +578,6 @@ def _positions(name, pos, rotary, n, device):
     if n > 1 and es != 1:
         raise ValueError(f"{name}: the positions of an axis must be contiguous")
     return pos.data_ptr(), rs if axes > 1 else 0
-
-
-def _on_stream(stream, device, call, *args):
-    """``call(*args)`` on ``stream`` of GPU ``device``.  What it allocates comes
-    from that stream's memory (a block that another stream let go of may still
-    be in use by the work queued there); what it returns also belongs to the
-    stream that was current, on which the caller reads it after a wait."""
-    import torch
-    if stream.device.index != device:
-        raise ValueError(f"the stream is on {stream.device}, the tensors on cuda:{device}")
-    current = torch.cuda.current_stream(device)
-    with torch.cuda.stream(stream):
-        out = call(*args)
-    for t in out if isinstance(out, tuple) else (out,):
-        if t is not None and not any(t is a for a in args):
-            t.record_stream(current)
-    return out
 
 
 def _launch(f, device, *args):

@@ -47,6 +47,7 @@ class Gpu:
         monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: gpu.current.cuda_stream)
         monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
         monkeypatch.setattr(torch, "empty", lambda *a, device=None, **kw: empty(*a, **kw) if device is None else self.tensor(empty(*a, **kw)))
+        monkeypatch.setattr(torch, "empty_like", lambda t: t.new_empty(t.shape))
 
     def tensor(self, t):
         x = torch.Tensor._make_subclass(Tensor, t)

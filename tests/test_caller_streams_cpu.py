@@ -134,3 +134,33 @@ def test_a_plain_launch_allocates_on_the_callers_stream(monkeypatch):
     out, made = sv.step("plain", 5, sv.gpu.side)
     assert len(made) == 3 and all(t.allocated is sv.gpu.side for t in made)  # out, lse, workspace
     assert all(sv.gpu.first in t.recorded for t in out)
+
+
+ATTENTION = ("padoc_tree_attn_fwd", "padoc_tree_attn_bwd", "padoc_branch_decode", "padoc_cache_from_rows")
+
+
+@pytest.mark.parametrize("what", ATTENTION)
+def test_attention_calls_allocate_on_the_callers_stream(monkeypatch, what):
+    seen = []
+    gpu = Gpu(monkeypatch, {n: lambda *a: seen.append(a) or 0 for n in ATTENTION})
+    t = lambda *shape, dtype=torch.bfloat16: gpu.tensor(torch.zeros(shape, dtype=dtype))  # noqa: E731
+    paged = what == "padoc_branch_decode"
+    segs = pa.segments_layout([(-1, 0, 20, 4)], 16 if paged else 0)
+    plan = pa.TreePlan(segs, 4, 2, 64, "bf16", 16 if paged else 0, num_kv_rows=2 if paged else 20,
+                       block_table_len=2 if paged else None)
+    n = plan.num_q_rows
+    q, lse, k, kc, vc, table = t(n, 4, 64), t(n, 4, dtype=torch.float32), t(20, 2, 64), t(2, 2, 8, 16, 8), t(2, 2, 64, 16), t(2, dtype=torch.int32)
+    rows = t(2, 2, 16, 64)
+    given = len(gpu.made)
+    out = {"padoc_tree_attn_fwd": lambda s: pa.tree_attn_fwd(q, k, k, plan, stream=s),
+           "padoc_tree_attn_bwd": lambda s: pa.tree_attn_bwd(q, k, k, q, lse, q, plan, stream=s),
+           "padoc_branch_decode": lambda s: pa.branch_decode(q, kc, vc, table, plan, stream=s),
+           "padoc_cache_from_rows": lambda s: pa.cache_from_rows(rows, rows, stream=s)}[what]
+    got = out(gpu.side)
+    made = gpu.made[given:]
+    assert made and all(m.allocated is gpu.side for m in made) and seen[0][-1].value == gpu.side.cuda_stream
+    assert all(gpu.first in m.recorded for m in got)
+    if what != "padoc_cache_from_rows":  # the plan's own workspace, used on another stream next
+        out(None)
+        assert sum(m.dtype == torch.uint8 for m in gpu.made) == 1
+        assert all(gpu.first in m.recorded for m in gpu.made if m.dtype == torch.uint8)

@@ -3,6 +3,7 @@ the program let go of: outputs and workspaces must not lie there."""
 import pytest
 import torch
 
+import padoc_synth as syn
 import paper_2608_06146_amd as pa
 from _rotary import Setup, normal, positions
 
@@ -91,3 +92,28 @@ def test_a_growing_session(form):
     want = run(None)
     got = run(torch.cuda.Stream())
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def attention_calls():
+    hq, hkv, d = 8, 2, 64
+    pages = [syn.Page(150, 150, 40, 40, (syn.Branch(7, 90, 90), syn.Branch(25, 45, 45)))] * 3
+    n = syn.count_tokens(pages)
+    plan = pa.TreePlan(pa.segments_from_pages(pages, 0), hq, hkv, d, "bf16", 0, num_kv_rows=n, num_q_rows=n)
+    q, k, v, g = normal((n, hq, d), 1, "bf16"), normal((n, hkv, d), 2, "bf16"), normal((n, hkv, d), 3, "bf16"), normal((n, hq, d), 4, "bf16")
+    o, lse = pa.tree_attn_fwd(q, k, v, plan)
+    lens = [33, 70, 5]
+    segs = pa.segments_layout([(-1, 0, t, 1) for t in lens], 16)
+    nb = sum(-(-t // 16) for t in lens)
+    decode = pa.TreePlan(segs, hq, hkv, d, "bf16", 16, num_kv_rows=nb, block_table_len=nb)
+    rows = normal((nb, hkv, 16, d), 5, "bf16")
+    kc, vc = pa.cache_from_rows(rows, rows)
+    table = torch.arange(nb, dtype=torch.int32, device="cuda")
+    return {"forward": lambda s: pa.tree_attn_fwd(q, k, v, plan, stream=s),
+            "backward": lambda s: pa.tree_attn_bwd(q, k, v, o, lse, g, plan, stream=s),
+            "decode": lambda s: pa.branch_decode(q[:3], kc, vc, table, decode, stream=s),
+            "cache": lambda s: pa.cache_from_rows(rows, rows, stream=s)}
+
+
+@pytest.mark.parametrize("what", ["forward", "backward", "decode", "cache"])
+def test_attention_calls(what):
+    on_a_busy_device(attention_calls()[what])
