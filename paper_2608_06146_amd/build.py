@@ -20,6 +20,7 @@ import shutil
 import subprocess
 import sys
 import sysconfig
+import warnings
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -104,13 +105,16 @@ def _compile_streams(cc: str, out: str) -> bool:
 
 
 def _compile_rows(cc: str, out: str, force: bool) -> bool:
-    """``_rows`` into file `out`; False where there are no Python or PyTorch
-    headers."""
+    """``_rows`` into file `out`; False where there are no Python headers or no
+    PyTorch headers and libraries for ROCm, and, with a warning, where this
+    PyTorch's do not compile or link (the package works without the module)."""
     inc = sysconfig.get_paths()["include"]
     spec = importlib.util.find_spec("torch")
     torch_dir = spec.submodule_search_locations[0] if spec and spec.submodule_search_locations else ""
-    if not os.path.exists(os.path.join(inc, "Python.h")) or \
-            not os.path.exists(os.path.join(torch_dir, "include", "torch", "csrc", "autograd", "python_variable.h")):
+    needs = [os.path.join(inc, "Python.h")] + [os.path.join(torch_dir, *p.split("/")) for p in
+                                               ("include/torch/csrc/autograd/python_variable.h",
+                                                "include/c10/hip/HIPStream.h", "lib/libc10_hip.so")]
+    if not all(os.path.exists(p) for p in needs):
         return False
     src = os.path.join(PKG, ROWS_SOURCE)
     paths = [inc, os.path.join(ROOT, "include"), os.path.join(torch_dir, "include"),
@@ -126,7 +130,8 @@ def _compile_rows(cc: str, out: str, force: bool) -> bool:
     if force or not os.path.exists(kept):
         r = subprocess.run(cmd + ["-o", kept + ".tmp", src] + libs, capture_output=True, text=True)
         if r.returncode != 0:
-            raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+            warnings.warn(f"the module _rows is left out, its compile failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+            return False
         os.replace(kept + ".tmp", kept)
     shutil.copyfile(kept, out)
     return True
