@@ -229,11 +229,12 @@ def native_rows():
     """The module ``_rows``, or None where it is not built for this interpreter
     and this PyTorch."""
     try:
-        import torch  # noqa: F401  (whose libraries the module needs)
+        import torch  # whose libraries the module needs
         from . import _rows
     except ImportError:
         return None
-    return _rows
+    # (another's tensors may be laid out otherwise)
+    return _rows if getattr(_rows, "torch_version", None) == str(torch.__version__) else None
 
 
 def rows(handle, head_dim: int, n_axes: int, bf16: bool):

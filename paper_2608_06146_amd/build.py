@@ -16,6 +16,7 @@ import concurrent.futures as cf
 import hashlib
 import importlib.util
 import os
+import re
 import shutil
 import subprocess
 import sys
@@ -122,9 +123,10 @@ def _compile_rows(cc: str, out: str, force: bool) -> bool:
     cmd = [cc, "-O2", "-std=c++17", "-fPIC", "-Wall", "-shared", "-no-hip-rt", "-DUSE_ROCM", "-D__HIP_PLATFORM_AMD__"]
     cmd += [x for i in paths for x in ("-isystem", i)]
     libs = ["-L", os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"]
-    with open(os.path.join(torch_dir, "version.py"), "rb") as f:
-        version = f.read()
-    tag = hashlib.sha256(version + " ".join(cmd + libs).encode() +
+    with open(os.path.join(torch_dir, "version.py")) as f:
+        version = re.search(r"^__version__ *= *['\"]([^'\"]+)", f.read(), re.M)
+    cmd.append(f'-DPADOC_TORCH_VERSION="{version.group(1) if version else ""}"')  # the module is for this one
+    tag = hashlib.sha256(" ".join(cmd + libs).encode() +
                          _digest([src, os.path.join(ROOT, "include", "padoc_attn.h")]).encode()).hexdigest()[:16]
     kept = os.path.join(BUILD, f"rows.{tag}.so")
     if force or not os.path.exists(kept):

@@ -368,5 +368,9 @@ PyMODINIT_FUNC PyInit__rows() {
     Py_DECREF(m);
     return nullptr;
   }
+  if (PyModule_AddStringConstant(m, "torch_version", PADOC_TORCH_VERSION) < 0) {
+    Py_DECREF(m);
+    return nullptr;
+  }
   return m;
 }

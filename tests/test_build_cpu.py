@@ -3,8 +3,9 @@ import os
 from types import SimpleNamespace
 
 import pytest
+import torch
 
-from paper_2608_06146_amd import build
+from paper_2608_06146_amd import _lib, build
 
 HEADER = "include/torch/csrc/autograd/python_variable.h"
 ROCM = ["include/c10/hip/HIPStream.h", "lib/libc10_hip.so"]
@@ -34,3 +35,10 @@ def test_a_pytorch_whose_headers_do_not_compile(monkeypatch, tmp_path):
     with pytest.warns(UserWarning, match="_rows is left out"):
         assert build._compile_rows(build.hipcc(), str(out), force=True) is False
     assert not out.exists() and not [f for f in os.listdir(tmp_path) if f.startswith("rows.")]
+
+
+def test_a_module_of_another_pytorch_is_not_used(monkeypatch):
+    rows = _lib.native_rows()
+    assert rows is not None and rows.torch_version == torch.__version__
+    monkeypatch.setattr(torch, "__version__", "2.0.0+other")
+    assert _lib.native_rows() is None
