@@ -60,10 +60,12 @@ struct Where {
   }
 };
 
-padoc_heads heads(const at::Tensor& t, const Rows* r, const Where& w, int64_t n, int64_t h) {
+// (What is written is no longer shared with a lazy clone: data_ptr.)
+padoc_heads heads(const at::Tensor& t, const Rows* r, const Where& w, int64_t n, int64_t h, bool written = false) {
   need(t.device() == w.device && t.scalar_type() == r->dtype && t.dim() == 3 && t.size(0) == n && t.size(1) == h &&
        t.size(2) == r->d && t.stride(2) == 1);
-  return padoc_heads{const_cast<void*>(t.const_data_ptr()), t.stride(0), t.stride(1)};
+  void* data = written ? t.data_ptr() : const_cast<void*>(t.const_data_ptr());
+  return padoc_heads{data, t.stride(0), t.stride(1)};
 }
 
 const void* weight(const at::Tensor* t, const Rows* r, const Where& w) {
@@ -117,7 +119,7 @@ Out out_rows(PyObject* given, const at::Tensor& like, const Rows* r, const Where
   Out o;
   if (given != Py_None) {
     o.given = given;
-    o.at = heads(*tensor(given), r, w, n, h);
+    o.at = heads(*tensor(given), r, w, n, h, /*written=*/true);
   } else {
     o.made = at::empty({n, h, r->d}, like.options());
     o.at = padoc_heads{o.made.data_ptr(), h * r->d, r->d};
