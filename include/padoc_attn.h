@@ -691,7 +691,7 @@ padoc_status padoc_session_compact(padoc_session* session, int32_t max_moves, in
 /* Change the pool to num_blocks blocks, in caches k_cache / v_cache that hold
    the present blocks at their ids (a shorter view of the same buffers after a
    compaction, or larger buffers the caller copied them to; NULL both for a
-   host-only session).  PADOC_ERR_BOUNDS when a kept block does not fit;
+   host-only session, and allowed for 0 blocks).  PADOC_ERR_BOUNDS when a kept block does not fit;
    PADOC_ERR_MODE while a compaction's copies wait for their launch, or
    between a prepare and its launch. */
 padoc_status padoc_session_resize(padoc_session* session, int64_t num_blocks, void* k_cache, void* v_cache);

@@ -604,7 +604,7 @@ padoc_status launch_step(padoc_session* s, const void* q, const void* k_new, con
   if (!s) return set_error(PADOC_ERR_ARG, "session is null");
   if (!s->prepared) return set_error(PADOC_ERR_MODE, "no step is prepared");
   const padoc_session_desc& d = s->desc;
-  if (!d.k_cache || !d.v_cache || !d.block_table)
+  if (!d.block_table || (d.num_blocks > 0 && (!d.k_cache || !d.v_cache)))
     return set_error(PADOC_ERR_ARG, "the session was created without device caches and block table");
   if (((uintptr_t)d.k_cache | (uintptr_t)d.v_cache) & 15)
     return set_error(PADOC_ERR_ARG, "the caches must be 16-byte aligned");

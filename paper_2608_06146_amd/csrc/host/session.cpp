@@ -385,7 +385,12 @@ extern "C" padoc_status padoc_session_resize(padoc_session* s, int64_t num_block
     return set_error(PADOC_ERR_ARG, "num_blocks=%lld must be in [0, 2^31-1]", (long long)num_blocks);
   if (!s->pending_copies.empty())
     return set_error(PADOC_ERR_MODE, "block copies wait for the launch of a step");
-  if ((k_cache != nullptr) != (s->desc.k_cache != nullptr) || (v_cache != nullptr) != (s->desc.v_cache != nullptr))
+  // (caches of no blocks may have no address)
+  const bool emptied = s->desc.num_blocks == 0 && s->desc.block_table;
+  const auto fits = [&](const void* now, const void* was) {
+    return now ? was || emptied : !was || num_blocks == 0;
+  };
+  if (!fits(k_cache, s->desc.k_cache) || !fits(v_cache, s->desc.v_cache))
     return set_error(PADOC_ERR_ARG, "a session has device caches or none, from its creation on");
   const int64_t old = s->desc.num_blocks;
   for (int64_t b = num_blocks; b < old; ++b)

@@ -290,3 +290,20 @@ def test_random_runs(seed):
                 r.close(i)
             r.step([0] * len(r.open))
     assert refused > 0
+
+
+def test_a_pool_emptied_and_filled_again():
+    """Caches of no blocks have no address: tensors of no elements."""
+    import ctypes as C
+    L, A = _lib.lib(), 1 << 20
+    h = C.c_void_p()
+    d = _lib.SessionDesc(4, 2, 64, 0.125, _lib.BF16, 8, 64, A, 2 * A, 3 * A, 0, 0)
+    assert L.padoc_session_create(C.byref(d), C.byref(h)) == _lib.OK
+    for n, k, v, want in ((4, A, 2 * A, _lib.OK), (4, None, None, _lib.ERR_ARG), (4, A, None, _lib.ERR_ARG), (0, None, None, _lib.OK),
+                          (0, None, None, _lib.OK), (5, 4 * A, 5 * A, _lib.OK), (5, None, 5 * A, _lib.ERR_ARG), (0, 4 * A, 5 * A, _lib.OK)):
+        assert L.padoc_session_resize(h, n, k, v) == want, (n, k, v)
+    L.padoc_session_destroy(h)
+    s = pa.DecodeSession(4, 2, 64, 8)  # host only: none, whatever the pool
+    for n in (0, 3):
+        assert L.padoc_session_resize(s.handle, n, None, None) == _lib.OK
+        assert L.padoc_session_resize(s.handle, n, A, 2 * A) == _lib.ERR_ARG
