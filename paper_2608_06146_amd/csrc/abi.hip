@@ -368,7 +368,6 @@ RotaryParams rotary_params(const padoc_rotary* r, int64_t n, int32_t Hq, int32_t
   p.table = r->table;
   p.pos = pos;
   p.pos_stride = pos_stride;
-  p.n_axes = r->n_axes;
   p.pairs = r->pairs;
   p.scale = r->scale;
   p.eps = r->eps;

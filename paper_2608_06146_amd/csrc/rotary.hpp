@@ -32,7 +32,7 @@ struct RotaryParams {
   RotaryTable table;
   const int32_t* pos;  // [n_axes][stride]
   int64_t pos_stride;
-  int32_t n_axes, pairs;  // pairs: rotary_dim / 2
+  int32_t pairs;  // rotary_dim / 2
   float scale, eps;
   int32_t inverse;  // rotate by the negative angle
   int32_t n, n_q;   // rows of k (and v), of q
