@@ -195,7 +195,8 @@ PyObject* rows_bwd(PyObject* self, PyObject* const* a, Py_ssize_t count) {
     const at::Tensor& like = g[0] ? *g[0] : *g[1];
     need(like.dim() == 3);
     const Where w(like);
-    const bool grads = PyObject_IsTrue(a[9]) == 1;
+    const int grads = PyObject_IsTrue(a[9]);
+    if (grads < 0) return nullptr;
     const int64_t n = like.size(0);
     int64_t h[2] = {0, 0};
     padoc_heads in[2]{}, x[2]{}, to[2]{};

@@ -562,3 +562,10 @@ def test_a_closed_handle_is_refused():
     for what in USED:
         with pytest.raises(ValueError, match="closed"):
             _call(what, st=st)
+
+
+def test_a_flag_without_a_truth_value():
+    st = Setup(64, "bf16")
+    q, w, pos = normal((6, 4, 64), 1, "bf16"), normal((64,), 2, "bf16"), positions(3, 6, 3)
+    with pytest.raises(RuntimeError, match="ambiguous"):
+        pa.rotary_bwd(q, None, pos, st.handle, q, None, w, weight_grads=torch.ones(2))
