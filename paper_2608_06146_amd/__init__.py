@@ -1,7 +1,9 @@
 """PaDoc tree attention on MI355X: thin Python binding of ``libpadoc_attn``.
 
 Every step of the computation runs in the HIP library; this module only
-marshals arguments.  PyTorch provides device memory and the current stream.
+marshals arguments.  PyTorch provides device memory and the current stream; a
+call's ``stream`` is where it runs instead (its inputs have to be ready there, its
+results are read elsewhere after a wait).
 
     segs = segments_from_pages(pages, block_size=0)        # tree -> segments
     plan = TreePlan(segs, Hq, Hkv, d, "bf16", block_size=0,
@@ -116,8 +118,15 @@ def _on_stream(stream, device, call, *args):
     if stream.device.index != device:
         raise ValueError(f"the stream is on {stream.device}, the tensors on cuda:{device}")
     current = torch.cuda.current_stream(device)
-    with torch.cuda.stream(stream):
-        out = call(*args)
+    if device == torch._C._cuda_getDevice():  # torch.cuda.stream(stream), 3 us sooner
+        torch.cuda.set_stream(stream)
+        try:
+            out = call(*args)
+        finally:
+            torch.cuda.set_stream(current)
+    else:
+        with torch.cuda.stream(stream):
+            out = call(*args)
     for t in out if isinstance(out, tuple) else (out,):
         if t is not None and not any(t is a for a in args):
             t.record_stream(current)
@@ -130,7 +139,7 @@ def cache_from_rows(k_rows, v_rows, k_cache=None, v_cache=None, stream=None):
     ``[num_blocks, Hkv, d/8, 16, 8]``, V ``[num_blocks, Hkv, d, 16]``, block
     for block.  Returns ``(k_cache, v_cache)`` (allocated when not given)."""
     import torch
-    if stream is not None:
+    if stream is not None and (k_cache is None or v_cache is None):
         return _on_stream(stream, k_rows.get_device(), cache_from_rows, k_rows, v_rows, k_cache, v_cache)
     if k_rows.dim() != 4 or k_rows.shape[2] != 16 or tuple(v_rows.shape) != tuple(k_rows.shape):
         raise ValueError("k_rows / v_rows must both be [num_blocks, Hkv, 16, d]")
@@ -149,7 +158,7 @@ def cache_from_rows(k_rows, v_rows, k_cache=None, v_cache=None, stream=None):
         _check_tensor(name, t, dt, dev)
         if tuple(t.shape) != shape:
             raise ValueError(f"{name} must be {shape}")
-    s = torch.cuda.current_stream(dev)
+    s = torch.cuda.current_stream(dev) if stream is None else stream
     _lib.check(_lib.lib().padoc_cache_from_rows(_ptr(k_rows), _ptr(v_rows), _ptr(k_cache), _ptr(v_cache), int(nb),
                                                 int(hkv), int(d), _lib.BF16 if dt == torch.bfloat16 else _lib.F32,
                                                 C.c_void_p(s.cuda_stream)))
@@ -310,7 +319,7 @@ def tree_attn_fwd(q, k, v, plan: TreePlan, out=None, lse=None, workspace=None, s
     """Packed forward (``padoc_tree_attn_fwd``).  q ``[n_q, Hq, d]``; k, v
     ``[T, Hkv, d]``; returns ``(O [n_q, Hq, d], LSE [n_q, Hq] float32)``."""
     import torch
-    if stream is not None:
+    if stream is not None and any(t is None for t in (out, lse, workspace)):
         return _on_stream(stream, q.get_device(), tree_attn_fwd, q, k, v, plan, out, lse, workspace)
     dt = _torch_dtype(plan)
     dev = q.device
@@ -318,7 +327,7 @@ def tree_attn_fwd(q, k, v, plan: TreePlan, out=None, lse=None, workspace=None, s
         _check_tensor(name, t, dt, dev)
     out, lse = _outputs(plan, q, out, lse)
     ws = plan.workspace(dev) if workspace is None else workspace
-    s = torch.cuda.current_stream(dev)
+    s = torch.cuda.current_stream(dev) if stream is None else stream
     _lib.check(_lib.lib().padoc_tree_attn_fwd(plan.handle, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse),
                                               _ptr(ws), ws.numel(), C.c_void_p(s.cuda_stream)))
     return out, lse
@@ -431,7 +440,7 @@ def tree_attn_bwd(q, k, v, o, lse, dout, plan: TreePlan, dq=None, dk=None, dv=No
     q, o, dout ``[n_q, Hq, d]``; k, v ``[T, Hkv, d]``; lse float32 ``[n_q,
     Hq]`` (the forward's outputs); returns ``(dQ, dK, dV)``."""
     import torch
-    if stream is not None:
+    if stream is not None and any(t is None for t in (dq, dk, dv, workspace)):
         return _on_stream(stream, q.get_device(), tree_attn_bwd, q, k, v, o, lse, dout, plan, dq, dk, dv, workspace)
     dt = _torch_dtype(plan)
     dev = q.device
@@ -446,7 +455,7 @@ def tree_attn_bwd(q, k, v, o, lse, dout, plan: TreePlan, dq=None, dk=None, dv=No
         if t.shape != ref.shape:
             raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(ref.shape)}")
     ws = plan.backward_workspace(dev) if workspace is None else workspace
-    s = torch.cuda.current_stream(dev)
+    s = torch.cuda.current_stream(dev) if stream is None else stream
     _lib.check(_lib.lib().padoc_tree_attn_bwd(plan.handle, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(dout),
                                               _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws), ws.numel(),
                                               C.c_void_p(s.cuda_stream)))

@@ -43,6 +43,7 @@ class Gpu:
         monkeypatch.setattr(_lib, "native_rows", lambda: None)
         monkeypatch.setattr(pa, "_copy_blocks", lambda *a: None)
         monkeypatch.setattr(torch.cuda, "stream", On)
+        monkeypatch.setattr(torch.cuda, "set_stream", lambda s: setattr(gpu, "current", s))
         monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: gpu.current)
         monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: gpu.current.cuda_stream)
         monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)

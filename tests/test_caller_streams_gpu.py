@@ -117,3 +117,40 @@ def attention_calls():
 @pytest.mark.parametrize("what", ["forward", "backward", "decode", "cache"])
 def test_attention_calls(what):
     on_a_busy_device(attention_calls()[what])
+
+
+def test_captured_on_a_forked_stream():
+    """Calls on a stream that a capture forked to, replayed with the program's
+    own work between."""
+    st, n, d = Setup(64, "bf16"), 700, 64
+    q, w, pos = normal((n, 8, d), 1, "bf16"), normal((d,), 2, "bf16"), positions(3, n, 3)
+    run = lambda s: [*pa.rotary_fwd(q, None, pos, st.handle, w, stream=s)[:1], *pa.rotary_bwd(q, None, pos, st.handle, q, None, w, stream=s)[::2]]  # noqa: E731
+    run(None)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        got = run(side)
+        torch.cuda.current_stream().wait_stream(side)
+    for i in range(4):
+        q.copy_(normal((n, 8, d), 10 + i, "bf16"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, run(None))), i
+
+
+def test_given_outputs_on_a_stream():
+    """Attention with every buffer the caller's."""
+    hq, hkv, d, n = 8, 2, 64, 150
+    plan = pa.TreePlan(pa.segments_layout([(-1, 0, n, n)], 0), hq, hkv, d, "bf16", 0, num_kv_rows=n, num_q_rows=n)
+    q, k = normal((n, hq, d), 1, "bf16"), normal((n, hkv, d), 2, "bf16")
+    o, lse = pa.tree_attn_fwd(q, k, k, plan)
+    grads = pa.tree_attn_bwd(q, k, k, o, lse, q, plan)
+    out, l2, g2 = torch.zeros_like(o), torch.zeros_like(lse), [torch.zeros_like(t) for t in grads]
+    ws, bws = plan.workspace("cuda"), plan.backward_workspace("cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    pa.tree_attn_fwd(q, k, k, plan, out, l2, ws, stream=side)
+    pa.tree_attn_bwd(q, k, k, out, l2, q, plan, *g2, bws, stream=side)
+    side.synchronize()
+    assert torch.equal(o, out) and torch.equal(lse, l2) and all(torch.equal(a, b) for a, b in zip(grads, g2))
