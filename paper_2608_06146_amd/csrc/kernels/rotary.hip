@@ -263,8 +263,8 @@ __device__ __forceinline__ const T* head_row(const padoc_heads& x, int64_t row, 
   return static_cast<const T*>(x.data) + row * x.row_stride + h * x.head_stride;
 }
 
-// Rows that a lane has in flight at once (4: more registers, 67.7 us where 2
-// take 65.9).
+// Rows that a lane has in flight at once.  Measured, 18 heads of 128: 43,067 rows
+// in bf16 69.9 us (74.4 with 4), 20,000 in fp32 67.5 (71.1).
 constexpr int kAhead = 2;
 
 // A tile of one tensor (q's or k's) as a workgroup sees it.
@@ -368,7 +368,12 @@ __global__ __launch_bounds__(kThreads) void rotary_fwd_kernel(const RotaryParams
   }
 }
 
-// Workgroups of the backward that a compute unit holds (by their registers).
+// Workgroups of the backward for a compute unit: its launch bound, and how many
+// items a unit gets of a long call.  (Its registers would let more run at once:
+// 84 of them in bf16, d = 128, so five.)  Measured with items for 2, 3, 4 and 5
+// workgroups a unit, 18 heads: 43,067 rows of 128 in bf16 120.7, 112.4, 117.9 and
+// 117.9 us; 40,000 of 64 in bf16 78.8, 60.5, 59.2 and 59.5; 20,000 of 128 in fp32
+// 115.0, 106.8, 110.5 and 110.5.
 constexpr int bwd_per_unit(int D, bool bf16) { return D == 64 ? 4 : bf16 ? 3 : 2; }
 
 // Backward: dx of an item's tiles, and the weight's gradient over them (fp32):
@@ -679,10 +684,12 @@ bool streams(int64_t rows, int D, bool bf16) { return rows * D * (bf16 ? 2 : 4) 
 
 dim3 grid_of(int64_t items) { return dim3((unsigned)std::min(items, kMaxGrid)); }
 
-// The backward's items.  A short call is cut into as many as half fill the chip
-// (the sums at their ends then weigh less: 3,479 rows of 18 heads 22.8 us a call
-// in 1,024 tiles, 20.1 in 384); a long one into as many as it holds at once, each
-// of them some tiles, with their D sums left once.
+// The backward's items.  A short call is cut into about 384 tiles, an item each
+// (the sums at their ends then weigh less than in more of them), a long one into
+// as many items as above, each of them some tiles, with their D sums left once.
+// Measured for 384, 512, 768 and 1,024 tiles, 18 heads of 128 in bf16: 3,479 rows
+// 18.3, 18.1, 16.3 and 21.0 us a call, 8,000 26.3, 26.3, 27.6 and 27.1; 3,479 in
+// fp32 24.4, 25.4, 24.6 and 25.3.
 constexpr int kComputeUnits = 256;
 void bwd_grids(int64_t n, int Hq, int Hkv, int D, bool bf16, TileGrid& q, TileGrid& k) {
   q = tile_grid(n, Hq, Hq + Hkv, 8, kComputeUnits * 3 / 2);
@@ -731,10 +738,14 @@ hipError_t launch_rotary_bwd(RotaryParams p, int D, bool bf16, bool pairs, float
 hipError_t launch_rotary_append(RotaryParams p, int D, bool bf16, bool pairs, hipStream_t s) {
   p.tiles_q = tile_grid(p.n_q, p.Hq, p.Hq + p.Hkv, 4, 4 * kComputeUnits);
   p.tiles_k = tile_grid(p.n, p.Hkv, p.Hq + p.Hkv, 4, 4 * kComputeUnits);
-  // V rows of a workgroup: 64 of many (whole runs of a prefill together), 8 of
-  // few (a decode step's scattered rows).  Measured, bf16, d = 128, 2 KV heads:
-  // 4,000 rows in runs 12.0 us a call (15.8 in eights), 20,000 42.5; 3,200
-  // scattered rows 20.4 us (17.7 in eights), 1,600 11.6, 5,000 25.3 either way.
+  // V rows of a workgroup: 64 of many (a prefill's runs, whole), 8 of few (a
+  // decode step's scattered rows, spread over the chip).  Where the rows lie is
+  // known on the device alone, so the count decides, about where the two cross for
+  // scattered rows.  Measured, bf16, d = 128, 2 KV heads, us a call in eights and
+  // in 64s: scattered, 1,600 rows 10.6 and 16.2, 2,400 12.9 and 17.1, 3,200 15.9
+  // and 17.8, 4,000 20.8 and 18.8, 5,000 25.4 and 22.0; in eight runs, 1,600 rows
+  // 10.5 and 9.5, 2,400 10.5 and 9.4, 3,200 12.0 and 9.8, 4,000 13.3 and 10.4,
+  // 20,000 53.4 and 41.8.
   const bool tall = (int64_t)p.n * p.Hkv >= 6144;
   p.items_v = ceil_div(p.n, tall ? 64 : 8) * p.Hkv;
   p.items = p.items_v + p.tiles_q.items + p.tiles_k.items + ceil_div(p.n_patch, kThreads);
