@@ -11,7 +11,7 @@ scale for each row (token and KV head) of K and of V.
 The cache: codes of K ``[blocks, Hkv, d/16, 16 tokens, 16 dims]``, codes of V
 ``[blocks, Hkv, d, 16 tokens]``, scales ``[blocks, Hkv, 2, 16]`` (K's tokens,
 then V's) as exponents with a bias of 127.  A row's scale is the smallest
-power of two 2^e with max |x| <= 448 * 2^e (and e >= -110).
+power of two 2^e with max |x| <= 448 * 2^e (and e >= -64).
 """
 from __future__ import annotations
 
@@ -25,7 +25,7 @@ own = False  # False: the plain forms in torch operations; True: the library's c
 DEVICE = "cuda"
 BLOCK = 16
 EPS = 1e-6
-MIN_EXPONENT = -110
+MIN_EXPONENT = -64
 
 
 def _blocks(name, kind, hkv, d, dtype, blocks, pairs):
