@@ -92,7 +92,12 @@ typedef enum {
   PADOC_ERR_MODE = -8        /* plan built for the other entry point            */
 } padoc_status;
 
-typedef enum { PADOC_F32 = 0, PADOC_BF16 = 1 } padoc_dtype;
+typedef enum {
+  PADOC_F32 = 0,
+  PADOC_BF16 = 1,
+  PADOC_BF16_E4M3 = 2, /* decode plans and sessions: Q, O and new rows in bf16, the caches in 8 bits */
+  PADOC_F32_E4M3 = 3   /* ... in fp32, the caches in 8 bits (see "8-bit caches" below)               */
+} padoc_dtype;
 
 /* One tree segment: a page prefix (root), a layout stream or a branch. */
 typedef struct {
@@ -455,6 +460,71 @@ padoc_status padoc_cache_copy_blocks(const void* k_src, const void* v_src, int64
                                      const int32_t* pairs_host, int32_t num_heads_kv, int32_t head_dim,
                                      padoc_dtype dtype, hipStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * 8-bit caches: half the memory of bf16 caches, and half the bytes that a
+ * decode step reads.  A row (token and KV head) of K or V is kept as e4m3 codes
+ * (OCP 8-bit floating point: 4 exponent and 3 fraction bits, largest value 448,
+ * smallest 2^-9) and one power of two:
+ *
+ *   a = max |x_i|,  e = the smallest whole number >= -64 with a <= 448 * 2^e,
+ *   code_i = x_i * 2^-e rounded to the nearest e4m3 value (ties to even),
+ *   standing for code_i * 2^e, off by at most 2^(e-10) or 2^-4 of itself.
+ *
+ * A row with a NaN, an infinity or a magnitude of 248 * 2^120 (3.3e38) and more,
+ * which would round to infinity, is kept as NaN: every query that sees its token
+ * gets NaN (O and LSE), and no other query does.
+ *
+ *   K codes  [num_blocks, Hkv, d/16, 16, 16]  (16-dim pieces, the 16 tokens'
+ *            pieces of one chunk contiguous, in token order)
+ *   V codes  [num_blocks, Hkv, d, 16]         (the 16 tokens of a block
+ *            contiguous for each d)
+ *   scales   [num_blocks, Hkv, 2, 16]         (K's 16 tokens, then V's: a byte
+ *            e + 127 each; 255: the row is NaN.  The library writes 63 to 247
+ *            and 255)
+ *
+ * K rows that are NaN hold code 0x7f, V rows that are NaN code 0.  A cache that
+ * somebody else wrote has to follow the same rules (scale bytes 0 to 62 and 248
+ * to 254 and NaN codes in V rows are not given a meaning).  All three buffers are
+ * 16-byte aligned and distinct; slots that no token is in may hold anything.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  void* k;
+  void* v;
+  void* scales;
+  int64_t num_blocks;
+} padoc_cache_e4m3;
+
+/* Blocks of caches in `dtype` (PADOC_BF16 or PADOC_F32, the layouts at the top of
+   this file) to blocks of 8-bit caches, every slot of them, one kernel: pair i of
+   `pairs` (device int32 [n_pairs][2]) turns block pairs[i][0] of k_src / v_src
+   into block pairs[i][1] of *dst; pairs NULL: block i into block i, for i <
+   n_pairs <= both block counts.  No destination may appear twice; a source may.
+   Pairs with an id outside [0, src_blocks) or [0, dst->num_blocks) are left out.
+   pairs_host (optional): a host copy of the pairs, used only to check all of this
+   (PADOC_ERR_BOUNDS).  Nothing is allocated; the launch may be captured. */
+padoc_status padoc_cache_quantize(const void* k_src, const void* v_src, int64_t src_blocks,
+                                  const padoc_cache_e4m3* dst, const int32_t* pairs, int64_t n_pairs,
+                                  const int32_t* pairs_host, int32_t num_heads_kv, int32_t head_dim,
+                                  padoc_dtype dtype, hipStream_t stream);
+
+/* The other way: the values that the codes stand for (exact in bf16 and fp32; a
+   row that is NaN gives NaN). */
+padoc_status padoc_cache_dequantize(const padoc_cache_e4m3* src, void* k_dst, void* v_dst, int64_t dst_blocks,
+                                    const int32_t* pairs, int64_t n_pairs, const int32_t* pairs_host,
+                                    int32_t num_heads_kv, int32_t head_dim, padoc_dtype dtype, hipStream_t stream);
+
+/* padoc_cache_copy_blocks between 8-bit caches (or within one: src and dst of
+   the same buffers): codes and scales. */
+padoc_status padoc_cache_copy_blocks_e4m3(const padoc_cache_e4m3* src, const padoc_cache_e4m3* dst,
+                                          const int32_t* pairs, int64_t n_pairs, const int32_t* pairs_host,
+                                          int32_t num_heads_kv, int32_t head_dim, hipStream_t stream);
+
+/* padoc_rotary_append into an 8-bit cache: rows in the rotary's dtype, normed and
+   rotated in fp32, each row of K and V rounded once, to its codes.  args->k_cache,
+   v_cache and num_blocks must be 0 (they are cache's). */
+padoc_status padoc_rotary_append_e4m3(const padoc_rotary* rotary, const padoc_rotary_append_args* args,
+                                      const padoc_cache_e4m3* cache, hipStream_t stream);
+
 /* Decode step over a paged cache.  Needs a plan with block_size == 16.
    k_cache / v_cache follow the paged layouts above (chunk-major K, d-major
    V).  block_table is the device copy of the table the plan was built for
@@ -510,6 +580,20 @@ padoc_status padoc_branch_decode_no_alloc(const padoc_plan* plan, const void* q,
                                           const void* k_cache, const void* v_cache,
                                           const int32_t* block_table, void* o, float* lse,
                                           hipStream_t stream);
+
+/* The decode calls on 8-bit caches, with plans of dtype PADOC_BF16_E4M3 or
+   PADOC_F32_E4M3 (which serve no other call; other plans return PADOC_ERR_DTYPE
+   here).  The attention is that of the values the codes stand for: matrix
+   products of bf16 (the values are exact in it) or fp32 operands with fp32 sums.
+   cache->num_blocks must be the plan's num_kv_rows. */
+padoc_status padoc_branch_decode_e4m3(const padoc_plan* plan, const void* q, const padoc_cache_e4m3* cache,
+                                      const int32_t* block_table, void* o, float* lse, void* workspace,
+                                      size_t workspace_bytes, hipStream_t stream);
+padoc_status padoc_branch_decode_resident_e4m3(const padoc_plan* plan, const void* q, const padoc_cache_e4m3* cache,
+                                               const int32_t* block_table, void* o, float* lse, void* workspace,
+                                               size_t workspace_bytes, hipStream_t stream);
+padoc_status padoc_branch_decode_no_alloc_e4m3(const padoc_plan* plan, const void* q, const padoc_cache_e4m3* cache,
+                                               const int32_t* block_table, void* o, float* lse, hipStream_t stream);
 
 /* Backward of the packed forward (bf16 plans with block_size == 0).
    Given the forward's inputs q, k, v, its outputs o and lse, and the
@@ -576,7 +660,8 @@ typedef struct padoc_session padoc_session;
 typedef struct {
   int32_t num_heads_q, num_heads_kv, head_dim;  /* as in padoc_tree_desc      */
   float softmax_scale;
-  padoc_dtype dtype;                 /* of the caches and the step's tensors   */
+  padoc_dtype dtype;                 /* of the caches and the step's tensors;
+                                        8-bit caches: padoc_session_set_scales  */
   int64_t num_blocks;                /* blocks in each cache (the pool)        */
   int64_t block_table_capacity;      /* int32 entries of the device block table */
   void* k_cache;                     /* device, may be NULL for host-only use  */
@@ -695,6 +780,14 @@ padoc_status padoc_session_compact(padoc_session* session, int32_t max_moves, in
    PADOC_ERR_MODE while a compaction's copies wait for their launch, or
    between a prepare and its launch. */
 padoc_status padoc_session_resize(padoc_session* session, int64_t num_blocks, void* k_cache, void* v_cache);
+
+/* A session on 8-bit caches: created with dtype PADOC_BF16_E4M3 or
+   PADOC_F32_E4M3, codes in k_cache / v_cache and their scales named here, before
+   the first launch and again after every resize (which forgets them; a launch
+   without scales returns PADOC_ERR_ARG).  Its launches take rows in the dtype's
+   bf16 or fp32 and quantise them as padoc_rotary_append_e4m3 does.
+   PADOC_ERR_DTYPE for other sessions. */
+padoc_status padoc_session_set_scales(padoc_session* session, void* scales);
 
 /* The block copies of the prepared step, which padoc_session_launch makes
    before it appends (a caller of padoc_session_commit makes them itself):

@@ -13,6 +13,10 @@ results are read elsewhere after a wait).
 
     rot = Rotary(d, "bf16", sections=(16, 24, 24))           # head norms and positions around it
     q, k = rotary_fwd(q, k, positions, rot, wq, wk)
+
+    kc, vc, sc = empty_cache_e4m3(blocks, Hkv, d, "cuda")    # the paged cache in 8 bits
+    plan = TreePlan(segs, Hq, Hkv, d, "bf16_e4m3", block_size=16, ...)
+    o, lse = branch_decode(q, kc, vc, bt, plan, scales=sc)
 """
 from __future__ import annotations
 
@@ -28,9 +32,10 @@ from ._lib import PadocError, SEGMENT_DTYPE, WORK_DTYPE, RANGE_DTYPE, BWD_DTYPE
 
 __all__ = ["TreePlan", "segments_from_pages", "segments_layout", "tree_attn_fwd", "tree_attn_bwd", "branch_decode",
            "DecodeSession", "tree_depths", "tree_remaining", "cache_from_rows", "Rotary", "rotary_fwd", "rotary_bwd",
-           "rotary_append", "cache_copy_blocks", "PadocError", "SEGMENT_DTYPE", "version", "set_kernel_events", "make_workspace"]
+           "rotary_append", "cache_copy_blocks", "empty_cache_e4m3", "cache_quantize", "cache_dequantize", "PadocError", "SEGMENT_DTYPE", "version", "set_kernel_events", "make_workspace"]
 
-_DTYPES = {"f32": _lib.F32, "fp32": _lib.F32, "float32": _lib.F32, "bf16": _lib.BF16, "bfloat16": _lib.BF16}
+_DTYPES = {"f32": _lib.F32, "fp32": _lib.F32, "float32": _lib.F32, "bf16": _lib.BF16, "bfloat16": _lib.BF16,
+           "bf16_e4m3": _lib.BF16_E4M3, "f32_e4m3": _lib.F32_E4M3}  # (of plans and sessions: rows in bf16 / fp32, 8-bit caches)
 
 
 def version() -> str:
@@ -302,8 +307,48 @@ def _check_tensor(name, t, dtype, device):
 
 
 def _torch_dtype(plan):
+    """Of the rows around a plan, a session or a rotary."""
     import torch
-    return torch.bfloat16 if _DTYPES[plan.dtype] == _lib.BF16 else torch.float32
+    return torch.bfloat16 if _DTYPES[plan.dtype] in (_lib.BF16, _lib.BF16_E4M3) else torch.float32
+
+
+def _is_e4m3(plan):
+    return _DTYPES[plan.dtype] >= _lib.BF16_E4M3
+
+
+def _check_cache_e4m3(k_cache, v_cache, scales, dev):
+    """Checks an 8-bit cache; ``(blocks, Hkv, d)``."""
+    import torch
+    if scales is None:
+        raise ValueError("an 8-bit cache needs scales")
+    for name, t, dt in (("k_cache", k_cache, torch.float8_e4m3fn), ("v_cache", v_cache, torch.float8_e4m3fn),
+                        ("scales", scales, torch.float8_e8m0fnu)):
+        _check_tensor(name, t, dt, dev)
+    nb, hkv, d, slots = v_cache.shape if v_cache.dim() == 4 else (0, 0, 0, 0)
+    if slots != 16 or k_cache.shape != (nb, hkv, d // 16, 16, 16) or scales.shape != (nb, hkv, 2, 16):
+        raise ValueError(f"8-bit caches must be K [blocks, Hkv, d/16, 16, 16], V [blocks, Hkv, d, 16] and scales "
+                         f"[blocks, Hkv, 2, 16], got {tuple(k_cache.shape)}, {tuple(v_cache.shape)} and {tuple(scales.shape)}")
+    return nb, hkv, d
+
+
+def _cache_e4m3(k_cache, v_cache, scales):
+    """The call's padoc_cache_e4m3."""
+    return _lib.CACHE_E4M3.pack(k_cache.data_ptr(), v_cache.data_ptr(), scales.data_ptr(), len(v_cache))
+
+
+def _caches(plan, k_cache, v_cache, scales, dev):
+    """The cache arguments of a decode call, checked."""
+    if not _is_e4m3(plan):
+        if scales is not None:
+            raise ValueError(f"scales belong to an 8-bit cache, the plan's dtype is {plan.dtype}")
+        dt = _torch_dtype(plan)
+        _check_tensor("k_cache", k_cache, dt, dev)
+        _check_tensor("v_cache", v_cache, dt, dev)
+        return _ptr(k_cache), _ptr(v_cache)
+    got = _check_cache_e4m3(k_cache, v_cache, scales, dev)
+    if got[1:] != (plan.num_heads_kv, plan.head_dim):
+        raise ValueError(f"the caches hold {got[1]} heads of {got[2]}, the plan has {plan.num_heads_kv} of {plan.head_dim}")
+    return (_cache_e4m3(k_cache, v_cache, scales),)
 
 
 def _outputs(plan, q, out, lse):
@@ -343,37 +388,42 @@ def _repeat_call(plan, key):
 
 
 def branch_decode(q, k_cache, v_cache, block_table, plan: TreePlan, out=None, lse=None, workspace=None,
-                  stream=None):
+                  stream=None, scales=None):
     """Decode step over a paged cache (``padoc_branch_decode``).  q ``[n_q,
     Hq, d]``; K cache chunk-major ``[blocks, Hkv, d/8, 16, 8]``, V cache
     d-major ``[blocks, Hkv, d, 16]`` (layouts in ``padoc_attn.h``);
-    block_table int32 on the device; returns ``(O, LSE)``."""
+    block_table int32 on the device; returns ``(O, LSE)``.  With ``scales`` the
+    cache is an 8-bit one (``empty_cache_e4m3``,
+    ``padoc_branch_decode_e4m3``), and the plan is of dtype "bf16_e4m3" or
+    "f32_e4m3"."""
     import torch
+    L = _lib.lib()
+    call = L.padoc_branch_decode if scales is None else L.padoc_branch_decode_e4m3
+    given = (q, k_cache, v_cache, block_table, out, lse, workspace) + (() if scales is None else (scales,))
     if out is not None and lse is not None and workspace is not None:
         s = torch.cuda.current_stream(q.device) if stream is None else stream
         key = ("decode", plan.handle, s.cuda_stream) + tuple(
-            (id(t), t.data_ptr(), t.shape, t.stride(), t.dtype) for t in (q, k_cache, v_cache, block_table, out, lse, workspace))
+            (id(t), t.data_ptr(), t.shape, t.stride(), t.dtype) for t in given)
         args = _repeat_call(plan, key)
         if args is not None:
-            _lib.check(_lib.lib().padoc_branch_decode(*args))
+            _lib.check(call(*args))
             return out, lse
     elif stream is not None:
-        return _on_stream(stream, q.get_device(), branch_decode, q, k_cache, v_cache, block_table, plan, out, lse, workspace)
-    dt = _torch_dtype(plan)
+        return _on_stream(stream, q.get_device(), branch_decode, q, k_cache, v_cache, block_table, plan, out, lse, workspace,
+                          None, scales)
     dev = q.device
-    for name, t in (("q", q), ("k_cache", k_cache), ("v_cache", v_cache)):
-        _check_tensor(name, t, dt, dev)
+    _check_tensor("q", q, _torch_dtype(plan), dev)
+    caches = _caches(plan, k_cache, v_cache, scales, dev)
     _check_tensor("block_table", block_table, torch.int32, dev)
     out, lse = _outputs(plan, q, out, lse)
     ws = plan.workspace(dev) if workspace is None else workspace
     s = torch.cuda.current_stream(dev) if stream is None else stream
-    args = (plan.handle, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(out), _ptr(lse), _ptr(ws),
-            ws.numel(), C.c_void_p(s.cuda_stream))
-    _lib.check(_lib.lib().padoc_branch_decode(*args))
+    args = (plan.handle, _ptr(q), *caches, _ptr(block_table), _ptr(out), _ptr(lse), _ptr(ws), ws.numel(),
+            C.c_void_p(s.cuda_stream))
+    _lib.check(call(*args))
     if workspace is not None:
         plan._last_call = (("decode", plan.handle, s.cuda_stream) + tuple(
-            (id(t), t.data_ptr(), t.shape, t.stride(), t.dtype) for t in (q, k_cache, v_cache, block_table, out, lse, workspace)),
-            args)
+            (id(t), t.data_ptr(), t.shape, t.stride(), t.dtype) for t in given), args)
     return out, lse
 
 
@@ -392,31 +442,35 @@ def plan_upload(plan: TreePlan, workspace, stream=None):
     return workspace
 
 
-def branch_decode_resident(q, k_cache, v_cache, block_table, plan: TreePlan, out, lse, workspace, stream=None):
+def branch_decode_resident(q, k_cache, v_cache, block_table, plan: TreePlan, out, lse, workspace, stream=None, scales=None):
     """Decode step on a workspace that holds the plan's schedule
     (``padoc_branch_decode_resident``, after ``plan_upload``): the kernels of
     ``branch_decode`` without the schedule copy."""
     import torch
+    L = _lib.lib()
+    call = L.padoc_branch_decode_resident if scales is None else L.padoc_branch_decode_resident_e4m3
     s = torch.cuda.current_stream(q.device) if stream is None else stream
     key = ("resident", plan.handle, s.cuda_stream) + tuple(
-        (id(t), t.data_ptr(), t.shape, t.stride(), t.dtype) for t in (q, k_cache, v_cache, block_table, out, lse, workspace))
+        (id(t), t.data_ptr(), t.shape, t.stride(), t.dtype)
+        for t in (q, k_cache, v_cache, block_table, out, lse, workspace) + (() if scales is None else (scales,)))
     args = _repeat_call(plan, key)
     if args is None:
         dt = _torch_dtype(plan)
         dev = q.device
-        for name, t in (("q", q), ("k_cache", k_cache), ("v_cache", v_cache), ("out", out)):
+        for name, t in (("q", q), ("out", out)):
             _check_tensor(name, t, dt, dev)
+        caches = _caches(plan, k_cache, v_cache, scales, dev)
         _check_tensor("block_table", block_table, torch.int32, dev)
         _check_tensor("lse", lse, torch.float32, dev)
         _check_tensor("workspace", workspace, torch.uint8, dev)
-        args = (plan.handle, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(out), _ptr(lse),
-                _ptr(workspace), workspace.numel(), C.c_void_p(s.cuda_stream))
-    _lib.check(_lib.lib().padoc_branch_decode_resident(*args))
+        args = (plan.handle, _ptr(q), *caches, _ptr(block_table), _ptr(out), _ptr(lse), _ptr(workspace),
+                workspace.numel(), C.c_void_p(s.cuda_stream))
+    _lib.check(call(*args))
     plan._last_call = (key, args)
     return out, lse
 
 
-def branch_decode_no_alloc(q, k_cache, v_cache, block_table, plan: TreePlan, out, lse, stream=None):
+def branch_decode_no_alloc(q, k_cache, v_cache, block_table, plan: TreePlan, out, lse, stream=None, scales=None):
     """Decode step with the library's fixed per-GPU workspace
     (``padoc_branch_decode_no_alloc``): the caller passes every input and
     both outputs; nothing is allocated.  Calls that overlap on one GPU race
@@ -424,14 +478,15 @@ def branch_decode_no_alloc(q, k_cache, v_cache, block_table, plan: TreePlan, out
     import torch
     dt = _torch_dtype(plan)
     dev = q.device
-    for name, t in (("q", q), ("k_cache", k_cache), ("v_cache", v_cache), ("out", out)):
+    for name, t in (("q", q), ("out", out)):
         _check_tensor(name, t, dt, dev)
+    caches = _caches(plan, k_cache, v_cache, scales, dev)
     _check_tensor("block_table", block_table, torch.int32, dev)
     _check_tensor("lse", lse, torch.float32, dev)
     s = torch.cuda.current_stream(dev) if stream is None else stream
-    _lib.check(_lib.lib().padoc_branch_decode_no_alloc(plan.handle, _ptr(q), _ptr(k_cache), _ptr(v_cache),
-                                                       _ptr(block_table), _ptr(out), _ptr(lse),
-                                                       C.c_void_p(s.cuda_stream)))
+    L = _lib.lib()
+    call = L.padoc_branch_decode_no_alloc if scales is None else L.padoc_branch_decode_no_alloc_e4m3
+    _lib.check(call(plan.handle, _ptr(q), *caches, _ptr(block_table), _ptr(out), _ptr(lse), C.c_void_p(s.cuda_stream)))
     return out, lse
 
 
@@ -741,16 +796,18 @@ def _check_caches(k_cache, v_cache, dtype, dev):
 
 
 def rotary_append(q, k, v, positions, slots, k_cache, v_cache, rotary: Rotary, q_weight=None, k_weight=None,
-                  q_positions=None, q_out=None, stream=None):
+                  q_positions=None, q_out=None, stream=None, scales=None):
     """A decode step's rows (``padoc_rotary_append``): q ``[n_q, Hq, d]``
     normed and rotated into ``q_out``, k and v ``[n_new, Hkv, d]`` into the
     caches (k normed and rotated) at ``slots`` (int32 ``[n_new, 2]``: block id
     and slot; a block id of -1 leaves the row out).  ``q_positions`` may be
-    left out when query row i is new row i; q may be None.  Returns q_out."""
+    left out when query row i is new row i; q may be None.  With ``scales`` the
+    cache is an 8-bit one, and every row of k and v is quantised
+    (``padoc_rotary_append_e4m3``).  Returns q_out."""
     if stream is not None:
         return _on_stream(stream, _rows_of(rotary, q if k is None else k)[0], rotary_append, q, k, v, positions, slots,
-                          k_cache, v_cache, rotary, q_weight, k_weight, q_positions, q_out)
-    if rotary._rows is not None:
+                          k_cache, v_cache, rotary, q_weight, k_weight, q_positions, q_out, None, scales)
+    if rotary._rows is not None and scales is None:
         done = rotary._rows.append(q, k, v, positions, slots, k_cache, v_cache, q_weight, k_weight, q_positions, q_out)
         if done is not None:
             return done[0] if type(done) is tuple else _lib.check(done)
@@ -758,12 +815,18 @@ def rotary_append(q, k, v, positions, slots, k_cache, v_cache, rotary: Rotary, q
     if k is None or v is None:
         raise ValueError("rotary_append needs k and v (rotary_fwd rotates q alone)")
     dev = k.device
-    nb, hkv, d = _check_caches(k_cache, v_cache, rotary.torch_dtype, dev)
+    nb, hkv, d = (_check_caches(k_cache, v_cache, rotary.torch_dtype, dev) if scales is None else
+                  _check_cache_e4m3(k_cache, v_cache, scales, dev))
     if k.shape[1:] != (hkv, d) or d != rotary.head_dim:
         raise ValueError(f"the caches hold {hkv} heads of {d}, the rows are {tuple(k.shape)}")
     _check_tensor("slots", slots, torch.int32, dev)
     if slots.shape != (k.shape[0], 2):
         raise ValueError(f"slots has shape {tuple(slots.shape)}, expected {(k.shape[0], 2)}")
+    if scales is not None:
+        args, q_out, device = _append_args(rotary, q, k, v, positions, q_weight, k_weight, q_positions, q_out,
+                                           slots.data_ptr())
+        _launch(_lib.lib().padoc_rotary_append_e4m3, device, rotary.handle, args, _cache_e4m3(k_cache, v_cache, scales))
+        return q_out
     args, q_out, device = _append_args(rotary, q, k, v, positions, q_weight, k_weight, q_positions, q_out,
                                        slots.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), nb)
     _launch(_lib.lib().padoc_rotary_append, device, rotary.handle, args)
@@ -777,15 +840,35 @@ def _copy_blocks(k_cache, v_cache, pairs):
     return _copy_blocks(k_cache, v_cache, pairs)
 
 
-def cache_copy_blocks(k_cache, v_cache, pairs, k_dst=None, v_dst=None, pairs_host=None, stream=None):
+def _pairs(pairs, pairs_host, dev):
+    """``(address, count, host copy)`` of block pairs."""
+    import torch
+    _check_tensor("pairs", pairs, torch.int32, dev)
+    if pairs.dim() != 2 or pairs.shape[1] != 2:
+        raise ValueError(f"pairs has shape {tuple(pairs.shape)}, expected [n, 2]")
+    host = None
+    if pairs_host is not None:
+        host = np.ascontiguousarray(pairs_host, dtype=np.int32)
+        if host.shape != pairs.shape:
+            raise ValueError(f"pairs_host has shape {host.shape}, expected {tuple(pairs.shape)}")
+    return pairs.data_ptr(), pairs.shape[0], host
+
+
+def cache_copy_blocks(k_cache, v_cache, pairs, k_dst=None, v_dst=None, pairs_host=None, stream=None, scales=None,
+                      scales_dst=None):
     """Copy blocks ``pairs[i, 0]`` of the paged caches to blocks ``pairs[i,
     1]`` of the same caches, or of ``k_dst`` / ``v_dst``
     (``padoc_cache_copy_blocks``; int32 ``[n, 2]`` on the device, with an
-    optional host copy that is only checked).  Returns the caches written."""
+    optional host copy that is only checked).  Returns the caches written; of
+    8-bit caches (``scales``, and ``scales_dst`` beside ``k_dst`` / ``v_dst``)
+    three tensors."""
     if stream is not None:
         if not k_cache.is_cuda:
             raise ValueError(f"k_cache is on {k_cache.device}, expected a GPU")
-        return _on_stream(stream, k_cache.get_device(), cache_copy_blocks, k_cache, v_cache, pairs, k_dst, v_dst, pairs_host)
+        return _on_stream(stream, k_cache.get_device(), cache_copy_blocks, k_cache, v_cache, pairs, k_dst, v_dst, pairs_host,
+                          None, scales, scales_dst)
+    if scales is not None or scales_dst is not None:
+        return _copy_blocks_e4m3(k_cache, v_cache, scales, pairs, k_dst, v_dst, scales_dst, pairs_host)
     if k_dst is None and v_dst is None and pairs_host is None:
         done = _copy_blocks(k_cache, v_cache, pairs)
         if done is not None:
@@ -807,17 +890,118 @@ def cache_copy_blocks(k_cache, v_cache, pairs, k_dst=None, v_dst=None, pairs_hos
         nd, h2, d2 = _check_caches(k_dst, v_dst, dt, dev)
         if (h2, d2) != (hkv, d):
             raise ValueError(f"blocks of {hkv} heads of {d} do not fit caches of {h2} heads of {d2}")
-    _check_tensor("pairs", pairs, torch.int32, dev)
-    if pairs.dim() != 2 or pairs.shape[1] != 2:
-        raise ValueError(f"pairs has shape {tuple(pairs.shape)}, expected [n, 2]")
-    host = None
-    if pairs_host is not None:
-        host = np.ascontiguousarray(pairs_host, dtype=np.int32)
-        if host.shape != pairs.shape:
-            raise ValueError(f"pairs_host has shape {host.shape}, expected {tuple(pairs.shape)}")
+    address, n, host = _pairs(pairs, pairs_host, dev)
     _launch(_lib.lib().padoc_cache_copy_blocks, dev.index, k_cache.data_ptr(), v_cache.data_ptr(), nb,
-            k_dst.data_ptr(), v_dst.data_ptr(), nd, pairs.data_ptr(), pairs.shape[0],
-            None if host is None else host.ctypes.data, hkv, d, _lib.BF16 if dt == torch.bfloat16 else _lib.F32)
+            k_dst.data_ptr(), v_dst.data_ptr(), nd, address, n, None if host is None else host.ctypes.data, hkv, d,
+            _lib.BF16 if dt == torch.bfloat16 else _lib.F32)
+    return k_dst, v_dst
+
+
+def _copy_blocks_e4m3(k_cache, v_cache, scales, pairs, k_dst, v_dst, scales_dst, pairs_host):
+    dev = k_cache.device
+    if not k_cache.is_cuda:
+        raise ValueError(f"k_cache is on {dev}, expected a GPU")
+    given = [t is not None for t in (k_dst, v_dst, scales_dst)]
+    if any(given) and not all(given):
+        raise ValueError("pass k_dst, v_dst and scales_dst together (or none of them)")
+    nb, hkv, d = _check_cache_e4m3(k_cache, v_cache, scales, dev)
+    dst = (k_dst, v_dst, scales_dst) if given[0] else (k_cache, v_cache, scales)
+    nd, h2, d2 = _check_cache_e4m3(*dst, dev)
+    if (h2, d2) != (hkv, d):
+        raise ValueError(f"blocks of {hkv} heads of {d} do not fit caches of {h2} heads of {d2}")
+    address, n, host = _pairs(pairs, pairs_host, dev)
+    _launch(_lib.lib().padoc_cache_copy_blocks_e4m3, dev.index, _cache_e4m3(k_cache, v_cache, scales), _cache_e4m3(*dst),
+            address, n, None if host is None else host.ctypes.data, hkv, d)
+    return dst
+
+
+def empty_cache_e4m3(num_blocks: int, num_heads_kv: int, head_dim: int, device):
+    """An 8-bit paged cache, uninitialised: ``(k_cache, v_cache, scales)``, e4m3
+    codes ``[blocks, Hkv, d/16, 16, 16]`` and ``[blocks, Hkv, d, 16]`` and a
+    power of two for each row, ``[blocks, Hkv, 2, 16]`` (K's tokens, then V's;
+    "8-bit caches" in ``padoc_attn.h``)."""
+    import torch
+    return (torch.empty((num_blocks, num_heads_kv, head_dim // 16, 16, 16), dtype=torch.float8_e4m3fn, device=device),
+            torch.empty((num_blocks, num_heads_kv, head_dim, 16), dtype=torch.float8_e4m3fn, device=device),
+            torch.empty((num_blocks, num_heads_kv, 2, 16), dtype=torch.float8_e8m0fnu, device=device))
+
+
+def _cast_blocks(f, k_cache, v_cache, e4m3, pairs, pairs_host, back):
+    """Blocks between caches of values and an 8-bit cache."""
+    import torch
+    dev, dt = k_cache.device, k_cache.dtype
+    if not k_cache.is_cuda:
+        raise ValueError(f"k_cache is on {dev}, expected a GPU")
+    if dt not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"caches must be bfloat16 or float32, got {dt}")
+    nb, hkv, d = _check_caches(k_cache, v_cache, dt, dev)
+    n8, h8, d8 = _check_cache_e4m3(*e4m3, dev)
+    if (h8, d8) != (hkv, d):
+        raise ValueError(f"blocks of {hkv} heads of {d} and of {h8} heads of {d8}")
+    if pairs is None:
+        if pairs_host is not None:
+            raise ValueError("pairs_host without pairs")
+        if nb != n8:
+            raise ValueError(f"caches of {nb} and {n8} blocks need pairs")
+        address, n, host = None, nb, None
+    else:
+        address, n, host = _pairs(pairs, pairs_host, dev)
+    host = None if host is None else host.ctypes.data
+    tail = hkv, d, _lib.BF16 if dt == torch.bfloat16 else _lib.F32
+    if back:
+        _launch(f, dev.index, _cache_e4m3(*e4m3), k_cache.data_ptr(), v_cache.data_ptr(), nb, address, n, host, *tail)
+    else:
+        _launch(f, dev.index, k_cache.data_ptr(), v_cache.data_ptr(), nb, _cache_e4m3(*e4m3), address, n, host, *tail)
+
+
+def cache_quantize(k_cache, v_cache, k_dst=None, v_dst=None, scales_dst=None, pairs=None, pairs_host=None, stream=None):
+    """Blocks of bf16 or fp32 caches in the library's layouts as blocks of an
+    8-bit cache (``padoc_cache_quantize``): blocks ``pairs[i, 0]`` to blocks
+    ``pairs[i, 1]`` of the given one, or block for block.  Returns ``(k_dst,
+    v_dst, scales_dst)`` (allocated when not given, and then every block
+    has to be written: no pairs)."""
+    if stream is not None:
+        if not k_cache.is_cuda:
+            raise ValueError(f"k_cache is on {k_cache.device}, expected a GPU")
+        return _on_stream(stream, k_cache.get_device(), cache_quantize, k_cache, v_cache, k_dst, v_dst, scales_dst, pairs,
+                          pairs_host)
+    given = [t is not None for t in (k_dst, v_dst, scales_dst)]
+    if any(given) and not all(given):
+        raise ValueError("pass k_dst, v_dst and scales_dst together (or none of them)")
+    if not given[0]:
+        if pairs is not None:
+            raise ValueError("pairs name blocks of a cache: pass k_dst, v_dst and scales_dst")
+        if v_cache.dim() != 4:
+            raise ValueError(f"v_cache must be [blocks, Hkv, d, 16], got {tuple(v_cache.shape)}")
+        k_dst, v_dst, scales_dst = empty_cache_e4m3(*v_cache.shape[:3], k_cache.device)
+    _cast_blocks(_lib.lib().padoc_cache_quantize, k_cache, v_cache, (k_dst, v_dst, scales_dst), pairs, pairs_host, False)
+    return k_dst, v_dst, scales_dst
+
+
+def cache_dequantize(k_cache, v_cache, scales, k_dst=None, v_dst=None, dtype: str = "bf16", pairs=None, pairs_host=None,
+                     stream=None):
+    """The values of an 8-bit cache's blocks as blocks of bf16 or fp32 caches
+    (``padoc_cache_dequantize``; exact in both).  ``pairs`` as in
+    ``cache_quantize``; returns ``(k_dst, v_dst)`` (of ``dtype`` where they are
+    not given)."""
+    import torch
+    if stream is not None:
+        if not k_cache.is_cuda:
+            raise ValueError(f"k_cache is on {k_cache.device}, expected a GPU")
+        return _on_stream(stream, k_cache.get_device(), cache_dequantize, k_cache, v_cache, scales, k_dst, v_dst, dtype, pairs,
+                          pairs_host)
+    if (k_dst is None) != (v_dst is None):
+        raise ValueError("pass k_dst and v_dst together (or neither)")
+    if k_dst is None:
+        if pairs is not None:
+            raise ValueError("pairs name blocks of a cache: pass k_dst and v_dst")
+        if dtype not in _DTYPES or _DTYPES[dtype] >= _lib.BF16_E4M3:
+            raise ValueError(f"dtype {dtype!r} is not \"bf16\" or \"f32\"")
+        dt = torch.bfloat16 if _DTYPES[dtype] == _lib.BF16 else torch.float32
+        nb, hkv, d = _check_cache_e4m3(k_cache, v_cache, scales, k_cache.device)
+        k_dst = torch.empty((nb, hkv, d // 8, 16, 8), dtype=dt, device=k_cache.device)
+        v_dst = torch.empty((nb, hkv, d, 16), dtype=dt, device=k_cache.device)
+    _cast_blocks(_lib.lib().padoc_cache_dequantize, k_dst, v_dst, (k_cache, v_cache, scales), pairs, pairs_host, True)
     return k_dst, v_dst
 
 
@@ -832,11 +1016,13 @@ class DecodeSession:
     ``launch(q, k_new, v_new)`` (device: append the K/V rows, patch the block
     table, attention); rows follow ascending open stream id.  Without caches
     (``k_cache=None``) the session is host-only: steps are completed with
-    ``commit()`` and inspected with ``view()``."""
+    ``commit()`` and inspected with ``view()``.  With dtype "bf16_e4m3" or
+    "f32_e4m3" the caches are 8-bit ones, with their ``scales``: rows come in
+    bf16 or fp32 and are quantised as they are appended."""
 
     def __init__(self, num_heads_q: int, num_heads_kv: int, head_dim: int, num_blocks: int, dtype: str = "bf16",
                  k_cache=None, v_cache=None, block_table=None, block_table_capacity: Optional[int] = None,
-                 softmax_scale: Optional[float] = None, max_chunk_keys: int = 0, target_workgroups: int = 0):
+                 softmax_scale: Optional[float] = None, max_chunk_keys: int = 0, target_workgroups: int = 0, scales=None):
         self.num_heads_q, self.num_heads_kv, self.head_dim = num_heads_q, num_heads_kv, head_dim
         self.dtype = dtype
         self.num_blocks = int(num_blocks)
@@ -844,18 +1030,27 @@ class DecodeSession:
         dev = (k_cache, v_cache, block_table)
         if any(t is not None for t in dev) and any(t is None for t in dev):
             raise ValueError("pass k_cache, v_cache and block_table together (or none of them)")
-        self.k_cache, self.v_cache, self.block_table = k_cache, v_cache, block_table
+        self.k_cache, self.v_cache, self.block_table, self.scales = k_cache, v_cache, block_table, scales
+        if scales is not None and (block_table is None or not _is_e4m3(self)):
+            raise ValueError(f"scales belong to 8-bit caches, the session's dtype is {dtype}" if block_table is not None
+                             else "scales without caches")
         if block_table is not None:
             import torch
-            dt = torch.bfloat16 if _DTYPES[dtype] == _lib.BF16 else torch.float32
             dv = k_cache.device
-            _check_tensor("k_cache", k_cache, dt, dv)
-            _check_tensor("v_cache", v_cache, dt, dv)
             _check_tensor("block_table", block_table, torch.int32, dv)
-            want_k = (self.num_blocks, num_heads_kv, head_dim // 8, 16, 8)
-            want_v = (self.num_blocks, num_heads_kv, head_dim, 16)
-            if tuple(k_cache.shape) != want_k or tuple(v_cache.shape) != want_v:
-                raise ValueError(f"caches must be K {want_k} and V {want_v}")
+            if _is_e4m3(self):
+                got = _check_cache_e4m3(k_cache, v_cache, scales, dv)
+                if got != (self.num_blocks, num_heads_kv, head_dim):
+                    raise ValueError(f"caches hold {got} blocks, heads and dimensions, expected "
+                                     f"{(self.num_blocks, num_heads_kv, head_dim)}")
+            else:
+                dt = _torch_dtype(self)
+                _check_tensor("k_cache", k_cache, dt, dv)
+                _check_tensor("v_cache", v_cache, dt, dv)
+                want_k = (self.num_blocks, num_heads_kv, head_dim // 8, 16, 8)
+                want_v = (self.num_blocks, num_heads_kv, head_dim, 16)
+                if tuple(k_cache.shape) != want_k or tuple(v_cache.shape) != want_v:
+                    raise ValueError(f"caches must be K {want_k} and V {want_v}")
             if block_table_capacity is None:
                 block_table_capacity = block_table.numel()
             if block_table_capacity > block_table.numel():
@@ -875,6 +1070,8 @@ class DecodeSession:
         h = C.c_void_p()
         _lib.check(_lib.lib().padoc_session_create(C.byref(desc), C.byref(h)))
         self._h = h
+        if scales is not None:
+            _lib.check(_lib.lib().padoc_session_set_scales(h, scales.data_ptr()))
         self._streams = _lib.streams(h)
         self.n_open = 0
         self.n_kv_rows = self.n_q_rows = 0
@@ -949,23 +1146,29 @@ class DecodeSession:
         _lib.check(_lib.lib().padoc_session_compact(self.handle, int(max_moves), C.byref(n)))
         return int(n.value)
 
-    def resize(self, num_blocks: int, k_cache=None, v_cache=None) -> None:
+    def resize(self, num_blocks: int, k_cache=None, v_cache=None, scales=None) -> None:
         """Change the pool to ``num_blocks`` blocks
         (``padoc_session_resize``): with device caches, into ``k_cache`` /
         ``v_cache`` of that many blocks, which hold the present blocks at their
         ids (``k_cache[:num_blocks]`` of the old caches after a compaction, or
-        larger ones the caller copied them to)."""
+        larger ones the caller copied them to); 8-bit caches with their
+        ``scales``."""
         if (k_cache is None) != (v_cache is None) or (k_cache is None) != (self.k_cache is None):
             raise ValueError("pass both caches, or neither for a host-only session")
+        if (scales is None) != (self.scales is None):
+            raise ValueError("8-bit caches come with scales, others without")
         if k_cache is not None:
-            got = _check_caches(k_cache, v_cache, self.k_cache.dtype, self.device)
+            got = (_check_caches(k_cache, v_cache, self.k_cache.dtype, self.device) if scales is None else
+                   _check_cache_e4m3(k_cache, v_cache, scales, self.device))
             if got != (num_blocks, self.num_heads_kv, self.head_dim):
                 raise ValueError(f"caches hold {got} blocks, heads and dimensions, expected "
                                  f"{(num_blocks, self.num_heads_kv, self.head_dim)}")
         _lib.check(_lib.lib().padoc_session_resize(self.handle, int(num_blocks),
                                                    None if k_cache is None else k_cache.data_ptr(),
                                                    None if v_cache is None else v_cache.data_ptr()))
-        self.k_cache, self.v_cache, self.num_blocks = k_cache, v_cache, int(num_blocks)
+        if scales is not None:
+            _lib.check(_lib.lib().padoc_session_set_scales(self.handle, scales.data_ptr()))
+        self.k_cache, self.v_cache, self.scales, self.num_blocks = k_cache, v_cache, scales, int(num_blocks)
         self._users = set()
 
     def copies(self):
@@ -1037,8 +1240,9 @@ class DecodeSession:
         if raw in self._users:
             return
         s = torch.cuda.current_stream(self.device)
-        for t in (self.k_cache, self.v_cache, self.block_table) + (() if self._ws is None else (self._ws[1],)):
-            t.record_stream(s)
+        for t in (self.k_cache, self.v_cache, self.block_table, self.scales, None if self._ws is None else self._ws[1]):
+            if t is not None:
+                t.record_stream(s)
         self._users.add(raw)
 
     def launch(self, q, k_new, v_new, out=None, lse=None, workspace=None, stream=None):
@@ -1049,7 +1253,7 @@ class DecodeSession:
             raise RuntimeError("host-only session: use commit()")
         if stream is not None:
             return _on_stream(stream, self.device.index, self.launch, q, k_new, v_new, out, lse, workspace)
-        dt = self.k_cache.dtype
+        dt = _torch_dtype(self)
         dev = self.device
         if self.n_kv_rows:
             for name, t in (("k_new", k_new), ("v_new", v_new)):
@@ -1095,9 +1299,9 @@ class DecodeSession:
             return _on_stream(stream, self.device.index, self.launch_rotary, q, k_new, v_new, positions, rotary, q_weight,
                               k_weight, q_positions, q_rot, out, lse, workspace)
         n_q, n_kv = self.n_q_rows, self.n_kv_rows
-        dt, dev = self.k_cache.dtype, self.device
+        dt, dev = _torch_dtype(self), self.device
         if _torch_dtype(rotary) != dt:
-            raise TypeError(f"the rotary is for {rotary.dtype}, the session's caches are {dt}")
+            raise TypeError(f"the rotary is for {rotary.dtype}, the session's rows are {dt}")
         if rotary.head_dim != self.head_dim:
             raise ValueError(f"the rotary is for heads of {rotary.head_dim}, the session's have {self.head_dim}")
         if n_kv:

@@ -18,7 +18,7 @@ OK, ERR_ARG, ERR_TREE, ERR_SHAPE, ERR_DTYPE, ERR_BOUNDS, ERR_WORKSPACE, ERR_HIP,
 STATUS_NAMES = {0: "PADOC_OK", -1: "PADOC_ERR_ARG", -2: "PADOC_ERR_TREE", -3: "PADOC_ERR_SHAPE",
                 -4: "PADOC_ERR_DTYPE", -5: "PADOC_ERR_BOUNDS", -6: "PADOC_ERR_WORKSPACE",
                 -7: "PADOC_ERR_HIP", -8: "PADOC_ERR_MODE"}
-F32, BF16 = 0, 1
+F32, BF16, BF16_E4M3, F32_E4M3 = 0, 1, 2, 3
 
 SEGMENT_DTYPE = np.dtype([("parent", "<i4"), ("fork", "<i4"), ("len", "<i4"), ("q_len", "<i4"),
                           ("kv_off", "<i8"), ("q_off", "<i8")])
@@ -95,6 +95,9 @@ ROTARY_FWD_ARGS = struct.Struct("=qiiQq" + 4 * "Qqq" + "QQ")
 ROTARY_BWD_ARGS = struct.Struct("=qiiQq" + 6 * "Qqq" + "QQQQ")
 ROTARY_APPEND_ARGS = struct.Struct("=qqiiQqQq" + 4 * "Qqq" + "QQQQQq")
 
+# A padoc_cache_e4m3: k, v, scales, blocks.
+CACHE_E4M3 = struct.Struct("=QQQq")
+
 EXPORTED = [
     "padoc_tree_from_pages", "padoc_tree_layout", "padoc_plan_create", "padoc_plan_workspace_bytes",
     "padoc_plan_export", "padoc_plan_destroy", "padoc_tree_attn_fwd", "padoc_branch_decode",
@@ -107,7 +110,9 @@ EXPORTED = [
     "padoc_rotary_create", "padoc_rotary_destroy", "padoc_rotary_fwd", "padoc_rotary_bwd_workspace_bytes",
     "padoc_rotary_bwd", "padoc_rotary_append", "padoc_cache_copy_blocks", "padoc_session_launch_rotary",
     "padoc_session_clone", "padoc_session_truncate", "padoc_session_compact", "padoc_session_resize",
-    "padoc_session_copies",
+    "padoc_session_copies", "padoc_cache_quantize", "padoc_cache_dequantize", "padoc_cache_copy_blocks_e4m3",
+    "padoc_rotary_append_e4m3", "padoc_branch_decode_e4m3", "padoc_branch_decode_resident_e4m3",
+    "padoc_branch_decode_no_alloc_e4m3", "padoc_session_set_scales",
 ]
 
 _lib = None
@@ -165,6 +170,15 @@ def lib():
     L.padoc_session_compact.argtypes = [vp, i32, C.POINTER(i32)]
     L.padoc_session_resize.argtypes = [vp, i64, vp, vp]
     L.padoc_session_copies.argtypes = [vp, C.POINTER(i32), C.POINTER(vp), C.POINTER(vp)]
+    cache = C.c_char_p  # a packed CACHE_E4M3
+    L.padoc_cache_quantize.argtypes = [vp, vp, i64, cache, vp, i64, vp, i32, i32, C.c_int, vp]
+    L.padoc_cache_dequantize.argtypes = [cache, vp, vp, i64, vp, i64, vp, i32, i32, C.c_int, vp]
+    L.padoc_cache_copy_blocks_e4m3.argtypes = [cache, cache, vp, i64, vp, i32, i32, vp]
+    L.padoc_rotary_append_e4m3.argtypes = [vp, C.c_char_p, cache, vp]
+    L.padoc_branch_decode_e4m3.argtypes = [vp, vp, cache, vp, vp, vp, vp, sz, vp]
+    L.padoc_branch_decode_resident_e4m3.argtypes = [vp, vp, cache, vp, vp, vp, vp, sz, vp]
+    L.padoc_branch_decode_no_alloc_e4m3.argtypes = [vp, vp, cache, vp, vp, vp, vp]
+    L.padoc_session_set_scales.argtypes = [vp, vp]
     L.padoc_last_error.argtypes = []
     L.padoc_last_error.restype = C.c_char_p
     L.padoc_set_kernel_events.argtypes = [vp, vp]
@@ -179,7 +193,10 @@ def lib():
                  "padoc_tree_remaining", "padoc_session_select", "padoc_cache_from_rows", "padoc_rotary_create",
                  "padoc_rotary_fwd", "padoc_rotary_bwd_workspace_bytes", "padoc_rotary_bwd", "padoc_rotary_append",
                  "padoc_cache_copy_blocks", "padoc_session_launch_rotary", "padoc_session_clone",
-                 "padoc_session_truncate", "padoc_session_compact", "padoc_session_resize", "padoc_session_copies"):
+                 "padoc_session_truncate", "padoc_session_compact", "padoc_session_resize", "padoc_session_copies",
+                 "padoc_cache_quantize", "padoc_cache_dequantize", "padoc_cache_copy_blocks_e4m3",
+                 "padoc_rotary_append_e4m3", "padoc_branch_decode_e4m3", "padoc_branch_decode_resident_e4m3",
+                 "padoc_branch_decode_no_alloc_e4m3", "padoc_session_set_scales"):
         getattr(L, name).restype = C.c_int
     _lib = L
     return L

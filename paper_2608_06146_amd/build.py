@@ -47,6 +47,8 @@ SOURCES = [
     "csrc/kernels/upload.hip",
     "csrc/kernels/rotary.hip",
     "csrc/kernels/copy_blocks.hip",
+    "csrc/kernels/cache_e4m3.hip",
+    "csrc/kernels/decode_e4m3.hip",
 ]
 # Every header under csrc/ (and the public header) enters each object's
 # digest, so an edit to any of them rebuilds every object.

@@ -28,6 +28,9 @@ hipError_t launch_rotary_fwd(RotaryParams p, int D, bool bf16, bool pairs, hipSt
 hipError_t launch_rotary_bwd(RotaryParams p, int D, bool bf16, bool pairs, float* dwq, float* dwk, hipStream_t s);
 hipError_t launch_rotary_append(RotaryParams p, int D, bool bf16, bool pairs, hipStream_t s);
 hipError_t launch_copy_blocks(const CopyParams& p, hipStream_t s);
+hipError_t launch_rotary_append_e4m3(RotaryParams p, int D, bool bf16, bool pairs, hipStream_t s);
+hipError_t launch_cast_blocks(const CastParams& p, int D, bool bf16, bool back, hipStream_t s);
+hipError_t launch_decode_e4m3(const TileParams& p, int n_shared, int n_private, int D, hipStream_t s);
 
 namespace {
 thread_local hipEvent_t t_ev_before = nullptr;
@@ -63,6 +66,25 @@ padoc_status check_common(const padoc_plan* P, const void* q, const void* k, con
   if (ws_bytes < P->ws_bytes)
     return set_error(PADOC_ERR_WORKSPACE, "workspace of %zu bytes is smaller than the %zu the plan needs", ws_bytes,
                      P->ws_bytes);
+  return PADOC_OK;
+}
+
+// What a decode call refuses of its plan and caches (check_common aside): a
+// plan for packed K/V, one for caches of the other kind, and no block table.
+padoc_status check_decode(const padoc_plan* P, const padoc_cache_e4m3* cache, bool e4m3, const int32_t* block_table) {
+  if (P->kind != 1)
+    return set_error(PADOC_ERR_MODE, "plan was built for packed K/V (block_size 0); use padoc_tree_attn_fwd");
+  if (is_e4m3(P->dtype) != e4m3)
+    return e4m3 ? set_error(PADOC_ERR_DTYPE, "the plan is not for 8-bit caches")
+                : set_error(PADOC_ERR_DTYPE, "the plan is for 8-bit caches; use the e4m3 form of this call");
+  if (P->work.empty()) return PADOC_OK;
+  if (!block_table) return set_error(PADOC_ERR_ARG, "block_table is null");
+  if (!e4m3) return PADOC_OK;
+  if (!cache->scales) return set_error(PADOC_ERR_ARG, "scales is null");
+  if ((uintptr_t)cache->scales & 15) return set_error(PADOC_ERR_ARG, "scales must be 16-byte aligned");
+  if (cache->num_blocks != P->num_kv_rows)
+    return set_error(PADOC_ERR_BOUNDS, "the cache has %lld blocks, the plan is for %lld", (long long)cache->num_blocks,
+                     (long long)P->num_kv_rows);
   return PADOC_OK;
 }
 
@@ -149,9 +171,10 @@ padoc_status upload_schedule(const padoc_plan* P, void* ws, hipStream_t stream, 
 // profiling events around the kernels.
 // `pinned`: upload from the plan's pinned host copy (made on first use);
 // else straight from the plan's own host memory, allocating nothing.
+// `scales`: of 8-bit caches (k and v are codes), for plans of such a dtype.
 padoc_status run(const padoc_plan* P, const void* q, const void* k, const void* v, const int32_t* bt, void* o,
                  float* lse, void* ws, hipStream_t stream, bool upload = true, bool events = true,
-                 bool pinned = true) {
+                 bool pinned = true, const void* scales = nullptr) {
   if (P->work.empty()) return PADOC_OK;
   hipError_t e = hipSuccess;
   if (upload) {
@@ -176,15 +199,18 @@ padoc_status run(const padoc_plan* P, const void* q, const void* k, const void* 
   tp.Hkv = P->Hkv;
   tp.G = P->G;
   tp.scale_log2 = P->scale * 1.4426950408889634f;
-  const bool paged = P->block_size != 0;
+  tp.scales = static_cast<const uint8_t*>(scales);
+  const bool paged = P->block_size != 0, bf16 = row_dtype(P->dtype) == PADOC_BF16;
   const bool partial = P->kind == 1;  // decode plans: wave items, split-KV partials
   const int n_work = (int)P->work.size();
   if (events && t_ev_before && t_ev_after) {
     e = hipEventRecord(t_ev_before, stream);
     if (e != hipSuccess) return hip_fail("hipEventRecord", e);
   }
-  if (P->dtype == PADOC_BF16) {
-    if (!paged)
+  if (bf16) {
+    if (scales)
+      e = launch_decode_e4m3(tp, P->n_work_shared, n_work - P->n_work_shared, P->D, stream);
+    else if (!paged)
       e = launch_tile_mfma_bf16(tp, n_work, P->D, stream);
     else  // shared-key tile items and private-key items in one launch
       e = launch_decode_step_bf16(tp, P->n_work_shared, n_work - P->n_work_shared, P->n_private_groups,
@@ -207,7 +233,7 @@ padoc_status run(const padoc_plan* P, const void* q, const void* k, const void* 
     cp.Hkv = P->Hkv;
     cp.G = P->G;
     cp.next = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + P->off_next);
-    e = launch_lse_combine(cp, P->D, P->dtype == PADOC_BF16, stream);
+    e = launch_lse_combine(cp, P->D, bf16, stream);
     if (e != hipSuccess) return hip_fail("combine kernel launch", e);
   }
   if (events && t_ev_before && t_ev_after) {
@@ -237,11 +263,21 @@ extern "C" padoc_status padoc_branch_decode(const padoc_plan* plan, const void* 
                                             void* workspace, size_t workspace_bytes, hipStream_t stream) {
   clear_error();
   padoc_status st = check_common(plan, q, k_cache, v_cache, o, lse, workspace, workspace_bytes);
+  if (st == PADOC_OK) st = check_decode(plan, nullptr, false, block_table);
   if (st != PADOC_OK) return st;
-  if (plan->kind != 1)
-    return set_error(PADOC_ERR_MODE, "plan was built for packed K/V (block_size 0); use padoc_tree_attn_fwd");
-  if (!plan->work.empty() && !block_table) return set_error(PADOC_ERR_ARG, "block_table is null");
   return run(plan, q, k_cache, v_cache, block_table, o, lse, workspace, stream);
+}
+
+extern "C" padoc_status padoc_branch_decode_e4m3(const padoc_plan* plan, const void* q, const padoc_cache_e4m3* cache,
+                                                 const int32_t* block_table, void* o, float* lse, void* workspace,
+                                                 size_t workspace_bytes, hipStream_t stream) {
+  clear_error();
+  if (!cache) return set_error(PADOC_ERR_ARG, "cache is null");
+  padoc_status st = check_common(plan, q, cache->k, cache->v, o, lse, workspace, workspace_bytes);
+  if (st == PADOC_OK) st = check_decode(plan, cache, true, block_table);
+  if (st != PADOC_OK) return st;
+  return run(plan, q, cache->k, cache->v, block_table, o, lse, workspace, stream, /*upload=*/true, /*events=*/true,
+             /*pinned=*/true, cache->scales);
 }
 
 extern "C" padoc_status padoc_plan_upload(const padoc_plan* plan, void* workspace, size_t workspace_bytes,
@@ -258,25 +294,46 @@ extern "C" padoc_status padoc_plan_upload(const padoc_plan* plan, void* workspac
   return upload_schedule(plan, workspace, stream, /*pinned=*/true);
 }
 
+namespace padoc {
+namespace {
+// Whether workspace `ws` holds the plan's schedule as it is now.
+padoc_status check_resident(const padoc_plan* plan, const void* ws) {
+  std::lock_guard<std::mutex> lk(plan->pin_mu);
+  if (plan->up_ws != ws || plan->up_build != plan->build_id)
+    return set_error(PADOC_ERR_MODE,
+                     "the workspace does not hold this plan's schedule (upload it with padoc_plan_upload after "
+                     "every build of the plan)");
+  return PADOC_OK;
+}
+}  // namespace
+}  // namespace padoc
+
 extern "C" padoc_status padoc_branch_decode_resident(const padoc_plan* plan, const void* q, const void* k_cache,
                                                      const void* v_cache, const int32_t* block_table, void* o,
                                                      float* lse, void* workspace, size_t workspace_bytes,
                                                      hipStream_t stream) {
   clear_error();
   padoc_status st = check_common(plan, q, k_cache, v_cache, o, lse, workspace, workspace_bytes);
+  if (st == PADOC_OK) st = check_decode(plan, nullptr, false, block_table);
   if (st != PADOC_OK) return st;
-  if (plan->kind != 1)
-    return set_error(PADOC_ERR_MODE, "plan was built for packed K/V (block_size 0); use padoc_tree_attn_fwd");
-  if (!plan->work.empty() && !block_table) return set_error(PADOC_ERR_ARG, "block_table is null");
   if (plan->work.empty()) return PADOC_OK;
-  {
-    std::lock_guard<std::mutex> lk(plan->pin_mu);
-    if (plan->up_ws != workspace || plan->up_build != plan->build_id)
-      return set_error(PADOC_ERR_MODE,
-                       "the workspace does not hold this plan's schedule (upload it with padoc_plan_upload after "
-                       "every build of the plan)");
-  }
+  if ((st = check_resident(plan, workspace)) != PADOC_OK) return st;
   return run(plan, q, k_cache, v_cache, block_table, o, lse, workspace, stream, /*upload=*/false);
+}
+
+extern "C" padoc_status padoc_branch_decode_resident_e4m3(const padoc_plan* plan, const void* q,
+                                                          const padoc_cache_e4m3* cache, const int32_t* block_table,
+                                                          void* o, float* lse, void* workspace, size_t workspace_bytes,
+                                                          hipStream_t stream) {
+  clear_error();
+  if (!cache) return set_error(PADOC_ERR_ARG, "cache is null");
+  padoc_status st = check_common(plan, q, cache->k, cache->v, o, lse, workspace, workspace_bytes);
+  if (st == PADOC_OK) st = check_decode(plan, cache, true, block_table);
+  if (st != PADOC_OK) return st;
+  if (plan->work.empty()) return PADOC_OK;
+  if ((st = check_resident(plan, workspace)) != PADOC_OK) return st;
+  return run(plan, q, cache->k, cache->v, block_table, o, lse, workspace, stream, /*upload=*/false, /*events=*/true,
+             /*pinned=*/true, cache->scales);
 }
 
 // Workspace of padoc_branch_decode_no_alloc: one array per GPU the library
@@ -313,10 +370,12 @@ padoc_status scratch_of_current_device(void** out) {
 }  // namespace
 }  // namespace padoc
 
-extern "C" padoc_status padoc_branch_decode_no_alloc(const padoc_plan* plan, const void* q, const void* k_cache,
-                                                     const void* v_cache, const int32_t* block_table, void* o,
-                                                     float* lse, hipStream_t stream) {
-  clear_error();
+namespace padoc {
+namespace {
+// `cache`: of 8-bit caches (k_cache and v_cache are its), else null.
+padoc_status decode_no_alloc(const padoc_plan* plan, const void* q, const void* k_cache, const void* v_cache,
+                             const padoc_cache_e4m3* cache, const int32_t* block_table, void* o, float* lse,
+                             hipStream_t stream) {
   if (!plan) return set_error(PADOC_ERR_ARG, "plan is null");
   if (plan->kind != 1)
     return set_error(PADOC_ERR_MODE, "plan was built for packed K/V (block_size 0); use padoc_tree_attn_fwd");
@@ -329,10 +388,27 @@ extern "C" padoc_status padoc_branch_decode_no_alloc(const padoc_plan* plan, con
   padoc_status st = scratch_of_current_device(&ws);
   if (st != PADOC_OK) return st;
   st = check_common(plan, q, k_cache, v_cache, o, lse, ws, kNoAllocScratchBytes);
+  if (st == PADOC_OK) st = check_decode(plan, cache, cache != nullptr, block_table);
   if (st != PADOC_OK) return st;
-  if (!plan->work.empty() && !block_table) return set_error(PADOC_ERR_ARG, "block_table is null");
   return run(plan, q, k_cache, v_cache, block_table, o, lse, ws, stream, /*upload=*/true, /*events=*/true,
-             /*pinned=*/false);
+             /*pinned=*/false, cache ? cache->scales : nullptr);
+}
+}  // namespace
+}  // namespace padoc
+
+extern "C" padoc_status padoc_branch_decode_no_alloc(const padoc_plan* plan, const void* q, const void* k_cache,
+                                                     const void* v_cache, const int32_t* block_table, void* o,
+                                                     float* lse, hipStream_t stream) {
+  clear_error();
+  return decode_no_alloc(plan, q, k_cache, v_cache, nullptr, block_table, o, lse, stream);
+}
+
+extern "C" padoc_status padoc_branch_decode_no_alloc_e4m3(const padoc_plan* plan, const void* q,
+                                                          const padoc_cache_e4m3* cache, const int32_t* block_table,
+                                                          void* o, float* lse, hipStream_t stream) {
+  clear_error();
+  if (!cache) return set_error(PADOC_ERR_ARG, "cache is null");
+  return decode_no_alloc(plan, q, cache->k, cache->v, cache, block_table, o, lse, stream);
 }
 
 extern "C" padoc_status padoc_cache_from_rows(const void* k_rows, const void* v_rows, void* k_cache, void* v_cache,
@@ -483,6 +559,24 @@ extern "C" padoc_status padoc_rotary_append(const padoc_rotary* r, const padoc_r
   return record(t_ev_after, stream);
 }
 
+extern "C" padoc_status padoc_rotary_append_e4m3(const padoc_rotary* r, const padoc_rotary_append_args* a,
+                                                 const padoc_cache_e4m3* cache, hipStream_t stream) {
+  clear_error();
+  padoc_status st = check_rotary_append_e4m3(r, a, cache);
+  if (st != PADOC_OK) return st;
+  if ((a->n_q == 0 || a->num_heads_q == 0) && (a->n_new == 0 || a->num_heads_kv == 0)) return PADOC_OK;
+  RotaryParams p = append_params(r, a);
+  p.k_cache = cache->k;
+  p.v_cache = cache->v;
+  p.scales = static_cast<uint8_t*>(cache->scales);
+  p.n_blocks = cache->num_blocks;
+  if ((st = record(t_ev_before, stream)) != PADOC_OK) return st;
+  const hipError_t e =
+      launch_rotary_append_e4m3(p, r->D, r->dtype == PADOC_BF16, r->style == PADOC_ROTARY_PAIRS, stream);
+  if (e != hipSuccess) return hip_fail("rotary append kernel launch", e);
+  return record(t_ev_after, stream);
+}
+
 extern "C" padoc_status padoc_cache_copy_blocks(const void* k_src, const void* v_src, int64_t src_blocks, void* k_dst,
                                                 void* v_dst, int64_t dst_blocks, const int32_t* pairs, int64_t n_pairs,
                                                 const int32_t* pairs_host, int32_t num_heads_kv, int32_t head_dim,
@@ -492,10 +586,56 @@ extern "C" padoc_status padoc_cache_copy_blocks(const void* k_src, const void* v
                                       num_heads_kv, head_dim, dtype);
   if (st != PADOC_OK || n_pairs == 0) return st;
   CopyParams p{k_src, v_src, k_dst, v_dst, pairs, n_pairs, src_blocks, dst_blocks,
-               (int64_t)num_heads_kv * head_dim * (dtype == PADOC_BF16 ? 2 : 4)};
+               (int64_t)num_heads_kv * head_dim * (dtype == PADOC_BF16 ? 2 : 4), nullptr, nullptr, 0};
   if ((st = record(t_ev_before, stream)) != PADOC_OK) return st;
   const hipError_t e = launch_copy_blocks(p, stream);
   if (e != hipSuccess) return hip_fail("block copy kernel launch", e);
+  return record(t_ev_after, stream);
+}
+
+extern "C" padoc_status padoc_cache_copy_blocks_e4m3(const padoc_cache_e4m3* src, const padoc_cache_e4m3* dst,
+                                                     const int32_t* pairs, int64_t n_pairs, const int32_t* pairs_host,
+                                                     int32_t num_heads_kv, int32_t head_dim, hipStream_t stream) {
+  clear_error();
+  padoc_status st = check_copy_blocks_e4m3(src, dst, pairs, n_pairs, pairs_host, num_heads_kv, head_dim);
+  if (st != PADOC_OK || n_pairs == 0) return st;
+  const CopyParams p{src->k, src->v, dst->k, dst->v, pairs, n_pairs, src->num_blocks, dst->num_blocks,
+                     (int64_t)num_heads_kv * head_dim, src->scales, dst->scales, (int64_t)num_heads_kv * 2};
+  if ((st = record(t_ev_before, stream)) != PADOC_OK) return st;
+  const hipError_t e = launch_copy_blocks(p, stream);
+  if (e != hipSuccess) return hip_fail("block copy kernel launch", e);
+  return record(t_ev_after, stream);
+}
+
+extern "C" padoc_status padoc_cache_quantize(const void* k_src, const void* v_src, int64_t src_blocks,
+                                             const padoc_cache_e4m3* dst, const int32_t* pairs, int64_t n_pairs,
+                                             const int32_t* pairs_host, int32_t num_heads_kv, int32_t head_dim,
+                                             padoc_dtype dtype, hipStream_t stream) {
+  clear_error();
+  padoc_status st = check_cast_blocks(k_src, v_src, src_blocks, dst, dst ? dst->num_blocks : 0, src_blocks, pairs,
+                                      n_pairs, pairs_host, num_heads_kv, head_dim, dtype, /*back=*/false);
+  if (st != PADOC_OK || n_pairs == 0) return st;
+  const CastParams p{k_src, v_src, nullptr, nullptr, static_cast<uint8_t*>(dst->k), static_cast<uint8_t*>(dst->v),
+                     static_cast<uint8_t*>(dst->scales), pairs, n_pairs, src_blocks, dst->num_blocks, num_heads_kv};
+  if ((st = record(t_ev_before, stream)) != PADOC_OK) return st;
+  const hipError_t e = launch_cast_blocks(p, head_dim, dtype == PADOC_BF16, /*back=*/false, stream);
+  if (e != hipSuccess) return hip_fail("quantise kernel launch", e);
+  return record(t_ev_after, stream);
+}
+
+extern "C" padoc_status padoc_cache_dequantize(const padoc_cache_e4m3* src, void* k_dst, void* v_dst,
+                                               int64_t dst_blocks, const int32_t* pairs, int64_t n_pairs,
+                                               const int32_t* pairs_host, int32_t num_heads_kv, int32_t head_dim,
+                                               padoc_dtype dtype, hipStream_t stream) {
+  clear_error();
+  padoc_status st = check_cast_blocks(k_dst, v_dst, dst_blocks, src, dst_blocks, src ? src->num_blocks : 0, pairs,
+                                      n_pairs, pairs_host, num_heads_kv, head_dim, dtype, /*back=*/true);
+  if (st != PADOC_OK || n_pairs == 0) return st;
+  const CastParams p{nullptr, nullptr, k_dst, v_dst, static_cast<uint8_t*>(src->k), static_cast<uint8_t*>(src->v),
+                     static_cast<uint8_t*>(src->scales), pairs, n_pairs, src->num_blocks, dst_blocks, num_heads_kv};
+  if ((st = record(t_ev_before, stream)) != PADOC_OK) return st;
+  const hipError_t e = launch_cast_blocks(p, head_dim, dtype == PADOC_BF16, /*back=*/true, stream);
+  if (e != hipSuccess) return hip_fail("dequantise kernel launch", e);
   return record(t_ev_after, stream);
 }
 
@@ -608,11 +748,15 @@ padoc_status launch_step(padoc_session* s, const void* q, const void* k_new, con
   if (((uintptr_t)d.k_cache | (uintptr_t)d.v_cache) & 15)
     return set_error(PADOC_ERR_ARG, "the caches must be 16-byte aligned");
   const int64_t n_new = s->new_off.back(), n_q = s->q_off.back();
-  const size_t esz = d.dtype == PADOC_BF16 ? 2 : 4;
+  const bool e4m3 = is_e4m3(d.dtype);
+  const padoc_dtype row_type = row_dtype(d.dtype);
+  const size_t esz = row_type == PADOC_BF16 ? 2 : 4;
+  if (e4m3 && d.num_blocks > 0 && !s->scales)
+    return set_error(PADOC_ERR_ARG, "the session's 8-bit caches have no scales (padoc_session_set_scales)");
   if (rows) {
     if (rotary->D != d.head_dim || rows->num_heads_q != d.num_heads_q || rows->num_heads_kv != d.num_heads_kv)
       return set_error(PADOC_ERR_SHAPE, "the rotary's head_dim or the rows' head counts are not the session's");
-    if (rotary->dtype != d.dtype) return set_error(PADOC_ERR_DTYPE, "the rotary's dtype is not the session's");
+    if (rotary->dtype != row_type) return set_error(PADOC_ERR_DTYPE, "the rotary's dtype is not the session's");
     if (rows->n_q != n_q || rows->n_new != n_new)
       return set_error(PADOC_ERR_BOUNDS, "%lld query rows and %lld new rows, the prepared step has %lld and %lld",
                        (long long)rows->n_q, (long long)rows->n_new, (long long)n_q, (long long)n_new);
@@ -683,7 +827,8 @@ padoc_status launch_step(padoc_session* s, const void* q, const void* k_new, con
     const int32_t c0 = s->copy_ptr[ph];
     const CopyParams cp{d.k_cache, d.v_cache, d.k_cache, d.v_cache, at<int32_t>(ws, s->off_copy) + 2 * (int64_t)c0,
                         s->copy_ptr[ph + 1] - c0, d.num_blocks, d.num_blocks,
-                        (int64_t)d.num_heads_kv * d.head_dim * (int64_t)esz};
+                        (int64_t)d.num_heads_kv * d.head_dim * (e4m3 ? 1 : (int64_t)esz), s->scales, s->scales,
+                        e4m3 ? 2 * (int64_t)d.num_heads_kv : 0};
     e = launch_copy_blocks(cp, stream);
     if (e != hipSuccess) return hip_fail("block copy kernel launch", e);
   }
@@ -696,15 +841,36 @@ padoc_status launch_step(padoc_session* s, const void* q, const void* k_new, con
     rp.patch = at<int32_t>(ws, s->off_patch);
     rp.n_patch = n_patch;
     rp.block_table = d.block_table;
-    e = launch_rotary_append(rp, rotary->D, d.dtype == PADOC_BF16, rotary->style == PADOC_ROTARY_PAIRS, stream);
+    rp.scales = static_cast<uint8_t*>(s->scales);
+    e = (e4m3 ? launch_rotary_append_e4m3 : launch_rotary_append)(rp, rotary->D, row_type == PADOC_BF16,
+                                                                  rotary->style == PADOC_ROTARY_PAIRS, stream);
     if (e != hipSuccess) return hip_fail("rotary append kernel launch", e);
+  } else if (e4m3 && (n_new > 0 || n_patch > 0)) {
+    // rows as they are: an append that turns no pair and has no queries
+    RotaryParams rp{};
+    const int64_t H = d.num_heads_kv, D = d.head_dim;
+    rp.scale = 1.f;
+    rp.n = (int32_t)n_new;
+    rp.Hkv = d.num_heads_kv;
+    rp.k = padoc_heads{const_cast<void*>(k_new), H * D, D};
+    rp.v = padoc_heads{const_cast<void*>(v_new), H * D, D};
+    rp.slots = at<int32_t>(ws, 0);
+    rp.k_cache = d.k_cache;
+    rp.v_cache = d.v_cache;
+    rp.scales = static_cast<uint8_t*>(s->scales);
+    rp.n_blocks = d.num_blocks;
+    rp.patch = at<int32_t>(ws, s->off_patch);
+    rp.n_patch = n_patch;
+    rp.block_table = d.block_table;
+    e = launch_rotary_append_e4m3(rp, d.head_dim, row_type == PADOC_BF16, /*pairs=*/false, stream);
+    if (e != hipSuccess) return hip_fail("append kernel launch", e);
   } else if (n_new > 0 || n_patch > 0) {
     e = launch_append_kv(k_new, v_new, d.k_cache, d.v_cache, at<int32_t>(ws, 0), n_new, d.num_heads_kv, d.head_dim,
                          d.dtype == PADOC_BF16, at<int32_t>(ws, s->off_patch), n_patch, d.block_table, stream);
     if (e != hipSuccess) return hip_fail("append kernel launch", e);
   }
   padoc_status st = run(P, q, d.k_cache, d.v_cache, d.block_table, o, lse, ws + s->ws_records, stream,
-                        /*upload=*/false, /*events=*/false);
+                        /*upload=*/false, /*events=*/false, /*pinned=*/true, s->scales);
   if (st != PADOC_OK) return st;
   if (t_ev_before && t_ev_after) {
     e = hipEventRecord(t_ev_after, stream);

@@ -321,8 +321,10 @@ class Builder {
 padoc_status validate(const padoc_tree_desc* d) {
   if (d->n_seg < 0) return set_error(PADOC_ERR_ARG, "n_seg = %d is negative", d->n_seg);
   if (d->n_seg > 0 && !d->seg) return set_error(PADOC_ERR_ARG, "seg is null with n_seg = %d", d->n_seg);
-  if (d->dtype != PADOC_F32 && d->dtype != PADOC_BF16)
-    return set_error(PADOC_ERR_DTYPE, "dtype %d is not PADOC_F32 or PADOC_BF16", (int)d->dtype);
+  if (d->dtype != PADOC_F32 && d->dtype != PADOC_BF16 && !padoc::is_e4m3(d->dtype))
+    return set_error(PADOC_ERR_DTYPE, "dtype %d is not a padoc_dtype", (int)d->dtype);
+  if (padoc::is_e4m3(d->dtype) && d->block_size == 0)
+    return set_error(PADOC_ERR_DTYPE, "8-bit caches are paged: block_size must be 16");
   if (d->num_heads_q <= 0 || d->num_heads_kv <= 0)
     return set_error(PADOC_ERR_SHAPE, "head counts must be positive (Hq=%d, Hkv=%d)", d->num_heads_q,
                      d->num_heads_kv);
@@ -1018,7 +1020,7 @@ void serialise(padoc_plan& P) {
   P.off_ranges = align256(P.off_work + P.work.size() * sizeof(padoc::WorkRec));
   // decode, bf16: each tile item's first range once more, at the item's index,
   // with the item's number of tiles in its reserved field
-  const size_t n_first = P.kind == 1 && P.dtype == PADOC_BF16 ? (size_t)P.n_work_shared : 0;
+  const size_t n_first = P.kind == 1 && row_dtype(P.dtype) == PADOC_BF16 ? (size_t)P.n_work_shared : 0;
   P.off_first = align256(P.off_ranges + P.ranges.size() * sizeof(padoc::RangeRec));
   P.off_lims = align256(P.off_first + n_first * sizeof(padoc::RangeRec));
   P.off_toks = align256(P.off_lims + P.lims.size() * 4);

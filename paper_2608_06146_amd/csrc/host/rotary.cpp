@@ -116,6 +116,65 @@ padoc_status check_sizes(int64_t n, int32_t Hq, int32_t Hkv) {
   return PADOC_OK;
 }
 
+// The host copy of a call's block pairs: ids in range, no destination twice, and
+// (`within` one cache) no block both source and destination.
+padoc_status check_pairs_host(const int32_t* pairs_host, int64_t n_pairs, int64_t src_blocks, int64_t dst_blocks,
+                              bool within) {
+  if (!pairs_host) return PADOC_OK;
+  try {
+    std::vector<int32_t> src((size_t)n_pairs), dst((size_t)n_pairs);
+    for (int64_t i = 0; i < n_pairs; ++i) {
+      src[i] = pairs_host[2 * i];
+      dst[i] = pairs_host[2 * i + 1];
+      if (src[i] < 0 || src[i] >= src_blocks || dst[i] < 0 || dst[i] >= dst_blocks)
+        return set_error(PADOC_ERR_BOUNDS, "pair %lld: blocks (%d, %d) outside [0, %lld) and [0, %lld)", (long long)i,
+                         src[i], dst[i], (long long)src_blocks, (long long)dst_blocks);
+    }
+    std::sort(dst.begin(), dst.end());
+    const auto twice = std::adjacent_find(dst.begin(), dst.end());
+    if (twice != dst.end()) return set_error(PADOC_ERR_BOUNDS, "block %d is a destination twice", *twice);
+    if (within) {
+      std::sort(src.begin(), src.end());
+      for (int32_t b : src)
+        if (std::binary_search(dst.begin(), dst.end(), b))
+          return set_error(PADOC_ERR_BOUNDS, "block %d is a source and a destination", b);
+    }
+  } catch (const std::bad_alloc&) {
+    return set_error(PADOC_ERR_ARG, "out of host memory");
+  }
+  return PADOC_OK;
+}
+
+// Sizes of a call on blocks.
+padoc_status check_block_sizes(int64_t src_blocks, int64_t dst_blocks, int64_t n_pairs, int32_t Hkv, int32_t D) {
+  if (D != 64 && D != 128) return set_error(PADOC_ERR_SHAPE, "head_dim=%d is not 64 or 128", D);
+  if (Hkv < 1 || Hkv > kMaxHeads) return set_error(PADOC_ERR_SHAPE, "Hkv=%d outside [1, %d]", Hkv, kMaxHeads);
+  if (n_pairs < 0) return set_error(PADOC_ERR_ARG, "n_pairs = %lld is negative", (long long)n_pairs);
+  if (n_pairs > kI32Max) return set_error(PADOC_ERR_BOUNDS, "%lld pairs exceed 2^31-1", (long long)n_pairs);
+  if (src_blocks < 0 || src_blocks > kI32Max || dst_blocks < 0 || dst_blocks > kI32Max)
+    return set_error(PADOC_ERR_ARG, "block counts (%lld, %lld) must be in [0, 2^31-1]", (long long)src_blocks,
+                     (long long)dst_blocks);
+  return PADOC_OK;
+}
+
+// Device memory of a call: `bytes` bytes from `p` on.
+struct Span {
+  const char* name;
+  const void* p;
+  int64_t bytes;
+};
+padoc_status check_spans(const Span* s, int n) {
+  for (int i = 0; i < n; ++i) {
+    if (!s[i].p) return set_error(PADOC_ERR_ARG, "%s is null", s[i].name);
+    if ((uintptr_t)s[i].p & 15) return set_error(PADOC_ERR_ARG, "%s must be 16-byte aligned", s[i].name);
+    for (int j = 0; j < i; ++j)
+      if ((uintptr_t)s[i].p < (uintptr_t)s[j].p + (uintptr_t)s[j].bytes &&
+          (uintptr_t)s[j].p < (uintptr_t)s[i].p + (uintptr_t)s[i].bytes)
+        return set_error(PADOC_ERR_ARG, "%s overlaps %s", s[i].name, s[j].name);
+  }
+  return PADOC_OK;
+}
+
 #define PADOC_TRY(expr)                     \
   do {                                      \
     const padoc_status st_ = (expr);        \
@@ -235,13 +294,7 @@ padoc_status check_copy_blocks(const void* k_src, const void* v_src, int64_t src
                                const int32_t* pairs_host, int32_t Hkv, int32_t D, padoc_dtype dtype) {
   if (dtype != PADOC_F32 && dtype != PADOC_BF16)
     return set_error(PADOC_ERR_DTYPE, "dtype %d is not PADOC_F32 or PADOC_BF16", (int)dtype);
-  if (D != 64 && D != 128) return set_error(PADOC_ERR_SHAPE, "head_dim=%d is not 64 or 128", D);
-  if (Hkv < 1 || Hkv > kMaxHeads) return set_error(PADOC_ERR_SHAPE, "Hkv=%d outside [1, %d]", Hkv, kMaxHeads);
-  if (n_pairs < 0) return set_error(PADOC_ERR_ARG, "n_pairs = %lld is negative", (long long)n_pairs);
-  if (n_pairs > kI32Max) return set_error(PADOC_ERR_BOUNDS, "%lld pairs exceed 2^31-1", (long long)n_pairs);
-  if (src_blocks < 0 || src_blocks > kI32Max || dst_blocks < 0 || dst_blocks > kI32Max)
-    return set_error(PADOC_ERR_ARG, "block counts (%lld, %lld) must be in [0, 2^31-1]", (long long)src_blocks,
-                     (long long)dst_blocks);
+  PADOC_TRY(check_block_sizes(src_blocks, dst_blocks, n_pairs, Hkv, D));
   if (n_pairs == 0) return PADOC_OK;
   if (!k_src || !v_src || !k_dst || !v_dst || !pairs) return set_error(PADOC_ERR_ARG, "null buffer pointer");
   if (((uintptr_t)k_src | (uintptr_t)v_src | (uintptr_t)k_dst | (uintptr_t)v_dst) & 15)
@@ -259,30 +312,68 @@ padoc_status check_copy_blocks(const void* k_src, const void* v_src, int64_t src
         if ((uintptr_t)s < (uintptr_t)d + dn && (uintptr_t)d < (uintptr_t)s + sn)
           return set_error(PADOC_ERR_ARG, "source and destination caches overlap without being the same");
   }
-  if (pairs_host) {
-    try {
-      std::vector<int32_t> src((size_t)n_pairs), dst((size_t)n_pairs);
-      for (int64_t i = 0; i < n_pairs; ++i) {
-        src[i] = pairs_host[2 * i];
-        dst[i] = pairs_host[2 * i + 1];
-        if (src[i] < 0 || src[i] >= src_blocks || dst[i] < 0 || dst[i] >= dst_blocks)
-          return set_error(PADOC_ERR_BOUNDS, "pair %lld: blocks (%d, %d) outside [0, %lld) and [0, %lld)", (long long)i,
-                           src[i], dst[i], (long long)src_blocks, (long long)dst_blocks);
-      }
-      std::sort(dst.begin(), dst.end());
-      const auto twice = std::adjacent_find(dst.begin(), dst.end());
-      if (twice != dst.end()) return set_error(PADOC_ERR_BOUNDS, "block %d is a destination twice", *twice);
-      if (k_src == k_dst) {
-        std::sort(src.begin(), src.end());
-        for (int32_t b : src)
-          if (std::binary_search(dst.begin(), dst.end(), b))
-            return set_error(PADOC_ERR_BOUNDS, "block %d is a source and a destination", b);
-      }
-    } catch (const std::bad_alloc&) {
-      return set_error(PADOC_ERR_ARG, "out of host memory");
-    }
-  }
-  return PADOC_OK;
+  return check_pairs_host(pairs_host, n_pairs, src_blocks, dst_blocks, k_src == k_dst);
+}
+
+padoc_status check_copy_blocks_e4m3(const padoc_cache_e4m3* src, const padoc_cache_e4m3* dst, const int32_t* pairs,
+                                    int64_t n_pairs, const int32_t* pairs_host, int32_t Hkv, int32_t D) {
+  if (!src || !dst) return set_error(PADOC_ERR_ARG, "src or dst is null");
+  PADOC_TRY(check_block_sizes(src->num_blocks, dst->num_blocks, n_pairs, Hkv, D));
+  if (n_pairs == 0) return PADOC_OK;
+  if (!pairs) return set_error(PADOC_ERR_ARG, "pairs is null");
+  if ((uintptr_t)pairs & 3) return set_error(PADOC_ERR_ARG, "pairs must be 4-byte aligned");
+  const int64_t codes = (int64_t)Hkv * 16 * D, bytes = (int64_t)Hkv * 32;
+  const Span spans[6] = {{"k of src", src->k, src->num_blocks * codes}, {"v of src", src->v, src->num_blocks * codes},
+                         {"scales of src", src->scales, src->num_blocks * bytes},
+                         {"k of dst", dst->k, dst->num_blocks * codes}, {"v of dst", dst->v, dst->num_blocks * codes},
+                         {"scales of dst", dst->scales, dst->num_blocks * bytes}};
+  const bool within = src->k == dst->k && src->v == dst->v && src->scales == dst->scales;
+  PADOC_TRY(check_spans(spans, within ? 3 : 6));
+  if (within && src->num_blocks != dst->num_blocks)
+    return set_error(PADOC_ERR_ARG, "one cache with two block counts (%lld, %lld)", (long long)src->num_blocks,
+                     (long long)dst->num_blocks);
+  return check_pairs_host(pairs_host, n_pairs, src->num_blocks, dst->num_blocks, within);
+}
+
+padoc_status check_cast_blocks(const void* k, const void* v, int64_t blocks, const padoc_cache_e4m3* cache,
+                               int64_t dst_blocks, int64_t src_blocks, const int32_t* pairs, int64_t n_pairs,
+                               const int32_t* pairs_host, int32_t Hkv, int32_t D, padoc_dtype dtype, bool back) {
+  if (!cache) return set_error(PADOC_ERR_ARG, "%s is null", back ? "src" : "dst");
+  if (dtype != PADOC_F32 && dtype != PADOC_BF16)
+    return set_error(PADOC_ERR_DTYPE, "dtype %d is not PADOC_F32 or PADOC_BF16", (int)dtype);
+  PADOC_TRY(check_block_sizes(src_blocks, dst_blocks, n_pairs, Hkv, D));
+  if (!pairs && n_pairs > std::min(src_blocks, dst_blocks))
+    return set_error(PADOC_ERR_BOUNDS, "%lld blocks without pairs, of caches of %lld and %lld", (long long)n_pairs,
+                     (long long)src_blocks, (long long)dst_blocks);
+  if (!pairs && pairs_host) return set_error(PADOC_ERR_ARG, "pairs_host without pairs");
+  if (n_pairs == 0) return PADOC_OK;
+  if ((uintptr_t)pairs & 3) return set_error(PADOC_ERR_ARG, "pairs must be 4-byte aligned");
+  const int64_t codes = (int64_t)Hkv * 16 * D, values = codes * (dtype == PADOC_BF16 ? 2 : 4);
+  const Span spans[5] = {{back ? "k_dst" : "k_src", k, blocks * values}, {back ? "v_dst" : "v_src", v, blocks * values},
+                         {"k of the 8-bit cache", cache->k, cache->num_blocks * codes},
+                         {"v of the 8-bit cache", cache->v, cache->num_blocks * codes},
+                         {"scales of the 8-bit cache", cache->scales, cache->num_blocks * Hkv * 32}};
+  PADOC_TRY(check_spans(spans, 5));
+  return check_pairs_host(pairs_host, n_pairs, src_blocks, dst_blocks, false);
+}
+
+padoc_status check_rotary_append_e4m3(const padoc_rotary* r, const padoc_rotary_append_args* a,
+                                      const padoc_cache_e4m3* cache) {
+  if (!a) return set_error(PADOC_ERR_ARG, "args is null");
+  if (!cache) return set_error(PADOC_ERR_ARG, "cache is null");
+  if (a->k_cache || a->v_cache || a->num_blocks)
+    return set_error(PADOC_ERR_ARG, "k_cache, v_cache and num_blocks are the 8-bit cache's and must be 0");
+  padoc_rotary_append_args rows = *a;
+  rows.k_cache = cache->k;
+  rows.v_cache = cache->v;
+  rows.num_blocks = cache->num_blocks;
+  PADOC_TRY(check_rotary_append(r, &rows, /*session=*/false));
+  if (a->n_new == 0 || a->num_heads_kv == 0) return PADOC_OK;
+  const int64_t codes = (int64_t)a->num_heads_kv * 16 * r->D;
+  const Span spans[3] = {{"k of the cache", cache->k, cache->num_blocks * codes},
+                         {"v of the cache", cache->v, cache->num_blocks * codes},
+                         {"scales of the cache", cache->scales, cache->num_blocks * a->num_heads_kv * 32}};
+  return check_spans(spans, 3);
 }
 
 }  // namespace padoc

@@ -22,4 +22,14 @@ padoc_status check_copy_blocks(const void* k_src, const void* v_src, int64_t src
                                const void* v_dst, int64_t dst_blocks, const int32_t* pairs, int64_t n_pairs,
                                const int32_t* pairs_host, int32_t Hkv, int32_t D, padoc_dtype dtype);
 
+padoc_status check_rotary_append_e4m3(const padoc_rotary* r, const padoc_rotary_append_args* a,
+                                      const padoc_cache_e4m3* cache);
+padoc_status check_copy_blocks_e4m3(const padoc_cache_e4m3* src, const padoc_cache_e4m3* dst, const int32_t* pairs,
+                                    int64_t n_pairs, const int32_t* pairs_host, int32_t Hkv, int32_t D);
+// Blocks between caches k, v of `blocks` blocks in `dtype` and an 8-bit cache
+// (`back`: from it), whose counts in the call's direction are src and dst.
+padoc_status check_cast_blocks(const void* k, const void* v, int64_t blocks, const padoc_cache_e4m3* cache,
+                               int64_t dst_blocks, int64_t src_blocks, const int32_t* pairs, int64_t n_pairs,
+                               const int32_t* pairs_host, int32_t Hkv, int32_t D, padoc_dtype dtype, bool back);
+
 }  // namespace padoc

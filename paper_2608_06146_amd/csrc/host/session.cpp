@@ -173,8 +173,8 @@ extern "C" padoc_status padoc_session_create(const padoc_session_desc* d, padoc_
   if (!out) return set_error(PADOC_ERR_ARG, "out is null");
   *out = nullptr;
   if (!d) return set_error(PADOC_ERR_ARG, "desc is null");
-  if (d->dtype != PADOC_F32 && d->dtype != PADOC_BF16)
-    return set_error(PADOC_ERR_DTYPE, "dtype %d is not PADOC_F32 or PADOC_BF16", (int)d->dtype);
+  if (d->dtype != PADOC_F32 && d->dtype != PADOC_BF16 && !padoc::is_e4m3(d->dtype))
+    return set_error(PADOC_ERR_DTYPE, "dtype %d is not a padoc_dtype", (int)d->dtype);
   if (d->num_blocks < 0 || d->num_blocks > kI32Max)
     return set_error(PADOC_ERR_ARG, "num_blocks=%lld must be in [0, 2^31-1]", (long long)d->num_blocks);
   if (d->block_table_capacity < 0 || d->block_table_capacity > kI32Max)
@@ -376,6 +376,18 @@ extern "C" padoc_status padoc_session_compact(padoc_session* s, int32_t max_move
   return PADOC_OK;
 }
 
+extern "C" padoc_status padoc_session_set_scales(padoc_session* s, void* scales) {
+  clear_error();
+  padoc_status st = check_session(s);
+  if (st != PADOC_OK) return st;
+  if (!padoc::is_e4m3(s->desc.dtype)) return set_error(PADOC_ERR_DTYPE, "the session's caches are not 8-bit caches");
+  if ((uintptr_t)scales & 15) return set_error(PADOC_ERR_ARG, "scales must be 16-byte aligned");
+  if (scales && (scales == s->desc.k_cache || scales == s->desc.v_cache))
+    return set_error(PADOC_ERR_ARG, "scales and codes must be distinct buffers");
+  s->scales = scales;
+  return PADOC_OK;
+}
+
 extern "C" padoc_status padoc_session_resize(padoc_session* s, int64_t num_blocks, void* k_cache, void* v_cache) {
   clear_error();
   padoc_status st = check_session(s);
@@ -413,6 +425,7 @@ extern "C" padoc_status padoc_session_resize(padoc_session* s, int64_t num_block
     s->desc.num_blocks = num_blocks;
     s->desc.k_cache = k_cache;
     s->desc.v_cache = v_cache;
+    s->scales = nullptr;  // of the caches before
   } catch (const std::bad_alloc&) {
     return set_error(PADOC_ERR_ARG, "out of host memory");
   }

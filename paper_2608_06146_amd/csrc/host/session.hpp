@@ -12,6 +12,7 @@
 
 struct padoc_session {
   padoc_session_desc desc{};
+  void* scales = nullptr;  // 8-bit caches
 
   struct Stream {
     int32_t parent = -1, fork = 0, len = 0;

@@ -20,6 +20,8 @@ constexpr int kThreads = 256, kUnroll = 2;
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 // Items: pieces of kThreads * kUnroll units, then the tensor, then the pair.
+// SCALES: of 8-bit caches, whose scales the workgroup of K's first piece copies.
+template <bool SCALES>
 __global__ __launch_bounds__(kThreads) void copy_blocks_kernel(const CopyParams p, int64_t pieces, int64_t items) {
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     const int64_t rest = item / pieces, piece = item - rest * pieces, pair = rest / 2;
@@ -35,6 +37,9 @@ __global__ __launch_bounds__(kThreads) void copy_blocks_kernel(const CopyParams 
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i)
       if (u0 + i * kThreads < p.units) __builtin_nontemporal_store(x[i], dst + u0 + i * kThreads);
+    if (SCALES && piece == 0 && rest % 2 == 0)
+      for (int64_t u = threadIdx.x; u < p.s_units; u += kThreads)
+        static_cast<u32x4*>(p.s_dst)[to * p.s_units + u] = static_cast<const u32x4*>(p.s_src)[from * p.s_units + u];
   }
 }
 
@@ -45,7 +50,10 @@ hipError_t launch_copy_blocks(const CopyParams& p, hipStream_t s) {
   const int64_t pieces = (p.units + kThreads * kUnroll - 1) / (kThreads * kUnroll);
   const int64_t items = p.n_pairs * 2 * pieces;
   const dim3 grid((unsigned)(items < (1 << 20) ? items : 1 << 20));
-  hipLaunchKernelGGL(copy_blocks_kernel, grid, dim3(kThreads), 0, s, p, pieces, items);
+  if (p.s_units)
+    hipLaunchKernelGGL(copy_blocks_kernel<true>, grid, dim3(kThreads), 0, s, p, pieces, items);
+  else
+    hipLaunchKernelGGL(copy_blocks_kernel<false>, grid, dim3(kThreads), 0, s, p, pieces, items);
   return hipGetLastError();
 }
 

@@ -28,6 +28,7 @@
 
 #include "../rotary.hpp"
 #include "device_common.hpp"
+#include "e4m3.hpp"
 
 namespace padoc {
 namespace {
@@ -617,6 +618,87 @@ __global__ __launch_bounds__(kThreads) void rotary_append_kernel(const RotaryPar
   }
 }
 
+// Maximum over the eight lanes of a group, in every one of them.
+__device__ __forceinline__ uint32_t group_max(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xf, 0xf, true));
+  return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xf, 0xf, true));
+}
+
+// The codes of a row that a group holds, and its scale byte.
+template <int N>
+__device__ __forceinline__ uint32_t quantize_row(const float (&x)[N], uint32_t (&codes)[N / 4], uint32_t nan_codes) {
+  uint32_t a = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) a = max(a, __float_as_uint(x[i]) & 0x7fffffffu);
+  const uint32_t b = e4m3::scale_byte(group_max(a));
+  const float r = e4m3::inverse_scale(b);
+#pragma unroll
+  for (int i = 0; i < N; i += 4)
+    codes[i / 4] = b == e4m3::kNan ? nan_codes : e4m3::codes4(x[i], x[i + 1], x[i + 2], x[i + 3], r);
+  return b;
+}
+
+// Append into an 8-bit cache: items of four roles, as above, but v's tiles are
+// cut like k's: a group takes a row of one head, and its lanes leave a byte per
+// dimension (d-major V).
+template <typename T, int D, bool PAIRS, bool STREAM>
+__global__ __launch_bounds__(kThreads) void rotary_append_e4m3_kernel(const RotaryParams p) {
+  __shared__ AngleTable<T, D, PAIRS> table;
+  constexpr int E = kUnit<T>;
+  const Place<T, D, PAIRS> pl(p.pairs);
+  const int64_t n_q = p.tiles_q.items, n_turned = n_q + p.tiles_k.items;
+  for (int64_t b = blockIdx.x; b < p.items; b += gridDim.x) {
+    if (b >= n_turned + p.items_v) {
+      const int64_t e = (b - n_turned - p.items_v) * kThreads + threadIdx.x;
+      if (e < p.n_patch) p.block_table[p.patch[2 * e]] = p.patch[2 * e + 1];
+      continue;
+    }
+    if (b >= n_turned) {
+      Tile t = tile_of(p, b - n_turned + n_q);  // (k's tile of the same rows and heads)
+      t.in = p.v;
+      const int dr = kGroups / t.heads, dh = kGroups - dr * t.heads;
+      for (Cursor c(t, threadIdx.x / kLanes); c.row < t.rows; c.next(t, dr, dh)) {
+        Raw<T, D> raw;
+        raw.template load<STREAM>(c.at<const T>(t.in, t), pl.at);
+        float x[kElems<D>];
+        raw.get(x);
+        uint32_t codes[kElems<D> / 4];
+        const uint32_t scale = quantize_row(x, codes, 0);
+        int32_t blk, slot;
+        if (!slot_of(p, t.row0 + c.row, blk, slot)) continue;
+        const int h = t.h0 + c.h;
+        uint8_t* dst = static_cast<uint8_t*>(p.v_cache) + e4m3::codes_at<D>(blk, h, p.Hkv) + slot;
+#pragma unroll
+        for (int i = 0; i < kElems<D>; ++i) dst[(pl.at[i / E] + i % E) * kBlock] = (uint8_t)(codes[i / 4] >> (8 * (i % 4)));
+        if (threadIdx.x % kLanes == 0) p.scales[e4m3::scales_at(blk, h, p.Hkv) + kBlock + slot] = (uint8_t)scale;
+      }
+      continue;
+    }
+    const Tile t = tile_of(p, b);
+    const bool is_q = b < n_q;
+    turn_tile<STREAM>(p, t, is_q ? p.q_pos : p.pos, is_q ? p.q_pos_stride : p.pos_stride, table, pl,
+              [&](const Cursor& c, const float (&x)[kElems<D>]) {
+      if (is_q) {
+        store_row(c.at<T>(t.out, t), pl.at, x);
+        return;
+      }
+      uint32_t codes[kElems<D> / 4];
+      const uint32_t scale = quantize_row(x, codes, e4m3::kNanCodes);
+      int32_t blk, slot;
+      if (!slot_of(p, t.row0 + c.row, blk, slot)) return;
+      const int h = t.h0 + c.h;
+      uint8_t* dst = static_cast<uint8_t*>(p.k_cache) + e4m3::codes_at<D>(blk, h, p.Hkv);
+#pragma unroll
+      for (int u = 0; u < kUnits<T, D>; ++u)
+#pragma unroll
+        for (int i = 0; i < E; i += 4)
+          *reinterpret_cast<uint32_t*>(dst + e4m3::k_at(slot, pl.at[u] + i)) = codes[(u * E + i) / 4];
+      if (threadIdx.x % kLanes == 0) p.scales[e4m3::scales_at(blk, h, p.Hkv) + slot] = (uint8_t)scale;
+    });
+  }
+}
+
 constexpr int64_t kMaxGrid = 1 << 20;  // workgroups of a launch: the rest by strides
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -675,6 +757,16 @@ struct Append {
   struct Call {
     static void go(const RotaryParams& p, dim3 grid, hipStream_t s) {
       hipLaunchKernelGGL((rotary_append_kernel<T, D, PAIRS, ROWS, STREAM>), grid, dim3(kThreads), 0, s, p);
+    }
+  };
+};
+
+template <bool STREAM>
+struct AppendE4m3 {
+  template <typename T, int D, bool PAIRS>
+  struct Call {
+    static void go(const RotaryParams& p, dim3 grid, hipStream_t s) {
+      hipLaunchKernelGGL((rotary_append_e4m3_kernel<T, D, PAIRS, STREAM>), grid, dim3(kThreads), 0, s, p);
     }
   };
 };
@@ -755,6 +847,17 @@ hipError_t launch_rotary_append(RotaryParams p, int D, bool bf16, bool pairs, hi
   return streams(((int64_t)p.n_q * p.Hq + (int64_t)p.n * p.Hkv * 2) * 2, D, bf16)
              ? dispatch<Append<64, true>::Call>(p, D, bf16, pairs, grid, s)
              : dispatch<Append<64, false>::Call>(p, D, bf16, pairs, grid, s);
+}
+
+hipError_t launch_rotary_append_e4m3(RotaryParams p, int D, bool bf16, bool pairs, hipStream_t s) {
+  p.tiles_q = tile_grid(p.n_q, p.Hq, p.Hq + p.Hkv, 4, 4 * kComputeUnits);
+  p.tiles_k = tile_grid(p.n, p.Hkv, p.Hq + p.Hkv, 4, 4 * kComputeUnits);
+  p.items_v = p.tiles_k.items;
+  p.items = p.items_v + p.tiles_q.items + p.tiles_k.items + ceil_div(p.n_patch, kThreads);
+  if (p.items == 0) return hipSuccess;
+  return streams((int64_t)p.n_q * p.Hq * 2 + (int64_t)p.n * p.Hkv * 3, D, bf16)
+             ? dispatch<AppendE4m3<true>::Call>(p, D, bf16, pairs, grid_of(p.items), s)
+             : dispatch<AppendE4m3<false>::Call>(p, D, bf16, pairs, grid_of(p.items), s);
 }
 
 }  // namespace padoc

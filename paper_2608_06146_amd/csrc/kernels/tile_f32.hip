@@ -41,9 +41,14 @@
 //                   is V[dim 16db+r][4 tokens of the group].
 // A wavefront's loads are whole 64-byte lines either way (paged: 1 KB
 // contiguous).
+//
+// 8-bit caches (E4M3): the same with a dword of four codes for every float4,
+// tokens in their order; K's scale multiplies the score (a power of two: the
+// score is that of the scaled row), V's the probability of its key.
 #include <type_traits>
 
 #include "device_common.hpp"
+#include "e4m3.hpp"
 
 namespace padoc {
 
@@ -58,8 +63,9 @@ constexpr int kGroups = kTileCols / kCols;  // column groups of a full item
 
 __device__ __forceinline__ f32x4_t load_f4(const float* p) { return *reinterpret_cast<const f32x4_t*>(p); }
 
-template <int D, bool PAGED>
+template <int D, bool PAGED, bool E4M3 = false>
 __global__ __launch_bounds__(64 * waves(PAGED)) void tile_f32_kernel(TileParams p, int n_full, int n_items) {
+  static_assert(PAGED || !E4M3, "8-bit caches are paged");
   constexpr int kWaves = waves(PAGED);
   constexpr int NJ = D / 16;  // float4 loads of a K or V block per lane
   // Workgroups of an item's column groups read the same keys: they are 8
@@ -91,7 +97,20 @@ __global__ __launch_bounds__(64 * waves(PAGED)) void tile_f32_kernel(TileParams 
   const int64_t row_f = (int64_t)p.Hkv * D;  // floats of a packed K/V row
   // first key of this lane's 4 scores in a block (paged: slots 4g.. hold the
   // tokens of kslot)
-  const int k0 = PAGED ? 4 * (((g & 1) << 1) | (g >> 1)) : 4 * g;
+  const int k0 = PAGED && !E4M3 ? 4 * (((g & 1) << 1) | (g >> 1)) : 4 * g;
+  // Four values of K or V as they are loaded: fp32, or e4m3 codes.
+  typedef std::conditional_t<E4M3, uint32_t, f32x4_t> Raw;
+  const uint8_t* K8 = static_cast<const uint8_t*>(p.k);
+  const uint8_t* V8 = static_cast<const uint8_t*>(p.v);
+  auto values = [](const Raw& x) __attribute__((always_inline)) -> f32x4_t {
+    if constexpr (E4M3) {
+      float y[4];
+      e4m3::values4(x, y);
+      return f32x4_t{y[0], y[1], y[2], y[3]};
+    } else {
+      return x;
+    }
+  };
 
   f32x4_t q[NJ];
   {
@@ -120,8 +139,12 @@ __global__ __launch_bounds__(64 * waves(PAGED)) void tile_f32_kernel(TileParams 
     if constexpr (PAGED) return load_scalar(p.block_table + x.R.kv_start + x.blk);
     else return 0;
   };
-  auto load_k = [&](const Cursor& x, int64_t id, f32x4_t (&kf)[NJ]) __attribute__((always_inline)) {
-    if constexpr (PAGED) {
+  auto load_k = [&](const Cursor& x, int64_t id, Raw (&kf)[NJ]) __attribute__((always_inline)) {
+    if constexpr (E4M3) {  // row r: token r
+      const uint8_t* kp = K8 + e4m3::codes_at<D>(id, w.kvh, p.Hkv) + r * 16 + 4 * g;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) kf[j] = *reinterpret_cast<const uint32_t*>(kp + j * (kBlock * 16));
+    } else if constexpr (PAGED) {
       const float* kp = K + (id * p.Hkv + w.kvh) * (int64_t)(D * kBlock) + (g >> 1) * (kBlock * 8) + r * 8 + 4 * (g & 1);
 #pragma unroll
       for (int j = 0; j < NJ; ++j) kf[j] = load_f4(kp + j * (2 * kBlock * 8));
@@ -133,8 +156,12 @@ __global__ __launch_bounds__(64 * waves(PAGED)) void tile_f32_kernel(TileParams 
     }
   };
   // Packed: vf[4q+i]; paged: vf[db].
-  auto load_v = [&](const Cursor& x, int64_t id, f32x4_t (&vf)[NJ]) __attribute__((always_inline)) {
-    if constexpr (PAGED) {
+  auto load_v = [&](const Cursor& x, int64_t id, Raw (&vf)[NJ]) __attribute__((always_inline)) {
+    if constexpr (E4M3) {
+      const uint8_t* vp = V8 + e4m3::codes_at<D>(id, w.kvh, p.Hkv) + r * kBlock + k0;
+#pragma unroll
+      for (int db = 0; db < NJ; ++db) vf[db] = *reinterpret_cast<const uint32_t*>(vp + db * 16 * kBlock);
+    } else if constexpr (PAGED) {
       const float* vp = V + (id * p.Hkv + w.kvh) * (int64_t)(D * kBlock) + r * kBlock + k0;
 #pragma unroll
       for (int db = 0; db < NJ; ++db) vf[db] = load_f4(vp + db * 16 * kBlock);
@@ -158,10 +185,18 @@ __global__ __launch_bounds__(64 * waves(PAGED)) void tile_f32_kernel(TileParams 
   Cursor C{0, wave, load_scalar(&p.ranges[w.rng_begin])};
   bool go = settle(C);
   if (go) {
-    f32x4_t kf[2][NJ], vf[NJ];
+    Raw kf[2][NJ], vf[NJ];
+    uint2 sc[E4M3 ? 2 : 1];  // scale bytes of the lane's four tokens, K's and V's
+    auto load_scales = [&](int64_t id, int X) __attribute__((always_inline)) {
+      if constexpr (E4M3) {
+        const uint8_t* sp = p.scales + e4m3::scales_at(id, w.kvh, p.Hkv) + k0;
+        sc[X] = make_uint2(*reinterpret_cast<const uint32_t*>(sp), *reinterpret_cast<const uint32_t*>(sp + kBlock));
+      }
+    };
     int lim = limit_of(C.R);
     int64_t id = block_id(C);
     load_k(C, id, kf[0]);
+    load_scales(id, 0);
     auto step = [&](auto xc) __attribute__((always_inline)) {
       constexpr int X = decltype(xc)::value;
       // The next block (this one again past the last: every step issues the
@@ -177,12 +212,25 @@ __global__ __launch_bounds__(64 * waves(PAGED)) void tile_f32_kernel(TileParams 
       // products that do not wait for one another.
       f32x4_t Sp[4];
 #pragma unroll
-      for (int j = 0; j < NJ; ++j)
+      for (int j = 0; j < NJ; ++j) {
+        const f32x4_t kj = values(kf[X][j]);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          Sp[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[X][j][e], q[j][e], j ? Sp[e] : f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+          Sp[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kj[e], q[j][e], j ? Sp[e] : f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+      }
       f32x4_t S = (Sp[0] + Sp[1]) + (Sp[2] + Sp[3]);
       load_k(N, id_n, kf[X ^ 1]);
+      load_scales(id_n, X ^ 1);
+      float sv[4];
+      if constexpr (E4M3) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t bk = (sc[X].x >> (8 * i)) & 255u, bv = (sc[X].y >> (8 * i)) & 255u;
+          // a row of V that is NaN: the scores of its token are
+          S[i] = bv == e4m3::kNan ? __uint_as_float(0x7fc00000u) : S[i] * e4m3::scale_value(bk);
+          sv[i] = bv == e4m3::kNan ? 0.f : e4m3::scale_value(bv);
+        }
+      }
       const int kb = C.blk * kKeys;
       const bool partial = kb + kKeys > C.R.min_lim;
       // Masked without a branch: the compiler leaves out the wait states
@@ -207,9 +255,26 @@ __global__ __launch_bounds__(64 * waves(PAGED)) void tile_f32_kernel(TileParams 
       for (int i = 0; i < 4; ++i) {
         e[i] = fast_exp2(fmaf(S[i], sl2, -ms));
         l += e[i];
+        if constexpr (E4M3) e[i] *= sv[i];
       }
+      f32x4_t decoded[NJ];
+      f32x4_t(&vx)[NJ] = [&]() __attribute__((always_inline)) -> f32x4_t(&)[NJ] {
+        if constexpr (E4M3) {
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) decoded[j] = values(vf[j]);
+          return decoded;
+        } else {
+          return vf;
+        }
+      }();
       bool plain = true;
-      if (PAGED && partial) {
+      if (E4M3 && partial) {  // (codes of V are finite, but for slots that no token is in)
+#pragma unroll
+        for (int db = 0; db < NJ; ++db)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (kb + k0 + i >= C.R.n_keys) vx[db][i] = 0.f;
+      } else if (PAGED && partial) {
         // Some column of the block does not see some of its slots, which may
         // hold anything; 0 * inf would be NaN.  Slots past the range's end
         // are zeroed; a non-finite value in a slot that only some columns
@@ -219,8 +284,8 @@ __global__ __launch_bounds__(64 * waves(PAGED)) void tile_f32_kernel(TileParams 
         for (int db = 0; db < NJ; ++db)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            if (kb + k0 + i >= C.R.n_keys) vf[db][i] = 0.f;
-            odd |= !(fabsf(vf[db][i]) < INFINITY);
+            if (kb + k0 + i >= C.R.n_keys) vx[db][i] = 0.f;
+            odd |= !(fabsf(vx[db][i]) < INFINITY);
           }
         plain = !__any(odd);
       }
@@ -229,7 +294,7 @@ __global__ __launch_bounds__(64 * waves(PAGED)) void tile_f32_kernel(TileParams 
         for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int j = 0; j < NJ; ++j)
-            acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(PAGED ? vf[j][i] : vf[4 * (j / 4) + i][j % 4], e[i], acc[j], 0, 0, 0);
+            acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(PAGED ? vx[j][i] : vx[4 * (j / 4) + i][j % 4], e[i], acc[j], 0, 0, 0);
       } else {
         for (int k = 0; k < kKeys && kb + k < C.R.n_keys; ++k) {
           // token k's probability for this column: element k % 4 of the lane
@@ -315,12 +380,17 @@ __global__ __launch_bounds__(64 * waves(PAGED)) void tile_f32_kernel(TileParams 
 
 // n_full: the first items of the schedule, of up to kTileCols columns each
 // (every packed item; the shared items of a decode step); the others are
-// private decode items of one column group.
+// private decode items of one column group.  p.scales: null, or 8-bit caches.
 hipError_t launch_tile_f32(const TileParams& p, int n_full, int n_items, int D, bool paged, hipStream_t stream) {
   static_assert(kCols == kPrivateCols, "a private item is one column group");
   if (n_items <= 0) return hipSuccess;
   const dim3 grid((unsigned)((n_full + 7) / 8 * 8 * kGroups + (n_items - n_full))), block(64 * waves(paged));
-  if (paged) {
+  if (paged && p.scales) {
+    if (D == 64)
+      hipLaunchKernelGGL((tile_f32_kernel<64, true, true>), grid, block, 0, stream, p, n_full, n_items);
+    else
+      hipLaunchKernelGGL((tile_f32_kernel<128, true, true>), grid, block, 0, stream, p, n_full, n_items);
+  } else if (paged) {
     if (D == 64)
       hipLaunchKernelGGL((tile_f32_kernel<64, true>), grid, block, 0, stream, p, n_full, n_items);
     else

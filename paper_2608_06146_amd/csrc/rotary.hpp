@@ -53,6 +53,7 @@ struct RotaryParams {
   const int32_t* slots;
   void* k_cache;
   void* v_cache;
+  uint8_t* scales;       // 8-bit caches (k_cache and v_cache hold codes)
   int64_t n_blocks;
   const int32_t* patch;  // (entry, block id) pairs of the block table
   int64_t n_patch;
@@ -68,6 +69,24 @@ struct CopyParams {
   const int32_t* pairs;
   int64_t n_pairs, src_blocks, dst_blocks;
   int64_t units;  // 16-byte units of a block, per tensor
+  // 8-bit caches: scales, and 16-byte units of a block's
+  const void* s_src;
+  void* s_dst;
+  int64_t s_units;
+};
+
+// Blocks between caches of values and 8-bit caches (one way or the other).
+struct CastParams {
+  const void* k;  // values in
+  const void* v;
+  void* k_out;    // values out
+  void* v_out;
+  uint8_t* k_codes;
+  uint8_t* v_codes;
+  uint8_t* scales;
+  const int32_t* pairs;  // null: block i to block i
+  int64_t n_pairs, src_blocks, dst_blocks;
+  int32_t Hkv;
 };
 
 // Items of a backward: each leaves D sums in the workspace.

@@ -58,7 +58,14 @@ struct TileParams {
   float* part_ml;         // partial mode: [slots, 2] (running max in log2 units, sum)
   int32_t Hq, Hkv, G;
   float scale_log2;       // softmax_scale * log2(e)
+  const uint8_t* scales;  // 8-bit caches: [blocks, Hkv, 2, 16] (k and v hold codes)
 };
+
+// 8-bit caches: whether a dtype names them, and the dtype of the rows around them.
+constexpr bool is_e4m3(padoc_dtype t) { return t == PADOC_BF16_E4M3 || t == PADOC_F32_E4M3; }
+constexpr padoc_dtype row_dtype(padoc_dtype t) {
+  return t == PADOC_BF16_E4M3 ? PADOC_BF16 : t == PADOC_F32_E4M3 ? PADOC_F32 : t;
+}
 
 // Backward of the packed forward (bf16).
 struct BwdParams {
