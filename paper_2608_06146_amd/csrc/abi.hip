@@ -30,7 +30,8 @@ hipError_t launch_rotary_append(RotaryParams p, int D, bool bf16, bool pairs, hi
 hipError_t launch_copy_blocks(const CopyParams& p, hipStream_t s);
 hipError_t launch_rotary_append_e4m3(RotaryParams p, int D, bool bf16, bool pairs, hipStream_t s);
 hipError_t launch_cast_blocks(const CastParams& p, int D, bool bf16, bool back, hipStream_t s);
-hipError_t launch_decode_e4m3(const TileParams& p, int n_shared, int n_private, int D, hipStream_t s);
+hipError_t launch_decode_e4m3(const TileParams& p, int n_shared, int n_private, int n_groups, int* next, int D,
+                              hipStream_t s);
 
 namespace {
 thread_local hipEvent_t t_ev_before = nullptr;
@@ -208,13 +209,12 @@ padoc_status run(const padoc_plan* P, const void* q, const void* k, const void* 
     if (e != hipSuccess) return hip_fail("hipEventRecord", e);
   }
   if (bf16) {
-    if (scales)
-      e = launch_decode_e4m3(tp, P->n_work_shared, n_work - P->n_work_shared, P->D, stream);
-    else if (!paged)
+    if (!paged)
       e = launch_tile_mfma_bf16(tp, n_work, P->D, stream);
     else  // shared-key tile items and private-key items in one launch
-      e = launch_decode_step_bf16(tp, P->n_work_shared, n_work - P->n_work_shared, P->n_private_groups,
-                                  reinterpret_cast<int*>(static_cast<char*>(ws) + P->off_next), P->D, stream);
+      e = (scales ? launch_decode_e4m3 : launch_decode_step_bf16)(
+          tp, P->n_work_shared, n_work - P->n_work_shared, P->n_private_groups,
+          reinterpret_cast<int*>(static_cast<char*>(ws) + P->off_next), P->D, stream);
   } else {
     e = launch_tile_f32(tp, paged ? P->n_work_shared : n_work, n_work, P->D, paged, stream);
   }

@@ -9,7 +9,7 @@
 // rounded to bf16.
 #include "device_common.hpp"
 #include "e4m3.hpp"
-#include "tile_common.hpp"
+#include "fwd_item.hpp"
 
 namespace padoc {
 namespace {
@@ -24,8 +24,8 @@ __device__ __forceinline__ u32x4 load16_nt(const uint8_t* p) {
   return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
 }
 
-// 16 columns (col0 .. col0+ncol-1) of work item `item` on one wavefront, whose
-// lane index is `lane`: keys in steps of 64, from HBM straight into
+// Private work item `item` (at most 16 columns) on one wavefront, whose lane
+// index is `lane`: keys in steps of 64, from HBM straight into
 // v_mfma_f32_16x16x32_bf16 operands (lane l: row / column n = l%16, group
 // g = l/16 with eight consecutive elements of the contraction).
 //   S^T = K Q^T    four 16-key M blocks; row m of block T holds token
@@ -38,16 +38,15 @@ __device__ __forceinline__ u32x4 load16_nt(const uint8_t* p) {
 constexpr int kSets = 2;
 
 template <int D>
-__device__ __forceinline__ void wave_item(const TileParams& p, int item, int col0, int ncol, int lane) {
+__device__ __forceinline__ void wave_item(const TileParams& p, int item, int lane) {
   constexpr int NP = D / 64;   // 16-dim pieces per lane and token
   constexpr int NDM = D / 16;  // 16-row blocks of O^T
   const WorkRec w = load_scalar(p.work + item);
-  if (w.rng_count <= 0) return;
   const int n = lane & 15, g = lane >> 4;
   const int G = p.G, kvh = w.kvh, Hkv = p.Hkv;
-  const int col = col0 + n;
+  const int col = w.col0 + n;
   const int t = col / G;
-  const bool valid = n < ncol && t < w.ntok;
+  const bool valid = n < w.ncol && t < w.ntok;
   const int32_t qrow = valid ? p.toks[w.tok_begin + t] : 0;
   const int32_t hq = kvh * G + (col - t * G);
   const uint8_t* Kc = static_cast<const uint8_t*>(p.k);
@@ -84,7 +83,7 @@ __device__ __forceinline__ void wave_item(const TileParams& p, int item, int col
   u32x4 kf[kSets][4][NP];  // [set][M block][piece]
   u32x4 vf[kSets][NDM];    // [set][16-row d block]
   u32x4 ks[kSets], vs[kSets];  // scales of the K tokens (cache block n/4) and of the V tokens (block g)
-  int32_t nid[4];          // ids of the load cursor's blocks, requested ahead
+  int32_t id0, id1, id2, id3;  // ids of the load cursor's blocks, requested ahead
 
   // Blocks past the range's end take the step's first; past the item's last
   // step block 0 is read over and over (every step issues the same loads, so
@@ -92,12 +91,14 @@ __device__ __forceinline__ void wave_item(const TileParams& p, int item, int col
   auto fetch_ids = [&](const Cursor& c) __attribute__((always_inline)) {
     const int kb = c.st * kStep;
     const int32_t* b = p.block_table + c.R.kv_start + (kb >> 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) nid[i] = load_scalar(b + (kb + 16 * i < c.R.n_keys ? i : 0));
+    id0 = load_scalar(b);
+    id1 = load_scalar(b + (kb + 16 < c.R.n_keys ? 1 : 0));
+    id2 = load_scalar(b + (kb + 32 < c.R.n_keys ? 2 : 0));
+    id3 = load_scalar(b + (kb + 48 < c.R.n_keys ? 3 : 0));
   };
   auto pick = [&](int i, bool real) __attribute__((always_inline)) -> int64_t {
-    const int id = i < 2 ? (i == 0 ? nid[0] : nid[1]) : (i == 2 ? nid[2] : nid[3]);
-    return real ? id : 0;
+    const int lo = (i & 1) ? id1 : id0, hi = (i & 1) ? id3 : id2;
+    return real ? ((i & 2) ? hi : lo) : 0;
   };
   int64_t vblk[kSets];
   auto load_k = [&](int X, bool real) __attribute__((always_inline)) {
@@ -232,32 +233,48 @@ __device__ __forceinline__ void wave_item(const TileParams& p, int item, int col
   }
 }
 
-// Wavefront f of the launch: column group f % groups of shared item f / groups,
-// then one private item each.
+// As decode_step_kernel: shared tile items on the first workgroups, then every
+// wavefront takes private items from its XCD's queue.
+constexpr int kQueues = kPrivateQueues;
+
+__device__ __forceinline__ int take_private(int* ctr, int lane) {
+  int v = 0;
+  if (lane == 0) v = atomicAdd(ctr, 1);
+  return __builtin_amdgcn_readfirstlane(v);
+}
+
 template <int D>
-__global__ __launch_bounds__(tile::kThreads) void decode_e4m3_kernel(TileParams p, int n_shared, int n_private) {
-  constexpr int kGroups = kTileCols / kPrivateCols;
-  const int lane = threadIdx.x & 63;
-  const int64_t f = (int64_t)blockIdx.x * tile::kWaves + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int64_t shared = (int64_t)n_shared * kGroups;
-  if (f >= shared + n_private) return;
-  const int item = (int)(f < shared ? f / kGroups : n_shared + (f - shared));
-  const WorkRec w = load_scalar(p.work + item);
-  const int c0 = f < shared ? (int)(f % kGroups) * kPrivateCols : 0;
-  if (c0 >= w.ncol) return;
-  wave_item<D>(p, item, w.col0 + c0, min(kPrivateCols, w.ncol - c0), lane);
+__global__ __launch_bounds__(tile::kThreads) void decode_e4m3_kernel(TileParams p, int n_shared, int n_private,
+                                                                     int n_groups, int* next) {
+  const int b = blockIdx.x;
+  if (b < n_shared) tile::fwd_item<D, true, true>(p, b);
+  if (n_private <= 0) return;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int q = b % kQueues;
+  const int n_q = (n_private - q + kQueues - 1) / kQueues;
+  const int end = n_shared + n_groups;
+  const int b0 = n_shared + (q - n_shared % kQueues + kQueues) % kQueues;
+  const int n_first = b0 < end ? ((end - 1 - b0) / kQueues + 1) * tile::kWaves : 0;
+  int* ctr = next + q * 64;
+  int k = b >= n_shared ? ((b - b0) / kQueues) * tile::kWaves + wave : n_first + take_private(ctr, lane);
+  while (k < n_q) {
+    wave_item<D>(p, n_shared + q + kQueues * k, lane);
+    k = n_first + take_private(ctr, lane);
+  }
 }
 
 }  // namespace
 
-hipError_t launch_decode_e4m3(const TileParams& p, int n_shared, int n_private, int D, hipStream_t stream) {
-  const int64_t waves = (int64_t)n_shared * (kTileCols / kPrivateCols) + n_private;
-  if (waves <= 0) return hipSuccess;
-  const dim3 grid((unsigned)((waves + tile::kWaves - 1) / tile::kWaves)), block(tile::kThreads);
+// n_groups, next: as launch_decode_step_bf16.
+hipError_t launch_decode_e4m3(const TileParams& p, int n_shared, int n_private, int n_groups, int* next, int D,
+                              hipStream_t stream) {
+  const int n_blocks = n_shared + n_groups;
+  if (n_blocks <= 0) return hipSuccess;
+  const dim3 grid(n_blocks), block(tile::kThreads);
   if (D == 64)
-    hipLaunchKernelGGL((decode_e4m3_kernel<64>), grid, block, 0, stream, p, n_shared, n_private);
+    hipLaunchKernelGGL((decode_e4m3_kernel<64>), grid, block, 0, stream, p, n_shared, n_private, n_groups, next);
   else
-    hipLaunchKernelGGL((decode_e4m3_kernel<128>), grid, block, 0, stream, p, n_shared, n_private);
+    hipLaunchKernelGGL((decode_e4m3_kernel<128>), grid, block, 0, stream, p, n_shared, n_private, n_groups, next);
   return hipGetLastError();
 }
 

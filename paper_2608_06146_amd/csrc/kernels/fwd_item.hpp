@@ -74,6 +74,7 @@
 // one page 66.4 / 65.0, of eight 851 / 842, 64-wide heads 569 / 565.
 #pragma once
 
+#include "e4m3.hpp"
 #include "tile_common.hpp"
 
 namespace padoc {
@@ -145,8 +146,9 @@ __device__ __forceinline__ void dma4_v(const void* a, uint32_t lds) {
 }
 #pragma clang diagnostic pop
 
-template <int D, bool PAGED>
+template <int D, bool PAGED, bool E4M3 = false>
 __device__ __forceinline__ void fwd_item(const TileParams& p, int item) {
+  static_assert(PAGED || !E4M3, "8-bit caches are paged");
   using Gm = FwdGeom<D>;
   constexpr int KT = Gm::KT, CPR = Gm::CPR, RPI = Gm::RPI, IPW = Gm::IPW, SEL = Gm::SEL;
   constexpr int NKK = D / 16;
@@ -328,6 +330,88 @@ __device__ __forceinline__ void fwd_item(const TileParams& p, int item) {
     const int32_t lim_off = c.R.lim_off;
     const int32_t* lb = lim_off < 0 ? &p.work[item].ntok : p.lims + lim_off;
     dma4(lb, lim_off < 0 || !valid ? 0u : 4u * tok, lds_addr(dst + wave * 64));
+  };
+
+  // 8-bit caches: a thread's 16 codes of K and of V of a tile (64-wide heads: K's
+  // on the first four wavefronts, V's on the others), of cache block `vb` of the
+  // tile, whose scales of V are the same for the whole wavefront.
+  using e4m3::u32x4;
+  constexpr bool kBoth = D == 128;  // every wavefront has codes of both
+  struct Staged {
+    u32x4 k, v, vs;    // codes; V's scale bytes
+    uint32_t ks;       // K's scale byte
+    int32_t lim, keep; // the column's limit; tokens of the block that exist
+  };
+  const int vb = kBoth ? wave >> 1 : wave & 3, unit = kBoth ? tid & 127 : lane;
+  const bool has_k = kBoth || wave < 4, has_v = kBoth || wave >= 4;
+  const int k_row = vb * kBlock + kslot(unit & 15);
+  auto load_codes = [&](const Cursor& c, Staged& x) {
+    if constexpr (E4M3) {
+      const int64_t blk = __builtin_amdgcn_readlane(tile_blocks(c), vb);
+      const int64_t at = e4m3::codes_at<D>(blk, kvh, p.Hkv), sat = e4m3::scales_at(blk, kvh, p.Hkv);
+      if (has_k) x.k = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(p.k) + at) + unit);
+      if (has_v) x.v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(p.v) + at) + unit);
+      x.ks = p.scales[sat + (unit & 15)];
+      x.vs = *reinterpret_cast<const u32x4*>(p.scales + sat + kBlock);
+      const int32_t* lb = c.R.lim_off < 0 ? &p.work[item].ntok : p.lims + c.R.lim_off;
+      x.lim = lb[c.R.lim_off < 0 || !valid ? 0 : tok];
+      x.keep = c.R.n_keys - c.kt * KT - vb * kBlock;
+    }
+  };
+  // The codes of a tile into stage SC as bf16, in pieces 0 .. 6.  Piece 0: what is
+  // rare, V's tokens past the range's end (zeros: their P is 0, but the slots may
+  // hold anything) and V rows that are NaN (scores of their tokens NaN, through
+  // K's codes, where a column sees them; V itself stays 0).
+  auto place_codes = [&](Staged& x, uint16_t* ks, uint16_t* vs, int32_t* lim, auto kc) {
+    constexpr int k = decltype(kc)::value;
+    if constexpr (E4M3) {
+      if constexpr (k == 0) {
+        uint32_t any = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x.vs[i] = __builtin_amdgcn_readfirstlane(x.vs[i]);
+          any |= (~x.vs[i] - 0x01010101u) & x.vs[i] & 0x80808080u;
+        }
+        if (any != 0 || x.keep < kBlock) {
+#pragma unroll
+          for (int e = 0; e < kBlock; ++e) {
+            const uint32_t m = 255u << (8 * (e & 3));
+            if ((x.vs[e >> 2] & m) == m) {
+              if ((unit & 15) == e) x.k = u32x4{e4m3::kNanCodes, e4m3::kNanCodes, e4m3::kNanCodes, e4m3::kNanCodes};
+              x.vs[e >> 2] &= ~m;
+            }
+            if (e >= x.keep) x.v[e >> 2] &= ~m;
+          }
+        }
+        lim[tid] = x.lim;
+      }
+      if constexpr (k == 1 || k == 2) {
+        if (has_k) {
+          const int c = 2 * (unit >> 4) + k - 1;
+          *reinterpret_cast<bf16x8_t*>(ks + k_row * D + 8 * (c ^ Gm::kswz(k_row))) =
+              e4m3::values8(x.k[2 * k - 2], x.k[2 * k - 1], e4m3::scale_value(x.ks));
+        }
+      }
+      if constexpr (k >= 3) {
+        constexpr int i = k - 3;  // tokens 4i .. 4i+3, in x.v[i] from here on as two pairs of bf16
+        if (has_v) {
+          uint32_t y[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+            const float s0 = __uint_as_float(((x.vs[i] >> (16 * h)) & 255u) << 23);
+            const float s1 = __uint_as_float(((x.vs[i] >> (16 * h + 8)) & 255u) << 23);
+            const bf16x2 a = h == 0 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x.v[i], s0, false)
+                                    : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x.v[i], s0, true);
+            const bf16x2 b = h == 0 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x.v[i], s1, false)
+                                    : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x.v[i], s1, true);
+            y[h] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060100u);
+          }
+          const int d = unit;
+          *reinterpret_cast<uint2*>(vs + (vb * D + d) * kBlock + 8 * ((i >> 1) ^ ((d >> 3) & 1)) + 4 * (i & 1)) = make_uint2(y[0], y[1]);
+        }
+      }
+    }
   };
 
   Cursor Lk{0, 0, R0, 1, 0};  // next tile to load (K, V, limits)
@@ -514,7 +598,7 @@ __device__ __forceinline__ void fwd_item(const TileParams& p, int item) {
   // u % D of block u / D; the caller has waited for the stage's loads and a
   // barrier separates this from the stage's reads.
   auto zero_v_tail = [&](uint16_t* vs) {
-    if constexpr (PAGED) {
+    if constexpr (PAGED && !E4M3) {
       const int keep = C.R.n_keys - C.kt * KT;  // valid keys of the tile
       if (keep < KT && tid < NBT * D) {
         const int b = tid / D, d = tid % D;
@@ -547,12 +631,30 @@ __device__ __forceinline__ void fwd_item(const TileParams& p, int item) {
     __builtin_amdgcn_s_waitcnt(0xC07F);  // the ids are in LDS; Q may be on its way
     bar();
   }
-  load_next(I0{});
-  load_next(I1{});
-  __builtin_amdgcn_s_waitcnt(0);
-  bar();
-  load_next(I2{});
-  if constexpr (PAGED) {
+  // 8-bit caches: tiles 0 and 1 placed, tile 2 in registers.
+  constexpr int kPlace = 7;  // pieces of place_codes
+  Staged staged;
+  auto load_staged = [&](Staged& x) {
+    load_codes(Lk, x);
+    advance(Lk);
+  };
+  if constexpr (E4M3) {
+    Staged other;
+    load_staged(staged);
+    load_staged(other);
+    static_for<kPlace>([&](auto kc) { place_codes(staged, smem, smem + 4 * SEL, Lb[0], kc); });
+    load_staged(staged);
+    static_for<kPlace>([&](auto kc) { place_codes(other, smem + SEL, smem + 5 * SEL, Lb[1], kc); });
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    bar();
+  } else {
+    load_next(I0{});
+    load_next(I1{});
+    __builtin_amdgcn_s_waitcnt(0);
+    bar();
+    load_next(I2{});
+  }
+  if constexpr (PAGED && !E4M3) {
     zero_v_tail(vst(I0{}));
     __builtin_amdgcn_s_waitcnt(0xC07F);
     bar();
@@ -565,6 +667,14 @@ __device__ __forceinline__ void fwd_item(const TileParams& p, int item) {
     // unused: 20.73 -> 20.37 us; forward with 64-wide heads, seven to a KV
     // head: 569 -> 563; all columns used: no difference).
     for (int t = 0; t < n_tiles; ++t) {
+      if constexpr (E4M3) {
+        __builtin_amdgcn_s_waitcnt(0xC07F);
+        bar();
+        uint16_t* ks = smem + ((t + 2) % 4) * SEL;
+        static_for<kPlace>([&](auto kc) { place_codes(staged, ks, ks + 4 * SEL, Lb[(t + 2) % 4], kc); });
+        load_staged(staged);
+        continue;
+      }
       wait_vm<2 * IPW + 1>();
       bar();
       advance(C);
@@ -598,7 +708,10 @@ __device__ __forceinline__ void fwd_item(const TileParams& p, int item) {
     constexpr int SC = decltype(sc)::value;
     using Y = std::integral_constant<int, SC % 2>;
     using YN = std::integral_constant<int, (SC + 1) % 2>;
-    wait_vm<2 * IPW + 1>();  // this wavefront's loads of step t-2 have landed
+    if constexpr (E4M3)
+      __builtin_amdgcn_s_waitcnt(0xC07F);  // this wavefront has placed its codes of tile t+1
+    else
+      wait_vm<2 * IPW + 1>();  // this wavefront's loads of step t-2 have landed
     bar();
     ls0 = 0.f;
     ls1 = 0.f;
@@ -635,12 +748,21 @@ __device__ __forceinline__ void fwd_item(const TileParams& p, int item) {
       mask_tile(YN{}, lst(std::integral_constant<int, SC + 1>{}));
       zero_v_tail(vst(std::integral_constant<int, SC + 1>{}));
     }
-    const int ids = tile_blocks(Lk);
+    const int ids = E4M3 ? 0 : tile_blocks(Lk);
     pv_product(std::integral_constant<int, SC>{}, [&](auto ic) {
       constexpr int i = decltype(ic)::value;
       static_for<kPieces / NB>([&](auto uc) {
         fma_piece(YN{}, std::integral_constant<int, i * (kPieces / NB) + decltype(uc)::value>{});
       });
+      if constexpr (E4M3) {
+        // the codes of tile t+2, and those of tile t+3 asked for
+        using Next = std::integral_constant<int, SC + 2>;
+        constexpr int first = NB - 1 - kPlace;
+        if constexpr (i >= first && i < first + kPlace)
+          place_codes(staged, kst(Next{}), vst(Next{}), lst(Next{}), std::integral_constant<int, i - first>{});
+        if constexpr (i == NB - 1) load_staged(staged);
+        return;
+      }
       if constexpr (i == NB / 2) load_tile(Kg, Lk, kst(std::integral_constant<int, SC + 3>{}), ld_k, false, ids);
       if constexpr (i == NB / 2 + 1) load_tile(Vg, Lk, vst(std::integral_constant<int, SC + 3>{}), ld_v, true, ids);
       if constexpr (i == NB / 2 + 2) {

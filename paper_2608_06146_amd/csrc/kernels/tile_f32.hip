@@ -257,23 +257,16 @@ __global__ __launch_bounds__(64 * waves(PAGED)) void tile_f32_kernel(TileParams 
         l += e[i];
         if constexpr (E4M3) e[i] *= sv[i];
       }
-      f32x4_t decoded[NJ];
-      f32x4_t(&vx)[NJ] = [&]() __attribute__((always_inline)) -> f32x4_t(&)[NJ] {
-        if constexpr (E4M3) {
-#pragma unroll
-          for (int j = 0; j < NJ; ++j) decoded[j] = values(vf[j]);
-          return decoded;
-        } else {
-          return vf;
-        }
-      }();
       bool plain = true;
-      if (E4M3 && partial) {  // (codes of V are finite, but for slots that no token is in)
+      f32x4_t decoded[E4M3 ? NJ : 1];
+      if constexpr (E4M3) {  // (codes of V are finite, but for slots that no token is in)
 #pragma unroll
-        for (int db = 0; db < NJ; ++db)
+        for (int j = 0; j < NJ; ++j) {
+          decoded[j] = values(vf[j]);
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (kb + k0 + i >= C.R.n_keys) vx[db][i] = 0.f;
+            if (partial && kb + k0 + i >= C.R.n_keys) decoded[j][i] = 0.f;
+        }
       } else if (PAGED && partial) {
         // Some column of the block does not see some of its slots, which may
         // hold anything; 0 * inf would be NaN.  Slots past the range's end
@@ -284,8 +277,8 @@ __global__ __launch_bounds__(64 * waves(PAGED)) void tile_f32_kernel(TileParams 
         for (int db = 0; db < NJ; ++db)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            if (kb + k0 + i >= C.R.n_keys) vx[db][i] = 0.f;
-            odd |= !(fabsf(vx[db][i]) < INFINITY);
+            if (kb + k0 + i >= C.R.n_keys) vf[db][i] = 0.f;
+            odd |= !(fabsf(vf[db][i]) < INFINITY);
           }
         plain = !__any(odd);
       }
@@ -293,8 +286,14 @@ __global__ __launch_bounds__(64 * waves(PAGED)) void tile_f32_kernel(TileParams 
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int j = 0; j < NJ; ++j)
-            acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(PAGED ? vx[j][i] : vx[4 * (j / 4) + i][j % 4], e[i], acc[j], 0, 0, 0);
+          for (int j = 0; j < NJ; ++j) {
+            float v;
+            if constexpr (E4M3)
+              v = decoded[j][i];
+            else
+              v = PAGED ? vf[j][i] : vf[4 * (j / 4) + i][j % 4];
+            acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, e[i], acc[j], 0, 0, 0);
+          }
       } else {
         for (int k = 0; k < kKeys && kb + k < C.R.n_keys; ++k) {
           // token k's probability for this column: element k % 4 of the lane
