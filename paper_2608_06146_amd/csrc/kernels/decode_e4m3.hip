@@ -7,6 +7,8 @@
 // four significant bits, so that nothing is rounded).  K's scale goes into the
 // conversion; V's, one for each key, into the probabilities before they are
 // rounded to bf16.
+#include <type_traits>
+
 #include "device_common.hpp"
 #include "e4m3.hpp"
 #include "fwd_item.hpp"
@@ -17,37 +19,44 @@ namespace {
 using e4m3::bf16x8_t;
 using e4m3::u32x4;
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kStep = 64;  // keys of a step: four blocks
+constexpr int kStep = 32;  // keys of a step: two blocks
+constexpr int kSets = 2;   // steps in flight
 
 __device__ __forceinline__ u32x4 load16_nt(const uint8_t* p) {
   return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
 }
+__device__ __forceinline__ u32x2 load8(const uint8_t* p) { return *reinterpret_cast<const u32x2*>(p); }
 
 // Private work item `item` (at most 16 columns) on one wavefront, whose lane
-// index is `lane`: keys in steps of 64, from HBM straight into
+// index is `lane`: keys in steps of 32, from HBM straight into
 // v_mfma_f32_16x16x32_bf16 operands (lane l: row / column n = l%16, group
 // g = l/16 with eight consecutive elements of the contraction).
-//   S^T = K Q^T    four 16-key M blocks; row m of block T holds token
-//                  4T + m%4 of cache block m/4, so that a lane's 16 scores are
-//                  the 16 tokens of cache block g, in order; a lane's 16 codes
-//                  (a 16-dim piece of a token) are two operands
-//   O^T += V^T P^T the lane's 16 codes of a V row are the tokens of cache block
-//                  g, two operands of eight
+//   S^T = K Q^T    two 16-key M blocks; row m of block T holds token 8 (m/4 % 2)
+//                  + 4T + m%4 of cache block m/8, so that a lane's eight scores
+//                  are tokens 8 (g%2) .. +7 of cache block g/2, in order; a
+//                  lane's 16 codes (a 16-dim piece of a token) are two operands
+//   O^T += V^T P^T a lane loads the 16 tokens of a V row: of row block 2e where g
+//                  is even, of 2e + 1 where it is odd.  Two lane swaps exchange
+//                  the halves, so that it has tokens 8 (g%2) .. +7 of both rows.
 // Two register sets hold the codes of two steps, refilled after their last use.
-constexpr int kSets = 2;
-
+// Fewer bytes in flight are better here: a read of 420 MB in random 2 KB pieces
+// took 62 us (6.5 TB/s) with 8 KB sets and 68 with 16 KB sets, two a wavefront,
+// eight wavefronts a unit.
 template <int D>
 __device__ __forceinline__ void wave_item(const TileParams& p, int item, int lane) {
   constexpr int NP = D / 64;   // 16-dim pieces per lane and token
   constexpr int NDM = D / 16;  // 16-row blocks of O^T
   const WorkRec w = load_scalar(p.work + item);
+  // (as private_item: such an item's first loads wait for one record, not three)
+  const bool direct = w.direct[0] >= 0;
   const int n = lane & 15, g = lane >> 4;
   const int G = p.G, kvh = w.kvh, Hkv = p.Hkv;
   const int col = w.col0 + n;
   const int t = col / G;
   const bool valid = n < w.ncol && t < w.ntok;
-  const int32_t qrow = valid ? p.toks[w.tok_begin + t] : 0;
+  const int32_t qrow = !valid ? 0 : direct ? w.direct[2] : p.toks[w.tok_begin + t];
   const int32_t hq = kvh * G + (col - t * G);
   const uint8_t* Kc = static_cast<const uint8_t*>(p.k);
   const uint8_t* Vc = static_cast<const uint8_t*>(p.v);
@@ -77,15 +86,29 @@ __device__ __forceinline__ void wave_item(const TileParams& p, int item, int lan
         c.ok = 0;
     }
   };
-  Cursor C{0, 0, load_scalar(p.ranges + w.rng_begin), 1, 0};
+  RangeRec R0;
+  int n_steps = 0;
+  if (direct) {
+    R0.kv_start = w.direct[0];
+    R0.n_keys = R0.min_lim = w.direct[1];
+    R0.lim_off = -1;
+    R0.seg = R0.key_begin = R0.reserved = 0;
+    n_steps = (R0.n_keys + kStep - 1) / kStep;
+  } else {
+    R0 = load_scalar(p.ranges + w.rng_begin);
+    for (int r = 0; r < w.rng_count; ++r)
+      n_steps += (load_scalar(p.ranges + w.rng_begin + r).n_keys + kStep - 1) / kStep;
+  }
+  n_steps = __builtin_amdgcn_readfirstlane(n_steps);
+  Cursor C{0, 0, R0, 1, 0};
   Cursor L = C;
 
-  u32x4 kf[kSets][4][NP];  // [set][M block][piece]
-  u32x4 vf[kSets][NDM];    // [set][16-row d block]
-  u32x4 ks[kSets], vs[kSets];  // scales of the K tokens (cache block n/4) and of the V tokens (block g)
-  int32_t id0, id1, id2, id3;  // ids of the load cursor's blocks, requested ahead
+  u32x4 kf[kSets][2][NP];    // [set][M block][piece]
+  u32x4 vf[kSets][NDM / 2];  // [set][pair of 16-row blocks]
+  u32x2 ks[kSets], vs[kSets];  // scales of eight K tokens of cache block n/8, of the lane's eight V tokens
+  int32_t id0, id1;          // ids of the load cursor's blocks, requested ahead
 
-  // Blocks past the range's end take the step's first; past the item's last
+  // A block past the range's end takes the step's first; past the item's last
   // step block 0 is read over and over (every step issues the same loads, so
   // that the compiler's waits for a set stay exact) and never used.
   auto fetch_ids = [&](const Cursor& c) __attribute__((always_inline)) {
@@ -93,38 +116,44 @@ __device__ __forceinline__ void wave_item(const TileParams& p, int item, int lan
     const int32_t* b = p.block_table + c.R.kv_start + (kb >> 4);
     id0 = load_scalar(b);
     id1 = load_scalar(b + (kb + 16 < c.R.n_keys ? 1 : 0));
-    id2 = load_scalar(b + (kb + 32 < c.R.n_keys ? 2 : 0));
-    id3 = load_scalar(b + (kb + 48 < c.R.n_keys ? 3 : 0));
-  };
-  auto pick = [&](int i, bool real) __attribute__((always_inline)) -> int64_t {
-    const int lo = (i & 1) ? id1 : id0, hi = (i & 1) ? id3 : id2;
-    return real ? ((i & 2) ? hi : lo) : 0;
   };
   int64_t vblk[kSets];
   auto load_k = [&](int X, bool real) __attribute__((always_inline)) {
-    const int64_t blk = pick(n >> 2, real);
-    vblk[X] = pick(g, real);
-    const uint8_t* kp = Kc + e4m3::codes_at<D>(blk, kvh, Hkv) + g * (kBlock * 16) + (n & 3) * 16;
+    const int64_t blk = real ? (n >= 8 ? id1 : id0) : 0;
+    vblk[X] = real ? (g >= 2 ? id1 : id0) : 0;
+    const uint8_t* kp = Kc + e4m3::codes_at<D>(blk, kvh, Hkv) + g * (kBlock * 16) + (8 * ((n >> 2) & 1) + (n & 3)) * 16;
 #pragma unroll
-    for (int T = 0; T < 4; ++T)
+    for (int T = 0; T < 2; ++T)
 #pragma unroll
       for (int j = 0; j < NP; ++j) kf[X][T][j] = load16_nt(kp + 4 * T * 16 + 4 * j * (kBlock * 16));
-    ks[X] = *reinterpret_cast<const u32x4*>(p.scales + e4m3::scales_at(blk, kvh, Hkv));
+    ks[X] = load8(p.scales + e4m3::scales_at(blk, kvh, Hkv) + 8 * ((n >> 2) & 1));
   };
   auto load_v = [&](int X) __attribute__((always_inline)) {
-    const uint8_t* vp = Vc + e4m3::codes_at<D>(vblk[X], kvh, Hkv) + n * kBlock;
+    const uint8_t* vp = Vc + e4m3::codes_at<D>(vblk[X], kvh, Hkv) + (16 * (g & 1) + n) * kBlock;
 #pragma unroll
-    for (int dm = 0; dm < NDM; ++dm) vf[X][dm] = load16_nt(vp + dm * 16 * kBlock);
-    vs[X] = *reinterpret_cast<const u32x4*>(p.scales + e4m3::scales_at(vblk[X], kvh, Hkv) + kBlock);
+    for (int e = 0; e < NDM / 2; ++e) vf[X][e] = load16_nt(vp + e * 32 * kBlock);
+    vs[X] = load8(p.scales + e4m3::scales_at(vblk[X], kvh, Hkv) + kBlock + 8 * (g & 1));
   };
 
   float m_run = -INFINITY, l_part = 0.f;
   f32x4_t acc[NDM];
 #pragma unroll
   for (int dm = 0; dm < NDM; ++dm) acc[dm] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  // This column's limit in the compute cursor's range (scalar loads, picked per
+  // lane: a vector load here would have the compiler wait for every load in flight).
   int lim = 0;
+  const int t_lo = w.col0 / G, t_hi = min(w.ntok - 1, (w.col0 + kPrivateCols - 1) / G);
   auto load_lim = [&]() __attribute__((always_inline)) {
-    lim = C.R.lim_off < 0 ? C.R.n_keys : valid ? p.lims[C.R.lim_off + t] : 0;
+    if (C.R.lim_off < 0) {
+      lim = C.R.n_keys;
+      return;
+    }
+    int v = 0;
+    for (int i = t_lo; i <= t_hi; ++i) {
+      const int32_t li = load_scalar(p.lims + C.R.lim_off + i);
+      v = t == i ? li : v;
+    }
+    lim = valid ? v : 0;
   };
   load_lim();
   const float sl2 = p.scale_log2;
@@ -143,12 +172,12 @@ __device__ __forceinline__ void wave_item(const TileParams& p, int item, int lan
   }
   fetch_ids(L);
 
-  auto step = [&](auto xc) __attribute__((always_inline)) -> bool {
+  auto step = [&](auto xc) __attribute__((always_inline)) {
     constexpr int X = decltype(xc)::value;
     const int kb = C.st * kStep;
-    f32x4_t S[4];
+    f32x4_t S[2];
 #pragma unroll
-    for (int T = 0; T < 4; ++T) {
+    for (int T = 0; T < 2; ++T) {
       S[T] = f32x4_t{0.f, 0.f, 0.f, 0.f};
       const float sk = e4m3::scale_value((ks[X][T] >> (8 * (n & 3))) & 255u);
 #pragma unroll
@@ -162,62 +191,80 @@ __device__ __forceinline__ void wave_item(const TileParams& p, int item, int lan
     load_k(X, more);  // set X's K is consumed
     // A V row that is NaN: the scores of its token are (where a column sees it);
     // no scale is infinite, so that probabilities of 0 stay 0.
-    if (__any(e4m3::has_nan(vs[X][0]) || e4m3::has_nan(vs[X][1]) || e4m3::has_nan(vs[X][2]) || e4m3::has_nan(vs[X][3]))) {
+    if (__any(e4m3::has_nan(vs[X][0]) || e4m3::has_nan(vs[X][1]))) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (e4m3::byte_of(vs[X], e) == e4m3::kNan) {
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t m = 255u << (8 * (e & 3));
+        if ((vs[X][e / 4] & m) == m) {
           S[e / 4][e % 4] = __uint_as_float(0x7fc00000u);
-          vs[X][e / 4] &= ~(255u << (8 * (e % 4)));
+          vs[X][e / 4] &= ~m;
         }
+      }
     }
     if (kb + kStep > C.R.min_lim) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (kb + 16 * g + e >= lim) S[e / 4][e % 4] = -INFINITY;
+      for (int e = 0; e < 8; ++e)
+        if (kb + 8 * g + e >= lim) S[e / 4][e % 4] = -INFINITY;
     }
-    float mx = S[0][0];
-#pragma unroll
-    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, S[e / 4][e % 4]);
+    float mx = fmaxf(fmaxf(fmaxf(S[0][0], S[0][1]), fmaxf(S[0][2], S[0][3])),
+                     fmaxf(fmaxf(S[1][0], S[1][1]), fmaxf(S[1][2], S[1][3])));
     mx = max_lane_halves(max_lane_rows(mx));
     const float m_new = fmaxf(m_run, mx * sl2);
     const float m_sub = m_new == -INFINITY ? 0.f : m_new;
     const float alpha = fast_exp2(m_run - m_sub);
     m_run = m_new;
     float ls = 0.f;
-    bf16x8_t pb[2];
-    const int keep = C.R.n_keys - (kb + 16 * g);  // tokens of the lane's V block that exist
+    bf16x8_t pb;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
+    for (int e = 0; e < 8; ++e) {
       const float x = fast_exp2(fmaf(S[e / 4][e % 4], sl2, -m_sub));
       ls += x;
-      pb[e / 8][e % 8] = (__bf16)(x * e4m3::scale_value(e4m3::byte_of(vs[X], e)));
+      pb[e] = (__bf16)(x * e4m3::scale_value((vs[X][e / 4] >> (8 * (e & 3))) & 255u));
     }
     l_part = fmaf(l_part, alpha, ls);
+    u32x2 v[NDM];  // codes of the lane's eight tokens of row blocks 0 .. NDM-1
+#pragma unroll
+    for (int e = 0; e < NDM / 2; ++e)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const auto r = __builtin_amdgcn_permlane16_swap(vf[X][e][i], vf[X][e][2 + i], false, false);
+        v[2 * e][i] = r[0];
+        v[2 * e + 1][i] = r[1];
+      }
+    if (kb + kStep > C.R.n_keys) {  // tokens past the range's end: their P is 0, but slots may hold anything
+      const int keep = C.R.n_keys - (kb + 8 * g);
+      uint32_t m[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int k = keep - 4 * i;
+        m[i] = k >= 4 ? 0xffffffffu : k <= 0 ? 0u : 0xffffffffu >> (8 * (4 - k));
+      }
+#pragma unroll
+      for (int dm = 0; dm < NDM; ++dm)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) v[dm][i] &= m[i];
+    }
 #pragma unroll
     for (int dm = 0; dm < NDM; ++dm) {
       acc[dm] *= alpha;
-      u32x4 v = vf[X][dm];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int k = keep - 4 * i;
-        v[i] = k >= 4 ? v[i] : k <= 0 ? 0u : v[i] & (0xffffffffu >> (8 * (4 - k)));
-      }
-      acc[dm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(e4m3::values8(v[0], v[1], 1.f), pb[0], acc[dm], 0, 0, 0);
-      acc[dm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(e4m3::values8(v[2], v[3], 1.f), pb[1], acc[dm], 0, 0, 0);
+      acc[dm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(e4m3::values8(v[dm][0], v[dm][1], 1.f), pb, acc[dm], 0, 0, 0);
     }
-    load_v(X);
+    load_v(X);  // set X's V is consumed
     advance(L);
     fetch_ids(L);
     const int ri_before = C.ri;
     advance(C);
-    if (!C.ok) return false;
-    if (C.ri != ri_before) load_lim();
-    return true;
+    if (C.ok && C.ri != ri_before) load_lim();
   };
-  for (bool go = true; go;)
-    tile::static_for<kSets>([&](auto xc) __attribute__((always_inline)) {
-      if (go) go = step(xc);
-    });
+  // Two steps a turn, counted ahead: left from within, the loop would have a path
+  // (for the compiler) from a step to itself, with half of the loads in flight,
+  // and its waits would allow no more.
+  static_assert(kSets == 2, "the loop names both sets");
+  for (; n_steps >= 2; n_steps -= 2) {
+    step(std::integral_constant<int, 0>{});
+    step(std::integral_constant<int, 1>{});
+  }
+  if (n_steps > 0) step(std::integral_constant<int, 0>{});
 
   float lt = l_part + __shfl_xor(l_part, 16);
   lt += __shfl_xor(lt, 32);

@@ -156,8 +156,12 @@ __device__ __forceinline__ void fwd_item(const TileParams& p, int item) {
 
   // One buffer: K stages 0-3, then V stages 0-3 (so every fragment read is a
   // per-lane base plus an immediate offset below 64 KB); limit stages.
-  __shared__ __attribute__((aligned(1024))) uint16_t smem[8 * SEL];
+  // 8-bit caches: four K stages, two V stages, then the codes that wait.
+  constexpr int kRawSlots = 3;
+  constexpr int kStages = E4M3 ? 6 + kRawSlots : 8;
+  __shared__ __attribute__((aligned(1024))) uint16_t smem[kStages * SEL];
   __shared__ int32_t Lb[4][kThreads];
+  __shared__ __attribute__((aligned(16))) uint8_t scale_bytes[E4M3 ? 4 : 1][E4M3 ? kWaves : 1][2 * kBlock];
   constexpr int NBT = KT / kBlock;  // paged blocks per tile
   __shared__ int32_t tile_ids[PAGED ? kMaxItemTiles * NBT : 1];
   static_assert(!PAGED || kMaxItemTiles * NBT == kThreads, "one block id per thread");
@@ -293,7 +297,7 @@ __device__ __forceinline__ void fwd_item(const TileParams& p, int item) {
   };
   // Stage of tile t: t % 4 (compile-time: the loop is unrolled by 4).
   auto kst = [&](auto sc) -> uint16_t* { return smem + (decltype(sc)::value % 4) * SEL; };
-  auto vst = [&](auto sc) -> uint16_t* { return smem + (4 + decltype(sc)::value % 4) * SEL; };
+  auto vst = [&](auto sc) -> uint16_t* { return smem + (4 + decltype(sc)::value % (E4M3 ? 2 : 4)) * SEL; };
   auto lst = [&](auto sc) -> int32_t* { return Lb[decltype(sc)::value % 4]; };
   // Block ids (paged): lane l (mod NBT) of a wavefront holds the id of block
   // l of the tile at cursor c (read from the item's staged ids).
@@ -332,86 +336,113 @@ __device__ __forceinline__ void fwd_item(const TileParams& p, int item) {
     dma4(lb, lim_off < 0 || !valid ? 0u : 4u * tok, lds_addr(dst + wave * 64));
   };
 
-  // 8-bit caches: a thread's 16 codes of K and of V of a tile (64-wide heads: K's
-  // on the first four wavefronts, V's on the others), of cache block `vb` of the
-  // tile, whose scales of V are the same for the whole wavefront.
+  // 8-bit caches.  A tile's codes wait in LDS as they came, three tiles ahead of
+  // their use, each lane's where the lane itself will read them (so that only its
+  // own wavefront waits for them): 16 codes of K and 16 of V a thread (64-wide
+  // heads: K's on the first four wavefronts, V's on the others), of cache block
+  // `vb` of the tile.  From there they go into the stages as bf16: K of tile t+2
+  // and V of tile t+1 in step t.
   using e4m3::u32x4;
   constexpr bool kBoth = D == 128;  // every wavefront has codes of both
-  struct Staged {
-    u32x4 k, v, vs;    // codes; V's scale bytes
-    uint32_t ks;       // K's scale byte
-    int32_t lim, keep; // the column's limit; tokens of the block that exist
-  };
   const int vb = kBoth ? wave >> 1 : wave & 3, unit = kBoth ? tid & 127 : lane;
   const bool has_k = kBoth || wave < 4, has_v = kBoth || wave >= 4;
   const int k_row = vb * kBlock + kslot(unit & 15);
-  auto load_codes = [&](const Cursor& c, Staged& x) {
+  // this wavefront's codes (one piece of K and one of V a slot) and scale bytes (K's, V's)
+  uint8_t* raw = E4M3 ? reinterpret_cast<uint8_t*>(smem + 6 * SEL) + wave * (kRawSlots * (kBoth ? 2048 : 1024)) : nullptr;
+  auto raw_k = [&](int slot) { return raw + slot * 1024; };
+  auto raw_v = [&](int slot) { return raw + (kBoth ? kRawSlots * 1024 : 0) + slot * 1024; };
+  auto ask_block = [&](int tile) -> int { return E4M3 ? tile_ids[min(tile, n_tiles - 1) * NBT + vb] : 0; };
+  auto block_of = [&](int tile) -> int { return __builtin_amdgcn_readfirstlane(ask_block(tile)); };
+  auto load_codes = [&](const void* codes, int64_t blk, uint8_t* dst) {
+    dma16_nt(static_cast<const uint8_t*>(codes) + e4m3::codes_at<D>(blk, kvh, p.Hkv), 16u * unit, lds_addr(dst));
+  };
+  auto load_scales = [&](int64_t blk, int tile) {
     if constexpr (E4M3) {
-      const int64_t blk = __builtin_amdgcn_readlane(tile_blocks(c), vb);
-      const int64_t at = e4m3::codes_at<D>(blk, kvh, p.Hkv), sat = e4m3::scales_at(blk, kvh, p.Hkv);
-      if (has_k) x.k = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(p.k) + at) + unit);
-      if (has_v) x.v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(p.v) + at) + unit);
-      x.ks = p.scales[sat + (unit & 15)];
-      x.vs = *reinterpret_cast<const u32x4*>(p.scales + sat + kBlock);
-      const int32_t* lb = c.R.lim_off < 0 ? &p.work[item].ntok : p.lims + c.R.lim_off;
-      x.lim = lb[c.R.lim_off < 0 || !valid ? 0 : tok];
-      x.keep = c.R.n_keys - c.kt * KT - vb * kBlock;
+      if (lane < 8)
+        dma4(p.scales + e4m3::scales_at(blk, kvh, p.Hkv), 4u * lane, lds_addr(&scale_bytes[tile % 4][wave][0]));
     }
   };
-  // The codes of a tile into stage SC as bf16, in pieces 0 .. 6.  Piece 0: what is
-  // rare, V's tokens past the range's end (zeros: their P is 0, but the slots may
-  // hold anything) and V rows that are NaN (scores of their tokens NaN, through
-  // K's codes, where a column sees them; V itself stays 0).
-  auto place_codes = [&](Staged& x, uint16_t* ks, uint16_t* vs, int32_t* lim, auto kc) {
-    constexpr int k = decltype(kc)::value;
+  u32x4 xk, xv;  // codes on their way
+  uint32_t sk = 0, sn = 0, sv[4];
+  auto read_k = [&](int slot, int tile) {
     if constexpr (E4M3) {
-      if constexpr (k == 0) {
-        uint32_t any = 0;
+      xk = *reinterpret_cast<const u32x4*>(raw_k(slot) + 16 * lane);
+      sk = scale_bytes[tile % 4][wave][unit & 15];
+      sn = scale_bytes[tile % 4][wave][kBlock + (unit & 15)];
+    }
+  };
+  // (a token whose V row is NaN: its score is, where a column sees it)
+  auto place_k = [&](uint16_t* st, auto hc) {
+    constexpr int h = decltype(hc)::value;
+    if constexpr (E4M3) {
+      const uint32_t lo = sn == e4m3::kNan ? e4m3::kNanCodes : xk[2 * h], hi = sn == e4m3::kNan ? e4m3::kNanCodes : xk[2 * h + 1];
+      *reinterpret_cast<bf16x8_t*>(st + k_row * D + 8 * ((2 * (unit >> 4) + h) ^ Gm::kswz(k_row))) =
+          e4m3::values8(lo, hi, e4m3::scale_value(sk));
+    }
+  };
+  // keep: tokens of the tile that exist.  The codes of the others are cleared (their
+  // P is 0, but slots may hold anything, and 0 * NaN is NaN), and so are the scale
+  // bytes of rows that are NaN (whose codes are 0).
+  auto read_v = [&](int slot, int tile) {
+    if constexpr (E4M3) {
+      xv = *reinterpret_cast<const u32x4*>(raw_v(slot) + 16 * lane);
+      const u32x4 y = *reinterpret_cast<const u32x4*>(&scale_bytes[tile % 4][wave][kBlock]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x.vs[i] = __builtin_amdgcn_readfirstlane(x.vs[i]);
-          any |= (~x.vs[i] - 0x01010101u) & x.vs[i] & 0x80808080u;
-        }
-        if (any != 0 || x.keep < kBlock) {
+      for (int i = 0; i < 4; ++i) sv[i] = y[i];
+    }
+  };
+  auto trim_v = [&](int keep) {
+    uint32_t any = 0;
 #pragma unroll
-          for (int e = 0; e < kBlock; ++e) {
-            const uint32_t m = 255u << (8 * (e & 3));
-            if ((x.vs[e >> 2] & m) == m) {
-              if ((unit & 15) == e) x.k = u32x4{e4m3::kNanCodes, e4m3::kNanCodes, e4m3::kNanCodes, e4m3::kNanCodes};
-              x.vs[e >> 2] &= ~m;
-            }
-            if (e >= x.keep) x.v[e >> 2] &= ~m;
-          }
-        }
-        lim[tid] = x.lim;
-      }
-      if constexpr (k == 1 || k == 2) {
-        if (has_k) {
-          const int c = 2 * (unit >> 4) + k - 1;
-          *reinterpret_cast<bf16x8_t*>(ks + k_row * D + 8 * (c ^ Gm::kswz(k_row))) =
-              e4m3::values8(x.k[2 * k - 2], x.k[2 * k - 1], e4m3::scale_value(x.ks));
-        }
-      }
-      if constexpr (k >= 3) {
-        constexpr int i = k - 3;  // tokens 4i .. 4i+3, in x.v[i] from here on as two pairs of bf16
-        if (has_v) {
-          uint32_t y[2];
+    for (int i = 0; i < 4; ++i) {
+      sv[i] = __builtin_amdgcn_readfirstlane(sv[i]);
+      any |= (~sv[i] - 0x01010101u) & sv[i] & 0x80808080u;
+    }
+    keep -= vb * kBlock;
+    if (any != 0 || keep < kBlock) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-            const float s0 = __uint_as_float(((x.vs[i] >> (16 * h)) & 255u) << 23);
-            const float s1 = __uint_as_float(((x.vs[i] >> (16 * h + 8)) & 255u) << 23);
-            const bf16x2 a = h == 0 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x.v[i], s0, false)
-                                    : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x.v[i], s0, true);
-            const bf16x2 b = h == 0 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x.v[i], s1, false)
-                                    : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x.v[i], s1, true);
-            y[h] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060100u);
-          }
-          const int d = unit;
-          *reinterpret_cast<uint2*>(vs + (vb * D + d) * kBlock + 8 * ((i >> 1) ^ ((d >> 3) & 1)) + 4 * (i & 1)) = make_uint2(y[0], y[1]);
-        }
+      for (int e = 0; e < kBlock; ++e) {
+        const uint32_t m = 255u << (8 * (e & 3));
+        if ((sv[e >> 2] & m) == m) sv[e >> 2] &= ~m;
+        if (e >= keep) xv[e >> 2] &= ~m;
       }
     }
+  };
+  auto place_v = [&](uint16_t* st, auto jc) {  // tokens 8j .. 8j+7
+    constexpr int j = decltype(jc)::value;
+    if constexpr (E4M3) {
+      typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+      u32x4 y;
+      static_for<4>([&](auto qc) {  // two tokens
+        constexpr int i = 2 * j + decltype(qc)::value / 2, h = decltype(qc)::value % 2;
+        const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(xv[i], e4m3::scale_value((sv[i] >> (16 * h)) & 255u), h);
+        const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(xv[i], e4m3::scale_value((sv[i] >> (16 * h + 8)) & 255u), h);
+        y[decltype(qc)::value] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060100u);
+      });
+      *reinterpret_cast<u32x4*>(st + (vb * D + unit) * kBlock + 8 * (j ^ ((unit >> 3) & 1))) = y;
+    }
+  };
+  // Step t's loads: the limits of tile t+3, codes of K of tile t+5 with its scales,
+  // of V of tile t+4 (64-wide heads: each wavefront the scales of what it loads).
+  // `rk`, `rv`: the slots freed by the tiles placed in this step.
+  constexpr int kStepLoads = kBoth ? 4 : 3;
+  int id_v = 0;  // (128-wide heads) block of V's next load
+  int slot = 2;  // slot of K of tile t+2
+  auto before = [](int x) { return x == 0 ? kRawSlots - 1 : x - 1; };
+  auto ask_step = [&](int t) -> int { return ask_block(kBoth || has_k ? t + 5 : t + 4); };
+  auto load_step = [&](int t, int asked) {
+    const int id = __builtin_amdgcn_readfirstlane(asked);
+    if constexpr (kBoth) {
+      load_codes(p.k, id, raw_k(slot));
+      load_scales(id, t + 5);
+      load_codes(p.v, id_v, raw_v(before(slot)));
+      id_v = id;
+    } else {
+      const int tile = has_k ? t + 5 : t + 4;
+      load_codes(has_k ? p.k : p.v, id, raw + (has_k ? slot : before(slot)) * 1024);
+      load_scales(id, tile);
+    }
+    slot = slot == kRawSlots - 1 ? 0 : slot + 1;
   };
 
   Cursor Lk{0, 0, R0, 1, 0};  // next tile to load (K, V, limits)
@@ -568,7 +599,7 @@ __device__ __forceinline__ void fwd_item(const TileParams& p, int item) {
   // O^T += V^T P^T from V stage vsc%4 (rvb: per-lane bases), with hook(i)
   // after MFMA i.
   auto pv_product = [&](auto vsc, auto&& hook) {
-    constexpr int VS = decltype(vsc)::value % 4;
+    constexpr int VS = decltype(vsc)::value % (E4M3 ? 2 : 4);
     auto frag = [&](int i) -> bf16x8_t {
       const int g = i / NDB, db = i % NDB;
       if constexpr (PAGED) {
@@ -631,21 +662,52 @@ __device__ __forceinline__ void fwd_item(const TileParams& p, int item) {
     __builtin_amdgcn_s_waitcnt(0xC07F);  // the ids are in LDS; Q may be on its way
     bar();
   }
-  // 8-bit caches: tiles 0 and 1 placed, tile 2 in registers.
-  constexpr int kPlace = 7;  // pieces of place_codes
-  Staged staged;
-  auto load_staged = [&](Staged& x) {
-    load_codes(Lk, x);
-    advance(Lk);
-  };
   if constexpr (E4M3) {
-    Staged other;
-    load_staged(staged);
-    load_staged(other);
-    static_for<kPlace>([&](auto kc) { place_codes(staged, smem, smem + 4 * SEL, Lb[0], kc); });
-    load_staged(staged);
-    static_for<kPlace>([&](auto kc) { place_codes(other, smem + SEL, smem + 5 * SEL, Lb[1], kc); });
+    // Tiles 0 to 2 asked for, K of tiles 0 and 1 and V of tile 0 placed; then K of
+    // tiles 3 and 4 and V of tile 3.
+    const int id0 = block_of(0), id1 = block_of(1), id2 = block_of(2), id3 = block_of(3), id4 = block_of(4);
+    if constexpr (kBoth) {
+      load_codes(p.k, id0, raw_k(0)), load_scales(id0, 0), load_codes(p.v, id0, raw_v(0));
+      load_codes(p.k, id1, raw_k(1)), load_scales(id1, 1);
+    } else if (has_k) {
+      load_codes(p.k, id0, raw_k(0)), load_scales(id0, 0);
+      load_codes(p.k, id1, raw_k(1)), load_scales(id1, 1);
+    } else {
+      load_codes(p.v, id0, raw_v(0)), load_scales(id0, 0);
+    }
+    for (int i = 0; i < 2; ++i) load_lim(Lk, Lb[i]), advance(Lk);
+    if constexpr (kBoth) {
+      load_codes(p.v, id1, raw_v(1)), load_codes(p.k, id2, raw_k(2)), load_scales(id2, 2), load_codes(p.v, id2, raw_v(2));
+    } else if (has_k) {
+      load_codes(p.k, id2, raw_k(2)), load_scales(id2, 2);
+    } else {
+      load_codes(p.v, id1, raw_v(1)), load_scales(id1, 1), load_codes(p.v, id2, raw_v(2)), load_scales(id2, 2);
+    }
+    load_lim(Lk, Lb[2]), advance(Lk);
+    wait_vm<kBoth ? 5 : 3>();
+    asm volatile("" ::: "memory");
+    if (has_k) {
+      read_k(0, 0);
+      place_k(smem, I0{}), place_k(smem, I1{});
+      read_k(1, 1);
+      place_k(smem + SEL, I0{}), place_k(smem + SEL, I1{});
+    }
+    if (has_v) {
+      read_v(0, 0);
+      trim_v(R0.n_keys);
+      place_v(smem + 4 * SEL, I0{}), place_v(smem + 4 * SEL, I1{});
+    }
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0xC07F);
+    if constexpr (kBoth) {
+      load_codes(p.k, id3, raw_k(0)), load_scales(id3, 3), load_codes(p.k, id4, raw_k(1)), load_scales(id4, 4);
+      load_codes(p.v, id3, raw_v(0));
+      id_v = id4;
+    } else if (has_k) {
+      load_codes(p.k, id3, raw_k(0)), load_scales(id3, 3), load_codes(p.k, id4, raw_k(1)), load_scales(id4, 4);
+    } else {
+      load_codes(p.v, id3, raw_v(0)), load_scales(id3, 3);
+    }
     bar();
   } else {
     load_next(I0{});
@@ -668,11 +730,23 @@ __device__ __forceinline__ void fwd_item(const TileParams& p, int item) {
     // head: 569 -> 563; all columns used: no difference).
     for (int t = 0; t < n_tiles; ++t) {
       if constexpr (E4M3) {
+        wait_vm<2 * kStepLoads - 1>();
         __builtin_amdgcn_s_waitcnt(0xC07F);
         bar();
-        uint16_t* ks = smem + ((t + 2) % 4) * SEL;
-        static_for<kPlace>([&](auto kc) { place_codes(staged, ks, ks + 4 * SEL, Lb[(t + 2) % 4], kc); });
-        load_staged(staged);
+        advance(C);
+        if (has_k) {
+          read_k(slot, t + 2);
+          place_k(smem + ((t + 2) % 4) * SEL, I0{}), place_k(smem + ((t + 2) % 4) * SEL, I1{});
+        }
+        if (has_v) {
+          read_v(before(slot), t + 1);
+          trim_v(C.R.n_keys - C.kt * KT);
+          uint16_t* st = smem + (4 + (t + 1) % 2) * SEL;
+          place_v(st, I0{}), place_v(st, I1{});
+        }
+        load_lim(Lk, Lb[(t + 3) % 4]);
+        advance(Lk);
+        load_step(t, ask_step(t));
         continue;
       }
       wait_vm<2 * IPW + 1>();
@@ -708,10 +782,12 @@ __device__ __forceinline__ void fwd_item(const TileParams& p, int item) {
     constexpr int SC = decltype(sc)::value;
     using Y = std::integral_constant<int, SC % 2>;
     using YN = std::integral_constant<int, (SC + 1) % 2>;
-    if constexpr (E4M3)
-      __builtin_amdgcn_s_waitcnt(0xC07F);  // this wavefront has placed its codes of tile t+1
-    else
+    if constexpr (E4M3) {
+      wait_vm<2 * kStepLoads - 1>();  // this wavefront's loads of step t-3, and the limits of step t-2, have landed
+      __builtin_amdgcn_s_waitcnt(0xC07F);  // its codes of K of tile t+1 and of V of tile t are in their stages
+    } else {
       wait_vm<2 * IPW + 1>();  // this wavefront's loads of step t-2 have landed
+    }
     bar();
     ls0 = 0.f;
     ls1 = 0.f;
@@ -749,18 +825,39 @@ __device__ __forceinline__ void fwd_item(const TileParams& p, int item) {
       zero_v_tail(vst(std::integral_constant<int, SC + 1>{}));
     }
     const int ids = E4M3 ? 0 : tile_blocks(Lk);
+    int next_id = 0;
     pv_product(std::integral_constant<int, SC>{}, [&](auto ic) {
       constexpr int i = decltype(ic)::value;
       static_for<kPieces / NB>([&](auto uc) {
         fma_piece(YN{}, std::integral_constant<int, i * (kPieces / NB) + decltype(uc)::value>{});
       });
       if constexpr (E4M3) {
-        // the codes of tile t+2, and those of tile t+3 asked for
-        using Next = std::integral_constant<int, SC + 2>;
-        constexpr int first = NB - 1 - kPlace;
-        if constexpr (i >= first && i < first + kPlace)
-          place_codes(staged, kst(Next{}), vst(Next{}), lst(Next{}), std::integral_constant<int, i - first>{});
-        if constexpr (i == NB - 1) load_staged(staged);
+        // K of tile t+2 and V of tile t+1 into their stages, spread over the products
+        constexpr int u = NB / 8;
+        using Next = std::integral_constant<int, SC + 1>;
+        uint16_t* ks = kst(std::integral_constant<int, SC + 2>{});
+        if constexpr (i == 0) {
+          if (has_k) read_k(slot, t + 2);
+          next_id = ask_step(t);
+        }
+        if constexpr (i == 2 * u || i == 2 * u + 1) {
+          if (has_k) place_k(ks, std::integral_constant<int, i - 2 * u>{});
+        }
+        if constexpr (i == (kBoth ? 6 : 0)) {
+          if (has_v) read_v(before(slot), t + 1);
+        }
+        if constexpr (i == (kBoth ? 9 : 2)) {
+          if (has_v) trim_v(C.R.n_keys - C.kt * KT);
+        }
+        constexpr int v0 = kBoth ? 10 : 3, apart = kBoth ? 2 : 1;
+        if constexpr (i == v0 || i == v0 + apart) {
+          if (has_v) place_v(vst(Next{}), std::integral_constant<int, (i - v0) / apart>{});
+        }
+        if constexpr (i == NB - 1) {
+          load_lim(Lk, lst(std::integral_constant<int, SC + 3>{}));
+          advance(Lk);
+          load_step(t, next_id);
+        }
         return;
       }
       if constexpr (i == NB / 2) load_tile(Kg, Lk, kst(std::integral_constant<int, SC + 3>{}), ld_k, false, ids);
