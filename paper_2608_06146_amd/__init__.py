@@ -21,6 +21,7 @@ results are read elsewhere after a wait).
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
 import struct
 from typing import Optional, Sequence
@@ -807,8 +808,11 @@ def rotary_append(q, k, v, positions, slots, k_cache, v_cache, rotary: Rotary, q
     if stream is not None:
         return _on_stream(stream, _rows_of(rotary, q if k is None else k)[0], rotary_append, q, k, v, positions, slots,
                           k_cache, v_cache, rotary, q_weight, k_weight, q_positions, q_out, None, scales)
-    if rotary._rows is not None and scales is None:
-        done = rotary._rows.append(q, k, v, positions, slots, k_cache, v_cache, q_weight, k_weight, q_positions, q_out)
+    if rotary._rows is not None:
+        done = (rotary._rows.append(q, k, v, positions, slots, k_cache, v_cache, q_weight, k_weight, q_positions, q_out)
+                if scales is None else
+                rotary._rows.append(q, k, v, positions, slots, k_cache, v_cache, q_weight, k_weight, q_positions, q_out,
+                                    scales))
         if done is not None:
             return done[0] if type(done) is tuple else _lib.check(done)
     import torch
@@ -926,9 +930,19 @@ def empty_cache_e4m3(num_blocks: int, num_heads_kv: int, head_dim: int, device):
             torch.empty((num_blocks, num_heads_kv, 2, 16), dtype=torch.float8_e8m0fnu, device=device))
 
 
-def _cast_blocks(f, k_cache, v_cache, e4m3, pairs, pairs_host, back):
+@functools.lru_cache(maxsize=None)
+def _native_cast(back):
+    return _lib.native_cast_blocks(back)
+
+
+def _cast_blocks(k_cache, v_cache, e4m3, pairs, pairs_host, back):
     """Blocks between caches of values and an 8-bit cache."""
+    if pairs_host is None:
+        done = _native_cast(back)(k_cache, v_cache, *e4m3, pairs)
+        if done is not None:
+            return _lib.check(done)
     import torch
+    f = _lib.lib().padoc_cache_dequantize if back else _lib.lib().padoc_cache_quantize
     dev, dt = k_cache.device, k_cache.dtype
     if not k_cache.is_cuda:
         raise ValueError(f"k_cache is on {dev}, expected a GPU")
@@ -974,7 +988,7 @@ def cache_quantize(k_cache, v_cache, k_dst=None, v_dst=None, scales_dst=None, pa
         if v_cache.dim() != 4:
             raise ValueError(f"v_cache must be [blocks, Hkv, d, 16], got {tuple(v_cache.shape)}")
         k_dst, v_dst, scales_dst = empty_cache_e4m3(*v_cache.shape[:3], k_cache.device)
-    _cast_blocks(_lib.lib().padoc_cache_quantize, k_cache, v_cache, (k_dst, v_dst, scales_dst), pairs, pairs_host, False)
+    _cast_blocks(k_cache, v_cache, (k_dst, v_dst, scales_dst), pairs, pairs_host, False)
     return k_dst, v_dst, scales_dst
 
 
@@ -1001,7 +1015,7 @@ def cache_dequantize(k_cache, v_cache, scales, k_dst=None, v_dst=None, dtype: st
         nb, hkv, d = _check_cache_e4m3(k_cache, v_cache, scales, k_cache.device)
         k_dst = torch.empty((nb, hkv, d // 8, 16, 8), dtype=dt, device=k_cache.device)
         v_dst = torch.empty((nb, hkv, d, 16), dtype=dt, device=k_cache.device)
-    _cast_blocks(_lib.lib().padoc_cache_dequantize, k_dst, v_dst, (k_cache, v_cache, scales), pairs, pairs_host, True)
+    _cast_blocks(k_dst, v_dst, (k_cache, v_cache, scales), pairs, pairs_host, True)
     return k_dst, v_dst
 
 

@@ -261,7 +261,8 @@ def rows(handle, head_dim: int, n_axes: int, bf16: bool):
         return None
     L = lib()
     at = [C.cast(getattr(L, f), C.c_void_p).value
-          for f in ("padoc_rotary_fwd", "padoc_rotary_bwd", "padoc_rotary_bwd_workspace_bytes", "padoc_rotary_append")]
+          for f in ("padoc_rotary_fwd", "padoc_rotary_bwd", "padoc_rotary_bwd_workspace_bytes", "padoc_rotary_append",
+                    "padoc_rotary_append_e4m3")]
     return m.Rows(handle.value, *at, head_dim, n_axes, bf16)
 
 
@@ -273,6 +274,18 @@ def native_copy_blocks():
         return lambda k_cache, v_cache, pairs: None
     f, address = m.copy_blocks, C.cast(lib().padoc_cache_copy_blocks, C.c_void_p).value
     return lambda k_cache, v_cache, pairs: f(address, k_cache, v_cache, pairs)
+
+
+def native_cast_blocks(back: bool):
+    """``cast_blocks(k, v, k_codes, v_codes, scales, pairs)`` of the native
+    module (values to codes, or ``back``), or a function that leaves every
+    call to the caller."""
+    m = native_rows()
+    if m is None:
+        return lambda *tensors: None
+    entry = lib().padoc_cache_dequantize if back else lib().padoc_cache_quantize
+    f, address = m.cast_blocks, C.cast(entry, C.c_void_p).value
+    return lambda *tensors: f(address, back, *tensors)
 
 
 def check(status: int) -> None:

@@ -1,8 +1,9 @@
-// Python's calls of the rotary entry points and padoc_cache_copy_blocks, for
-// layers of a decode step whose kernels are shorter than the call: the checks
-// and the packing of a call take some 4 us more in Python than here (forward of 81
-// rows 13.1 and 9.9 us a call, of which its launch 4.3; append 14.0 and 9.1,
-// backward 22.0 and 15.1, block copy 6.0 and 3.2).
+// Python's calls of the rotary entry points, padoc_cache_copy_blocks and the
+// casts of 8-bit caches, for layers of a decode step whose kernels are shorter
+// than the call: the checks and the packing of a call take some 4 us more in
+// Python than here (forward of 81 rows 13.1 and 9.9 us a call, of which its launch
+// 4.3; append 14.0 and 9.1, into an 8-bit cache 16.9 and 7.8, backward 22.0 and
+// 15.1, block copy 6.0 and 3.2, cast of 160 blocks 8.3 and 4.0).
 //
 // Each function makes the call where its arguments are in order and the stream
 // is the tensors' device's current one, and otherwise returns None: the Python
@@ -24,6 +25,10 @@ using Fwd = padoc_status (*)(const padoc_rotary*, const padoc_rotary_fwd_args*, 
 using Bwd = padoc_status (*)(const padoc_rotary*, const padoc_rotary_bwd_args*, void*, size_t, hipStream_t);
 using BwdBytes = padoc_status (*)(const padoc_rotary*, int64_t, int32_t, int32_t, size_t*);
 using Append = padoc_status (*)(const padoc_rotary*, const padoc_rotary_append_args*, hipStream_t);
+using AppendE4m3 = padoc_status (*)(const padoc_rotary*, const padoc_rotary_append_args*, const padoc_cache_e4m3*,
+                                    hipStream_t);
+using Quantize = decltype(&padoc_cache_quantize);
+using Dequantize = decltype(&padoc_cache_dequantize);
 using Copy = padoc_status (*)(const void*, const void*, int64_t, void*, void*, int64_t, const int32_t*, int64_t,
                               const int32_t*, int32_t, int32_t, padoc_dtype, hipStream_t);
 
@@ -34,6 +39,7 @@ struct Rows {
   Bwd bwd;
   BwdBytes bwd_bytes;
   Append append;
+  AppendE4m3 append_e4m3;
   int64_t d, axes;
   at::ScalarType dtype;
 };
@@ -96,6 +102,26 @@ Caches caches(const at::Tensor& k, const at::Tensor& v, const Where& w) {
   const Caches c{v.size(0), v.size(1), v.size(2)};
   need(v.size(3) == 16 && k.size(0) == c.blocks && k.size(1) == c.heads && k.size(2) == c.d / 8 && k.size(3) == 16 &&
        k.size(4) == 8);
+  return c;
+}
+
+// An 8-bit cache (written or read).
+Caches caches_e4m3(const at::Tensor& k, const at::Tensor& v, const at::Tensor& s, const Where& w, bool written,
+                   padoc_cache_e4m3* out) {
+  need(k.device() == w.device && v.device() == w.device && s.device() == w.device &&
+       k.scalar_type() == at::kFloat8_e4m3fn && v.scalar_type() == at::kFloat8_e4m3fn &&
+       s.scalar_type() == at::kFloat8_e8m0fnu && k.is_contiguous() && v.is_contiguous() && s.is_contiguous() &&
+       v.dim() == 4 && k.dim() == 5 && s.dim() == 4);
+  const Caches c{v.size(0), v.size(1), v.size(2)};
+  need(v.size(3) == 16 && k.size(0) == c.blocks && k.size(1) == c.heads && k.size(2) == c.d / 16 && c.d % 16 == 0 &&
+       k.size(3) == 16 && k.size(4) == 16 && s.size(0) == c.blocks && s.size(1) == c.heads && s.size(2) == 2 &&
+       s.size(3) == 16);
+  auto at = [&](const at::Tensor& t) { return written ? t.data_ptr() : const_cast<void*>(t.const_data_ptr()); };
+  *out = padoc_cache_e4m3{};
+  out->k = at(k);
+  out->v = at(v);
+  out->scales = at(s);
+  out->num_blocks = c.blocks;
   return c;
 }
 
@@ -257,10 +283,10 @@ PyObject* rows_bwd(PyObject* self, PyObject* const* a, Py_ssize_t count) {
 }
 
 // append(q, k, v, positions, slots, k_cache, v_cache, q_weight, k_weight,
-// q_positions, q_out) -> (q_out,)
+// q_positions, q_out[, scales]) -> (q_out,)
 PyObject* rows_append(PyObject* self, PyObject* const* a, Py_ssize_t count) {
   return call([&]() -> PyObject* {
-    need(count == 11);
+    need(count == 11 || count == 12);
     const Rows* r = reinterpret_cast<Rows*>(self);
     const at::Tensor *q = tensor(a[0]), *k = tensor(a[1]), *v = tensor(a[2]);
     const at::Tensor *kc = tensor(a[5]), *vc = tensor(a[6]);
@@ -273,11 +299,19 @@ PyObject* rows_append(PyObject* self, PyObject* const* a, Py_ssize_t count) {
     p.v = heads(*v, r, w, p.n_new, p.num_heads_kv);
     p.pos = positions(tensor(a[3]), r, w, p.n_new, &p.pos_stride);
     p.slots = pairs(tensor(a[4]), w, p.n_new);
-    const Caches c = caches(*kc, *vc, w);
-    need(kc->scalar_type() == r->dtype && c.heads == p.num_heads_kv && c.d == r->d);
-    p.k_cache = kc->data_ptr();
-    p.v_cache = vc->data_ptr();
-    p.num_blocks = c.blocks;
+    padoc_cache_e4m3 e4m3{};
+    if (count == 12) {
+      const at::Tensor* sc = tensor(a[11]);
+      need(sc);
+      const Caches c = caches_e4m3(*kc, *vc, *sc, w, /*written=*/true, &e4m3);
+      need(c.heads == p.num_heads_kv && c.d == r->d);
+    } else {
+      const Caches c = caches(*kc, *vc, w);
+      need(kc->scalar_type() == r->dtype && c.heads == p.num_heads_kv && c.d == r->d);
+      p.k_cache = kc->data_ptr();
+      p.v_cache = vc->data_ptr();
+      p.num_blocks = c.blocks;
+    }
     p.q_weight = weight(tensor(a[7]), r, w);
     p.k_weight = weight(tensor(a[8]), r, w);
     Out qo;
@@ -289,7 +323,9 @@ PyObject* rows_append(PyObject* self, PyObject* const* a, Py_ssize_t count) {
       if (a[9] != Py_None) p.q_pos = positions(tensor(a[9]), r, w, p.n_q, &p.q_pos_stride);
       p.q_out = (qo = out_rows(a[10], *q, r, w, p.n_q, p.num_heads_q)).at;
     }
-    const padoc_status st = unlocked([&] { return r->append(r->handle, &p, w.stream); });
+    const padoc_status st = unlocked([&] {
+      return count == 12 ? r->append_e4m3(r->handle, &p, &e4m3, w.stream) : r->append(r->handle, &p, w.stream);
+    });
     if (st != PADOC_OK) return PyLong_FromLong(st);
     return Py_BuildValue("(N)", q ? qo.take() : Py_NewRef(Py_None));
   });
@@ -315,12 +351,49 @@ PyObject* rows_copy(PyObject*, PyObject* const* a, Py_ssize_t count) {
   });
 }
 
-// Rows(handle, fwd, bwd, bwd_workspace_bytes, append, head_dim, n_axes, bf16)
+// cast_blocks(function, back, k, v, k_codes, v_codes, scales, pairs or None) -> 0:
+// values to codes, or codes to values
+PyObject* rows_cast(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  return call([&]() -> PyObject* {
+    need(count == 8);
+    void* function = PyLong_AsVoidPtr(a[0]);
+    const bool back = a[1] == Py_True;
+    const at::Tensor *k = tensor(a[2]), *v = tensor(a[3]);
+    const at::Tensor *kc = tensor(a[4]), *vc = tensor(a[5]), *sc = tensor(a[6]);
+    need(function && k && v && kc && vc && sc);
+    const Where w(*k);
+    const Caches c = caches(*k, *v, w);
+    need(k->scalar_type() == at::kBFloat16 || k->scalar_type() == at::kFloat);
+    const padoc_dtype dt = k->scalar_type() == at::kBFloat16 ? PADOC_BF16 : PADOC_F32;
+    padoc_cache_e4m3 e{};
+    const Caches c8 = caches_e4m3(*kc, *vc, *sc, w, !back, &e);
+    need(c8.heads == c.heads && c8.d == c.d);
+    const int32_t* p = nullptr;
+    int64_t n = c.blocks;
+    if (a[7] != Py_None) {
+      p = pairs(tensor(a[7]), w, -1);
+      n = tensor(a[7])->size(0);
+    } else {
+      need(c8.blocks == c.blocks);
+    }
+    auto at = [&](const at::Tensor* t) { return back ? t->data_ptr() : const_cast<void*>(t->const_data_ptr()); };
+    void *kp = at(k), *vp = at(v);
+    return PyLong_FromLong(unlocked([&] {
+      return back ? reinterpret_cast<Dequantize>(function)(&e, kp, vp, c.blocks, p, n, nullptr, (int32_t)c.heads,
+                                                           (int32_t)c.d, dt, w.stream)
+                  : reinterpret_cast<Quantize>(function)(kp, vp, c.blocks, &e, p, n, nullptr, (int32_t)c.heads,
+                                                         (int32_t)c.d, dt, w.stream);
+    }));
+  });
+}
+
+// Rows(handle, fwd, bwd, bwd_workspace_bytes, append, append_e4m3, head_dim, n_axes, bf16)
 PyObject* rows_new(PyTypeObject* type, PyObject* args, PyObject*) {
-  unsigned long long handle, fwd, bwd, bytes, append;
+  unsigned long long handle, fwd, bwd, bytes, append, append_e4m3;
   long long d, axes;
   int bf16;
-  if (!PyArg_ParseTuple(args, "KKKKKLLp", &handle, &fwd, &bwd, &bytes, &append, &d, &axes, &bf16)) return nullptr;
+  if (!PyArg_ParseTuple(args, "KKKKKKLLp", &handle, &fwd, &bwd, &bytes, &append, &append_e4m3, &d, &axes, &bf16))
+    return nullptr;
   Rows* r = reinterpret_cast<Rows*>(type->tp_alloc(type, 0));
   if (!r) return nullptr;
   r->handle = reinterpret_cast<const padoc_rotary*>((uintptr_t)handle);
@@ -328,6 +401,7 @@ PyObject* rows_new(PyTypeObject* type, PyObject* args, PyObject*) {
   r->bwd = reinterpret_cast<Bwd>((uintptr_t)bwd);
   r->bwd_bytes = reinterpret_cast<BwdBytes>((uintptr_t)bytes);
   r->append = reinterpret_cast<Append>((uintptr_t)append);
+  r->append_e4m3 = reinterpret_cast<AppendE4m3>((uintptr_t)append_e4m3);
   r->d = d;
   r->axes = axes;
   r->dtype = bf16 ? at::kBFloat16 : at::kFloat;
@@ -356,7 +430,9 @@ PyType_Slot kSlots[] = {{Py_tp_new, reinterpret_cast<void*>(rows_new)},
 
 PyType_Spec kSpec = {"paper_2608_06146_amd._rows.Rows", sizeof(Rows), 0, Py_TPFLAGS_DEFAULT, kSlots};
 
-PyMethodDef kFunctions[] = {{"copy_blocks", fast(rows_copy), METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr}};
+PyMethodDef kFunctions[] = {{"copy_blocks", fast(rows_copy), METH_FASTCALL, nullptr},
+                            {"cast_blocks", fast(rows_cast), METH_FASTCALL, nullptr},
+                            {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_rows", nullptr, -1, kFunctions, nullptr, nullptr, nullptr, nullptr};
 

@@ -6,10 +6,22 @@ import torch
 
 from oracle import e4m3 as orc
 import paper_2608_06146_amd as pa
+from paper_2608_06146_amd import _lib
 from _e4m3 import on_gpu, on_host
 from _rotary import Setup, check, f64, normal, positions
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True, params=["native", "python"])
+def binding(request, monkeypatch):
+    """Every test through the native module and without it."""
+    if request.param == "python":
+        monkeypatch.setattr(_lib, "native_rows", lambda: None)
+        monkeypatch.setattr(pa, "_native_cast", lambda back: lambda *a: None)
+    else:
+        assert _lib.native_rows() is not None, "the native module is not built"
+    return request.param
 
 
 def places(n, blocks, seed, together=False):

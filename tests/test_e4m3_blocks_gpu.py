@@ -6,10 +6,22 @@ import torch
 
 from oracle import e4m3 as orc
 import paper_2608_06146_amd as pa
+from paper_2608_06146_amd import _lib
 from _e4m3 import on_gpu, on_host
 from _rotary import f64, k_block_view, torch_dtype, v_block_view
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True, params=["native", "python"])
+def binding(request, monkeypatch):
+    """Every test through the native module and without it."""
+    if request.param == "python":
+        monkeypatch.setattr(_lib, "native_rows", lambda: None)
+        monkeypatch.setattr(pa, "_native_cast", lambda back: lambda *a: None)
+    else:
+        assert _lib.native_rows() is not None, "the native module is not built"
+    return request.param
 
 
 def value_rows(blocks, hkv, d, dtype, seed):
@@ -183,3 +195,44 @@ def test_refusals():
             pa.cache_copy_blocks(*args, **kw)
     with pytest.raises(pa.PadocError):
         pa.cache_quantize(k, v, k8, v8, s8, pairs=pairs, pairs_host=np.array([[0, 4]], np.int32))
+
+
+def lazily(t):
+    """A clone that shares t's memory until one of them is written."""
+    c = t.view(torch.uint8)._lazy_clone().view(t.dtype)
+    assert torch._C._is_cow_tensor(c)
+    return c
+
+
+def test_outputs_that_share_memory(binding):
+    """Codes written into lazy clones leave the caches that those were cloned from."""
+    k = torch.randn(3, 2, 8, 16, 8, device="cuda", dtype=torch.bfloat16)
+    v = torch.randn(3, 2, 64, 16, device="cuda", dtype=torch.bfloat16)
+    held = [torch.zeros_like(t.view(torch.uint8)).view(t.dtype) for t in pa.empty_cache_e4m3(3, 2, 64, "cuda")]
+    to = [lazily(t) for t in held]
+    if binding == "native":
+        assert pa._native_cast(False)(k, v, *to, None) == 0
+    else:
+        pa.cache_quantize(k, v, *to)
+    assert all((t.view(torch.uint8) == 0).all() for t in held)
+    want = pa.cache_quantize(k, v)
+    assert all((a.view(torch.uint8) == b.view(torch.uint8)).all() for a, b in zip(to, want))
+    kd, vd = torch.zeros_like(k), torch.zeros_like(v)
+    k2, v2 = kd._lazy_clone(), vd._lazy_clone()
+    pa.cache_dequantize(*want, k2, v2)
+    assert (kd == 0).all() and (vd == 0).all() and (k2 != 0).any()
+
+
+def test_native_calls_leave_what_they_cannot_check(binding):
+    """Odd calls come back unanswered, and the Python function says what is wrong (or makes the call)."""
+    if binding != "native":
+        return
+    k = torch.zeros(2, 1, 8, 16, 8, device="cuda", dtype=torch.bfloat16)
+    v = torch.zeros(2, 1, 64, 16, device="cuda", dtype=torch.bfloat16)
+    e = pa.empty_cache_e4m3(2, 1, 64, "cuda")
+    cast = pa._native_cast(False)
+    assert cast(k, v, *e, None) == 0
+    for bad in ((k.half(), v, *e, None), (k, v.cpu(), *e, None), (k, v, e[0], e[1], e[2].view(torch.uint8), None),
+                (k, v, e[0][:1], e[1], e[2], None), (k, v, *[t[:1] for t in e], None),
+                (k, v, *e, torch.zeros(2, 2, device="cuda")), (k, v, *e, torch.zeros(2, 2, dtype=torch.int32))):
+        assert cast(*bad) is None
