@@ -639,45 +639,160 @@ __device__ __forceinline__ uint32_t quantize_row(const float (&x)[N], uint32_t (
   return b;
 }
 
-// Append into an 8-bit cache: items of four roles, as above, but v's tiles are
-// cut like k's: a group takes a row of one head, and its lanes leave a byte per
-// dimension (d-major V).
-template <typename T, int D, bool PAIRS, bool STREAM>
-__global__ __launch_bounds__(kThreads) void rotary_append_e4m3_kernel(const RotaryParams p) {
-  __shared__ AngleTable<T, D, PAIRS> table;
+// V's codes of one row and head, byte by byte (d-major V).
+template <typename T, int D, bool PAIRS>
+__device__ __forceinline__ void store_bytes(uint8_t* dst, const Place<T, D, PAIRS>& pl, const uint32_t (&codes)[kElems<D> / 4]) {
+  constexpr int E = kUnit<T>;
+#pragma unroll
+  for (int i = 0; i < kElems<D>; ++i) dst[(pl.at[i / E] + i % E) * kBlock] = (uint8_t)(codes[i / 4] >> (8 * (i % 4)));
+}
+
+// V rows of a prefill into an 8-bit cache: ROWS consecutive new rows of one head
+// a workgroup, whose codes are staged.  Sixteen rows that fill a block are written
+// together, 16 bytes for each dimension, by the workgroup that their first row is
+// in (so the fifteen rows after its own are staged too); the others byte by byte.
+template <int D, int ROWS>
+struct VCodes {
+  static constexpr int kAround = kBlock - 1;  // rows before and after that a whole block can reach
+  static constexpr int kRows = ROWS + kAround;
+  static constexpr int kStride = D + 4;  // codes and the scale
+  uint8_t tile[kRows * kStride];
+  int64_t place[kRows + kAround];  // slot of row first - kAround + i, counted through the pool; -2: none
+  bool whole[kRows];               // whether row first - kAround + i is the first of a whole block
+  int32_t runs[ROWS];              // own rows that are
+  int32_t n_runs;
+};
+
+template <bool STREAM, typename T, int D, bool PAIRS, int ROWS>
+__device__ __forceinline__ void append_v_e4m3(const RotaryParams& p, const Place<T, D, PAIRS>& pl, int64_t item,
+                                              VCodes<D, ROWS>& m) {
+  using M = VCodes<D, ROWS>;
+  constexpr int kRows = M::kRows, kStride = M::kStride, kAround = M::kAround;
+  constexpr int E = kUnit<T>, kTurns = (kRows + kGroups - 1) / kGroups;
+  static_assert(ROWS == 64 && kRows + kAround <= kThreads, "whole blocks among the own rows are listed by one wavefront");
+  const int64_t tiles = ((int64_t)p.n + ROWS - 1) / ROWS;
+  const int h = (int)(item / tiles);
+  const int64_t first = (item - h * tiles) * ROWS;
+  const int tid = threadIdx.x, group = tid / kLanes;
+  if (tid < kRows + kAround) {
+    const int64_t row = first - kAround + tid;
+    int32_t blk, slot;
+    const bool ok = row >= 0 && row < p.n && slot_of(p, row, blk, slot);
+    m.place[tid] = ok ? (int64_t)blk * kBlock + slot : -2;
+  }
+#pragma unroll
+  for (int i = 0; i < kTurns; ++i) {
+    const int r = i * kGroups + group;
+    if (r >= kRows || first + r >= p.n) continue;  // (a group's lanes together)
+    Raw<T, D> raw;
+    raw.template load<STREAM>(head_row<T>(p.v, first + r, h), pl.at);
+    float x[kElems<D>];
+    raw.get(x);
+    uint32_t codes[kElems<D> / 4];
+    const uint32_t scale = quantize_row(x, codes, 0);
+    if (tid % kLanes == 0) m.tile[r * kStride + D] = (uint8_t)scale;
+#pragma unroll
+    for (int u = 0; u < kUnits<T, D>; ++u)
+#pragma unroll
+      for (int e = 0; e < E; e += 4)
+        *reinterpret_cast<uint32_t*>(&m.tile[r * kStride + pl.at[u] + e]) = codes[(u * E + e) / 4];
+  }
+  __syncthreads();
+  if (tid < kRows) {  // the own rows, then those before
+    const int i = tid < ROWS ? kAround + tid : tid - ROWS;
+    const int64_t s = m.place[i];
+    bool whole = s >= 0 && s % kBlock == 0;
+#pragma unroll
+    for (int j = 1; j < kBlock; ++j) whole = whole && m.place[i + j] == s + j;
+    m.whole[i] = whole;
+    if (tid < ROWS) {
+      const uint64_t all = __ballot(whole);
+      if (whole) m.runs[__popcll(all & ((1ull << tid) - 1))] = tid;
+      if (tid == 0) m.n_runs = __popcll(all);
+    }
+  }
+  __syncthreads();
+  const int lane = tid % 64, n = m.n_runs;
+  for (int step = tid / 64; step < n * (D / 64); step += kThreads / 64) {
+    const int c = step % (D / 64) * 64 + lane;
+    const int r = m.runs[step / (D / 64)];
+    const int64_t s = m.place[r + kAround];
+    const uint8_t* src = m.tile + r * kStride + c;
+    u32x4 y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      y[i] = (uint32_t)src[4 * i * kStride] | (uint32_t)src[(4 * i + 1) * kStride] << 8 |
+             (uint32_t)src[(4 * i + 2) * kStride] << 16 | (uint32_t)src[(4 * i + 3) * kStride] << 24;
+    *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(p.v_cache) + e4m3::codes_at<D>(s / kBlock, h, p.Hkv) + c * kBlock) = y;
+  }
+#pragma unroll
+  for (int i = 0; i < ROWS / kGroups; ++i) {
+    const int r = i * kGroups + group;
+    const int64_t s = m.place[r + kAround];
+    if (s < 0) continue;
+    const int slot = (int)(s % kBlock), lead = r + kAround - slot;
+    if (!(m.whole[lead] && m.place[lead] == s - slot)) {
+      uint32_t codes[kElems<D> / 4];
+#pragma unroll
+      for (int u = 0; u < kUnits<T, D>; ++u)
+#pragma unroll
+        for (int e = 0; e < E; e += 4)
+          codes[(u * E + e) / 4] = *reinterpret_cast<const uint32_t*>(&m.tile[r * kStride + pl.at[u] + e]);
+      store_bytes<T, D>(static_cast<uint8_t*>(p.v_cache) + e4m3::codes_at<D>(s / kBlock, h, p.Hkv) + slot, pl, codes);
+    }
+    if (tid % kLanes == 0) p.scales[e4m3::scales_at(s / kBlock, h, p.Hkv) + kBlock + slot] = m.tile[r * kStride + D];
+  }
+  __syncthreads();
+}
+
+// Append into an 8-bit cache: items of four roles, as above.  ROWS == 0: v's
+// tiles are cut like k's, a group takes a row of one head, and its lanes leave a
+// byte per dimension (d-major V).  Bound by memory: 20,456 rows of 16 + 2 + 2 heads
+// of 128 in bf16, in 8 runs, take 41.5 us (4.81 TB/s; a copy reaches 5.1 to 5.3),
+// with V byte by byte 52.9, with three wavefronts a SIMD instead of four 43.5.
+template <typename T, int D, bool PAIRS, int ROWS, bool STREAM>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) void rotary_append_e4m3_kernel(const RotaryParams p) {
+  __shared__ union Shared {
+    AngleTable<T, D, PAIRS> table;
+    VCodes<D, 64> v;
+    __device__ Shared() {}
+  } shared;
   constexpr int E = kUnit<T>;
   const Place<T, D, PAIRS> pl(p.pairs);
-  const int64_t n_q = p.tiles_q.items, n_turned = n_q + p.tiles_k.items;
   for (int64_t b = blockIdx.x; b < p.items; b += gridDim.x) {
-    if (b >= n_turned + p.items_v) {
-      const int64_t e = (b - n_turned - p.items_v) * kThreads + threadIdx.x;
-      if (e < p.n_patch) p.block_table[p.patch[2 * e]] = p.patch[2 * e + 1];
-      continue;
-    }
-    if (b >= n_turned) {
-      Tile t = tile_of(p, b - n_turned + n_q);  // (k's tile of the same rows and heads)
-      t.in = p.v;
-      const int dr = kGroups / t.heads, dh = kGroups - dr * t.heads;
-      for (Cursor c(t, threadIdx.x / kLanes); c.row < t.rows; c.next(t, dr, dh)) {
-        Raw<T, D> raw;
-        raw.template load<STREAM>(c.at<const T>(t.in, t), pl.at);
-        float x[kElems<D>];
-        raw.get(x);
-        uint32_t codes[kElems<D> / 4];
-        const uint32_t scale = quantize_row(x, codes, 0);
-        int32_t blk, slot;
-        if (!slot_of(p, t.row0 + c.row, blk, slot)) continue;
-        const int h = t.h0 + c.h;
-        uint8_t* dst = static_cast<uint8_t*>(p.v_cache) + e4m3::codes_at<D>(blk, h, p.Hkv) + slot;
-#pragma unroll
-        for (int i = 0; i < kElems<D>; ++i) dst[(pl.at[i / E] + i % E) * kBlock] = (uint8_t)(codes[i / 4] >> (8 * (i % 4)));
-        if (threadIdx.x % kLanes == 0) p.scales[e4m3::scales_at(blk, h, p.Hkv) + kBlock + slot] = (uint8_t)scale;
+    if (b < p.items_v) {
+      if constexpr (ROWS > 0) {
+        append_v_e4m3<STREAM>(p, pl, b, shared.v);
+      } else {
+        Tile t = tile_of(p, b + p.tiles_q.items);  // (k's tile of the same rows and heads)
+        t.in = p.v;
+        const int dr = kGroups / t.heads, dh = kGroups - dr * t.heads;
+        for (Cursor c(t, threadIdx.x / kLanes); c.row < t.rows; c.next(t, dr, dh)) {
+          Raw<T, D> raw;
+          raw.template load<STREAM>(c.at<const T>(t.in, t), pl.at);
+          float x[kElems<D>];
+          raw.get(x);
+          uint32_t codes[kElems<D> / 4];
+          const uint32_t scale = quantize_row(x, codes, 0);
+          int32_t blk, slot;
+          if (!slot_of(p, t.row0 + c.row, blk, slot)) continue;
+          const int h = t.h0 + c.h;
+          uint8_t* dst = static_cast<uint8_t*>(p.v_cache) + e4m3::codes_at<D>(blk, h, p.Hkv) + slot;
+          store_bytes<T, D>(dst, pl, codes);
+          if (threadIdx.x % kLanes == 0) p.scales[e4m3::scales_at(blk, h, p.Hkv) + kBlock + slot] = (uint8_t)scale;
+        }
       }
       continue;
     }
-    const Tile t = tile_of(p, b);
-    const bool is_q = b < n_q;
-    turn_tile<STREAM>(p, t, is_q ? p.q_pos : p.pos, is_q ? p.q_pos_stride : p.pos_stride, table, pl,
+    const int64_t i = b - p.items_v, n_q = p.tiles_q.items, n_turned = n_q + p.tiles_k.items;
+    if (i >= n_turned) {
+      const int64_t e = (i - n_turned) * kThreads + threadIdx.x;
+      if (e < p.n_patch) p.block_table[p.patch[2 * e]] = p.patch[2 * e + 1];
+      continue;
+    }
+    const Tile t = tile_of(p, i);
+    const bool is_q = i < n_q;
+    turn_tile<STREAM>(p, t, is_q ? p.q_pos : p.pos, is_q ? p.q_pos_stride : p.pos_stride, shared.table, pl,
               [&](const Cursor& c, const float (&x)[kElems<D>]) {
       if (is_q) {
         store_row(c.at<T>(t.out, t), pl.at, x);
@@ -691,9 +806,7 @@ __global__ __launch_bounds__(kThreads) void rotary_append_e4m3_kernel(const Rota
       uint8_t* dst = static_cast<uint8_t*>(p.k_cache) + e4m3::codes_at<D>(blk, h, p.Hkv);
 #pragma unroll
       for (int u = 0; u < kUnits<T, D>; ++u)
-#pragma unroll
-        for (int i = 0; i < E; i += 4)
-          *reinterpret_cast<uint32_t*>(dst + e4m3::k_at(slot, pl.at[u] + i)) = codes[(u * E + i) / 4];
+        __builtin_memcpy(__builtin_assume_aligned(dst + e4m3::k_at(slot, pl.at[u]), E), &codes[u * E / 4], E);
       if (threadIdx.x % kLanes == 0) p.scales[e4m3::scales_at(blk, h, p.Hkv) + slot] = (uint8_t)scale;
     });
   }
@@ -761,12 +874,12 @@ struct Append {
   };
 };
 
-template <bool STREAM>
+template <int ROWS, bool STREAM>
 struct AppendE4m3 {
   template <typename T, int D, bool PAIRS>
   struct Call {
     static void go(const RotaryParams& p, dim3 grid, hipStream_t s) {
-      hipLaunchKernelGGL((rotary_append_e4m3_kernel<T, D, PAIRS, STREAM>), grid, dim3(kThreads), 0, s, p);
+      hipLaunchKernelGGL((rotary_append_e4m3_kernel<T, D, PAIRS, ROWS, STREAM>), grid, dim3(kThreads), 0, s, p);
     }
   };
 };
@@ -849,15 +962,26 @@ hipError_t launch_rotary_append(RotaryParams p, int D, bool bf16, bool pairs, hi
              : dispatch<Append<64, false>::Call>(p, D, bf16, pairs, grid, s);
 }
 
+// Rows (of all heads) from which V's go in tiles of 64 rows.  As above, the
+// count decides.  Measured without queries, us a call byte by byte and in tiles, in
+// runs and scattered: 2 heads of 128 in bf16, 2,400 rows 6.7 and 6.2, 9.4 and 11.2;
+// 3,200 rows 6.7 and 6.1, 10.6 and 12.6; 6,400 rows 9.1 and 6.3, 15.4 and 16.7; 8 heads,
+// 400 rows 6.2 and 6.2, 6.9 and 10.2; 800 rows 9.6 and 6.1, 10.3 and 12.2; 4 heads of
+// 64 in fp32, 1,600 rows 5.1 and 5.1, 7.0 and 8.0.
+constexpr int64_t kTallE4m3 = 6144;
+
 hipError_t launch_rotary_append_e4m3(RotaryParams p, int D, bool bf16, bool pairs, hipStream_t s) {
   p.tiles_q = tile_grid(p.n_q, p.Hq, p.Hq + p.Hkv, 4, 4 * kComputeUnits);
   p.tiles_k = tile_grid(p.n, p.Hkv, p.Hq + p.Hkv, 4, 4 * kComputeUnits);
-  p.items_v = p.tiles_k.items;
+  const bool tall = (int64_t)p.n * p.Hkv >= kTallE4m3;
+  p.items_v = tall ? ceil_div(p.n, 64) * p.Hkv : p.tiles_k.items;
   p.items = p.items_v + p.tiles_q.items + p.tiles_k.items + ceil_div(p.n_patch, kThreads);
   if (p.items == 0) return hipSuccess;
+  const dim3 grid = grid_of(p.items);
+  if (!tall) return dispatch<AppendE4m3<0, false>::Call>(p, D, bf16, pairs, grid, s);
   return streams((int64_t)p.n_q * p.Hq * 2 + (int64_t)p.n * p.Hkv * 3, D, bf16)
-             ? dispatch<AppendE4m3<true>::Call>(p, D, bf16, pairs, grid_of(p.items), s)
-             : dispatch<AppendE4m3<false>::Call>(p, D, bf16, pairs, grid_of(p.items), s);
+             ? dispatch<AppendE4m3<64, true>::Call>(p, D, bf16, pairs, grid, s)
+             : dispatch<AppendE4m3<64, false>::Call>(p, D, bf16, pairs, grid, s);
 }
 
 }  // namespace padoc

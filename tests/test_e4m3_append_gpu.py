@@ -85,6 +85,36 @@ def test_rows(dtype, d, rd, style, axes, norm, n, hq, hkv, together):
     check_rows(st, before, on_host(gpu), slots, k, v, pos, wk)
 
 
+@pytest.mark.parametrize("dtype,d,hkv,n", [("bf16", 128, 2, 3331), ("f32", 128, 3, 2101), ("bf16", 64, 7, 901), ("f32", 64, 1, 6200)])
+def test_rows_of_many_runs(dtype, d, hkv, n):
+    """A prefill's rows: runs of every length from 1 to 49 and every first slot, whole blocks among them, rows left out and
+    single rows in between, runs that go on in the block that the next run is in."""
+    rng = np.random.default_rng([n, 6])
+    slots, blocks, free = np.zeros((n, 2), np.int32), n // 4, list(rng.permutation(n // 4))
+    i = r = 0
+    while i < n:
+        at, blk = r % 16, free.pop()
+        for _ in range(min(n - i, 1 + r * 7 % 49)):
+            if at == 16:
+                at, blk = 0, free.pop()
+            slots[i] = blk, at
+            at += 1
+            i += 1
+        r += 1
+    gone = rng.choice(n, n // 40, replace=False)
+    slots[gone[::2], 0], slots[gone[1::2], 1] = -1, 16
+    st = Setup(d, dtype, base=1e5)
+    qkv = normal((n, 1 + 2 * hkv, d), n, dtype, spread=3.0)
+    q, k, v = qkv[:, :1], qkv[:, 1:1 + hkv], qkv[:, 1 + hkv:]
+    pos, wk = positions(3, n, 4), normal((d,), 3, dtype)
+    before = orc.empty(blocks, hkv, d, n)
+    gpu = on_gpu(before)
+    print("[case] append e4m3 runs", dtype, d, hkv, n, flush=True)
+    out = pa.rotary_append(q, k, v, pos, torch.from_numpy(slots).cuda(), *gpu[:2], st.handle, None, wk, scales=gpu[2])
+    check("q", out, *st.forward(q, pos))
+    check_rows(st, before, on_host(gpu), slots, k, v, pos, wk)
+
+
 def test_rows_of_every_kind():
     """Zeros, the largest and the smallest numbers, infinities and NaN: V bit for bit, K's NaN rows NaN; without
     queries, without a rotation that mixes them (position 0)."""
