@@ -27,19 +27,23 @@ constexpr int kSets = 2;   // steps in flight
 __device__ __forceinline__ u32x4 load16_nt(const uint8_t* p) {
   return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
 }
-__device__ __forceinline__ u32x2 load8(const uint8_t* p) { return *reinterpret_cast<const u32x2*>(p); }
+__device__ __forceinline__ u32x2 load_pair(const uint8_t* p) {  // four bytes, and four eight bytes on
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(p);
+  return u32x2{w[0], w[2]};
+}
 
 // Private work item `item` (at most 16 columns) on one wavefront, whose lane
 // index is `lane`: keys in steps of 32, from HBM straight into
 // v_mfma_f32_16x16x32_bf16 operands (lane l: row / column n = l%16, group
 // g = l/16 with eight consecutive elements of the contraction).
-//   S^T = K Q^T    two 16-key M blocks; row m of block T holds token 8 (m/4 % 2)
-//                  + 4T + m%4 of cache block m/8, so that a lane's eight scores
-//                  are tokens 8 (g%2) .. +7 of cache block g/2, in order; a
-//                  lane's 16 codes (a 16-dim piece of a token) are two operands
+//   S^T = K Q^T    two 16-key M blocks; row m of block T holds token 8T + m%8 of
+//                  cache block m/8 (eight tokens of a 16-dim piece are a line of
+//                  128 bytes, whole in one load), so that a lane's scores are
+//                  tokens 8T + 4 (g%2) .. +3 of cache block g/2; a lane's 16 codes
+//                  (a piece of a token) are two operands
 //   O^T += V^T P^T a lane loads the 16 tokens of a V row: of row block 2e where g
 //                  is even, of 2e + 1 where it is odd.  Two lane swaps exchange
-//                  the halves, so that it has tokens 8 (g%2) .. +7 of both rows.
+//                  words, so that it has its scores' tokens of both rows.
 // Two register sets hold the codes of two steps, refilled after their last use.
 // Fewer bytes in flight are better here: a read of 420 MB in random 2 KB pieces
 // took 62 us (6.5 TB/s) with 8 KB sets and 68 with 16 KB sets, two a wavefront,
@@ -121,18 +125,18 @@ __device__ __forceinline__ void wave_item(const TileParams& p, int item, int lan
   auto load_k = [&](int X, bool real) __attribute__((always_inline)) {
     const int64_t blk = real ? (n >= 8 ? id1 : id0) : 0;
     vblk[X] = real ? (g >= 2 ? id1 : id0) : 0;
-    const uint8_t* kp = Kc + e4m3::codes_at<D>(blk, kvh, Hkv) + g * (kBlock * 16) + (8 * ((n >> 2) & 1) + (n & 3)) * 16;
+    const uint8_t* kp = Kc + e4m3::codes_at<D>(blk, kvh, Hkv) + g * (kBlock * 16) + (n & 7) * 16;
 #pragma unroll
     for (int T = 0; T < 2; ++T)
 #pragma unroll
-      for (int j = 0; j < NP; ++j) kf[X][T][j] = load16_nt(kp + 4 * T * 16 + 4 * j * (kBlock * 16));
-    ks[X] = load8(p.scales + e4m3::scales_at(blk, kvh, Hkv) + 8 * ((n >> 2) & 1));
+      for (int j = 0; j < NP; ++j) kf[X][T][j] = load16_nt(kp + 8 * T * 16 + 4 * j * (kBlock * 16));
+    ks[X] = load_pair(p.scales + e4m3::scales_at(blk, kvh, Hkv) + 4 * ((n >> 2) & 1));
   };
   auto load_v = [&](int X) __attribute__((always_inline)) {
     const uint8_t* vp = Vc + e4m3::codes_at<D>(vblk[X], kvh, Hkv) + (16 * (g & 1) + n) * kBlock;
 #pragma unroll
     for (int e = 0; e < NDM / 2; ++e) vf[X][e] = load16_nt(vp + e * 32 * kBlock);
-    vs[X] = load8(p.scales + e4m3::scales_at(vblk[X], kvh, Hkv) + kBlock + 8 * (g & 1));
+    vs[X] = load_pair(p.scales + e4m3::scales_at(vblk[X], kvh, Hkv) + kBlock + 4 * (g & 1));
   };
 
   float m_run = -INFINITY, l_part = 0.f;
@@ -174,7 +178,7 @@ __device__ __forceinline__ void wave_item(const TileParams& p, int item, int lan
 
   auto step = [&](auto xc) __attribute__((always_inline)) {
     constexpr int X = decltype(xc)::value;
-    const int kb = C.st * kStep;
+    const int kb = C.st * kStep, first = kb + 16 * (g >> 1) + 4 * (g & 1);  // (of the lane's tokens)
     f32x4_t S[2];
 #pragma unroll
     for (int T = 0; T < 2; ++T) {
@@ -204,7 +208,7 @@ __device__ __forceinline__ void wave_item(const TileParams& p, int item, int lan
     if (kb + kStep > C.R.min_lim) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (kb + 8 * g + e >= lim) S[e / 4][e % 4] = -INFINITY;
+        if (first + 8 * (e / 4) + e % 4 >= lim) S[e / 4][e % 4] = -INFINITY;
     }
     float mx = fmaxf(fmaxf(fmaxf(S[0][0], S[0][1]), fmaxf(S[0][2], S[0][3])),
                      fmaxf(fmaxf(S[1][0], S[1][1]), fmaxf(S[1][2], S[1][3])));
@@ -227,16 +231,16 @@ __device__ __forceinline__ void wave_item(const TileParams& p, int item, int lan
     for (int e = 0; e < NDM / 2; ++e)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const auto r = __builtin_amdgcn_permlane16_swap(vf[X][e][i], vf[X][e][2 + i], false, false);
+        const auto r = __builtin_amdgcn_permlane16_swap(vf[X][e][2 * i], vf[X][e][2 * i + 1], false, false);
         v[2 * e][i] = r[0];
         v[2 * e + 1][i] = r[1];
       }
     if (kb + kStep > C.R.n_keys) {  // tokens past the range's end: their P is 0, but slots may hold anything
-      const int keep = C.R.n_keys - (kb + 8 * g);
+      const int keep = C.R.n_keys - first;
       uint32_t m[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int k = keep - 4 * i;
+        const int k = keep - 8 * i;
         m[i] = k >= 4 ? 0xffffffffu : k <= 0 ? 0u : 0xffffffffu >> (8 * (4 - k));
       }
 #pragma unroll
