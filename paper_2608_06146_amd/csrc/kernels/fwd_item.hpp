@@ -48,8 +48,9 @@
 // K, still in its stage, and the accumulator is rescaled.  That is exactly
 // the set of tiles whose maximum passes the reference by more than the
 // slack, so the result equals that of a per-tile maximum.  The row sum adds
-// the bf16-rounded probabilities the PV product uses; O is rounded to bf16
-// (RNE) at the end.
+// the bf16-rounded probabilities the PV product uses (E4M3: the unrounded ones,
+// which the private items of the same step add, so that LSE is as close as fp32
+// sums are); O is rounded to bf16 (RNE) at the end.
 //
 // Loads and waits.  Step t reads K(t+1), V(t) and the limits of tile t+1,
 // loaded at step t-2, and (on the slow path) K(t) and the limits of tile t;
@@ -546,10 +547,15 @@ __device__ __forceinline__ void fwd_item(const TileParams& p, int item) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = xs[8 * g + e];
       P[g >> 1][g & 1] = __builtin_convertvector(x, bf16x8_t);
+      if constexpr (E4M3) {
+        ls0 += (x[0] + x[1]) + (x[2] + x[3]);
+        ls1 += (x[4] + x[5]) + (x[6] + x[7]);
+      } else {
 #pragma unroll
-      for (int e = 0; e < 8; e += 4) {
-        ls0 = add_bf16x2(bf16x2_t{P[g >> 1][g & 1][e], P[g >> 1][g & 1][e + 1]}, ls0);
-        ls1 = add_bf16x2(bf16x2_t{P[g >> 1][g & 1][e + 2], P[g >> 1][g & 1][e + 3]}, ls1);
+        for (int e = 0; e < 8; e += 4) {
+          ls0 = add_bf16x2(bf16x2_t{P[g >> 1][g & 1][e], P[g >> 1][g & 1][e + 1]}, ls0);
+          ls1 = add_bf16x2(bf16x2_t{P[g >> 1][g & 1][e + 2], P[g >> 1][g & 1][e + 3]}, ls1);
+        }
       }
     }
   };

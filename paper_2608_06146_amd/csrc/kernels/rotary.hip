@@ -258,6 +258,17 @@ __device__ __forceinline__ float rms_scale(const float (&x)[kElems<D>], float ep
   for (int i = 0; i < kElems<D>; ++i) s += x[i] * x[i];
   return __builtin_amdgcn_rsqf(group_sum(s) * (1.f / D) + eps);
 }
+// With a Newton step: v_rsq_f32 is off by up to a unit in the last place, and in
+// bf16 that does not show, but a row's codes are compared one by one.  (Its error
+// is NaN where the mean is 0 or infinite, and the root is exact.)
+template <int D>
+__device__ __forceinline__ float rms_scale_exact(const float (&x)[kElems<D>], float eps) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < kElems<D>; ++i) s += x[i] * x[i];
+  const float v = group_sum(s) * (1.f / D) + eps, r = __builtin_amdgcn_rsqf(v), e = fmaf(-v * r, r, 1.f);
+  return e == e ? fmaf(0.5f * r, e, r) : r;
+}
 
 template <typename T>
 __device__ __forceinline__ const T* head_row(const padoc_heads& x, int64_t row, int h) {
@@ -318,7 +329,7 @@ struct Cursor {
 // Rows of a tile: norm, rotation, and `put(row, head, values)`.  The first
 // rows are asked for before the angles are computed, the others kAhead turns
 // before theirs.
-template <bool STREAM, typename T, int D, bool PAIRS, class Put>
+template <bool STREAM, bool EXACT = false, typename T, int D, bool PAIRS, class Put>
 __device__ __forceinline__ void turn_tile(const RotaryParams& p, const Tile& t, const int32_t* pos, int64_t pos_stride,
                                           AngleTable<T, D, PAIRS>& table, const Place<T, D, PAIRS>& pl, Put put) {
   constexpr int U = kAhead;
@@ -344,7 +355,7 @@ __device__ __forceinline__ void turn_tile(const RotaryParams& p, const Tile& t, 
       if (ahead.row < t.rows) raw[u].template load<STREAM>(ahead.at<const T>(t.in, t), pl.at);
       ahead.next(t, dr, dh);
       if (t.w) {
-        const float rho = rms_scale<D>(x, p.eps);
+        const float rho = EXACT ? rms_scale_exact<D>(x, p.eps) : rms_scale<D>(x, p.eps);
 #pragma unroll
         for (int i = 0; i < kElems<D>; ++i) x[i] *= rho * wt[i];
       }
@@ -792,7 +803,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) void rotary_appen
     }
     const Tile t = tile_of(p, i);
     const bool is_q = i < n_q;
-    turn_tile<STREAM>(p, t, is_q ? p.q_pos : p.pos, is_q ? p.q_pos_stride : p.pos_stride, shared.table, pl,
+    turn_tile<STREAM, true>(p, t, is_q ? p.q_pos : p.pos, is_q ? p.q_pos_stride : p.pos_stride, shared.table, pl,
               [&](const Cursor& c, const float (&x)[kElems<D>]) {
       if (is_q) {
         store_row(c.at<T>(t.out, t), pl.at, x);
