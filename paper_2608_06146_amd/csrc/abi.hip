@@ -14,7 +14,7 @@ namespace padoc {
 hipError_t launch_tile_mfma_bf16(const TileParams& p, int n_work, int D, hipStream_t s);
 hipError_t launch_decode_step_bf16(const TileParams& p, int n_shared, int n_private, int n_groups, int* next, int D,
                                    hipStream_t s);
-hipError_t launch_tile_f32(const TileParams& p, int n_full, int n_items, int D, bool paged, hipStream_t s);
+hipError_t launch_tile_f32(const TileParamsE4m3& p, int n_full, int n_items, int D, bool paged, hipStream_t s);
 hipError_t launch_lse_combine(const CombineParams& p, int D, bool bf16, hipStream_t s);
 hipError_t launch_tree_attn_bwd(const BwdParams& p, int n_work, int n_bwd, int D, hipStream_t s);
 hipError_t launch_relayout_kv(const void* k_rows, const void* v_rows, void* k_cache, void* v_cache, int64_t n_blocks,
@@ -30,7 +30,7 @@ hipError_t launch_rotary_append(RotaryParams p, int D, bool bf16, bool pairs, hi
 hipError_t launch_copy_blocks(const CopyParams& p, hipStream_t s);
 hipError_t launch_rotary_append_e4m3(RotaryParams p, int D, bool bf16, bool pairs, hipStream_t s);
 hipError_t launch_cast_blocks(const CastParams& p, int D, bool bf16, bool back, hipStream_t s);
-hipError_t launch_decode_e4m3(const TileParams& p, int n_shared, int n_private, int n_groups, int* next, int D,
+hipError_t launch_decode_e4m3(const TileParamsE4m3& p, int n_shared, int n_private, int n_groups, int* next, int D,
                               hipStream_t s);
 
 namespace {
@@ -182,7 +182,7 @@ padoc_status run(const padoc_plan* P, const void* q, const void* k, const void* 
     padoc_status st = upload_schedule(P, ws, stream, pinned);
     if (st != PADOC_OK) return st;
   }
-  TileParams tp{};
+  TileParamsE4m3 tp{};
   tp.q = q;
   tp.k = k;
   tp.v = v;
@@ -209,12 +209,14 @@ padoc_status run(const padoc_plan* P, const void* q, const void* k, const void* 
     if (e != hipSuccess) return hip_fail("hipEventRecord", e);
   }
   if (bf16) {
-    if (!paged)
+    if (!paged) {
       e = launch_tile_mfma_bf16(tp, n_work, P->D, stream);
-    else  // shared-key tile items and private-key items in one launch
-      e = (scales ? launch_decode_e4m3 : launch_decode_step_bf16)(
-          tp, P->n_work_shared, n_work - P->n_work_shared, P->n_private_groups,
-          reinterpret_cast<int*>(static_cast<char*>(ws) + P->off_next), P->D, stream);
+    } else {  // shared-key tile items and private-key items in one launch
+      const int n_private = n_work - P->n_work_shared;
+      int* next = reinterpret_cast<int*>(static_cast<char*>(ws) + P->off_next);
+      e = scales ? launch_decode_e4m3(tp, P->n_work_shared, n_private, P->n_private_groups, next, P->D, stream)
+                 : launch_decode_step_bf16(tp, P->n_work_shared, n_private, P->n_private_groups, next, P->D, stream);
+    }
   } else {
     e = launch_tile_f32(tp, paged ? P->n_work_shared : n_work, n_work, P->D, paged, stream);
   }

@@ -49,7 +49,7 @@ __device__ __forceinline__ u32x2 load_pair(const uint8_t* p) {  // four bytes, a
 // took 62 us (6.5 TB/s) with 8 KB sets and 68 with 16 KB sets, two a wavefront,
 // eight wavefronts a unit.
 template <int D>
-__device__ __forceinline__ void wave_item(const TileParams& p, int item, int lane) {
+__device__ __forceinline__ void wave_item(const TileParamsE4m3& p, int item, int lane) {
   constexpr int NP = D / 64;   // 16-dim pieces per lane and token
   constexpr int NDM = D / 16;  // 16-row blocks of O^T
   const WorkRec w = load_scalar(p.work + item);
@@ -295,8 +295,8 @@ __device__ __forceinline__ int take_private(int* ctr, int lane) {
 }
 
 template <int D>
-__global__ __launch_bounds__(tile::kThreads) void decode_e4m3_kernel(TileParams p, int n_shared, int n_private,
-                                                                     int n_groups, int* next) {
+__global__ __launch_bounds__(tile::kThreads) void decode_e4m3_kernel(TileParamsE4m3 p, int n_shared,
+                                                                     int n_private, int n_groups, int* next) {
   const int b = blockIdx.x;
   if (b < n_shared) tile::fwd_item<D, true, true>(p, b);
   if (n_private <= 0) return;
@@ -317,7 +317,7 @@ __global__ __launch_bounds__(tile::kThreads) void decode_e4m3_kernel(TileParams 
 }  // namespace
 
 // n_groups, next: as launch_decode_step_bf16.
-hipError_t launch_decode_e4m3(const TileParams& p, int n_shared, int n_private, int n_groups, int* next, int D,
+hipError_t launch_decode_e4m3(const TileParamsE4m3& p, int n_shared, int n_private, int n_groups, int* next, int D,
                               hipStream_t stream) {
   const int n_blocks = n_shared + n_groups;
   if (n_blocks <= 0) return hipSuccess;

@@ -148,7 +148,7 @@ __device__ __forceinline__ void dma4_v(const void* a, uint32_t lds) {
 #pragma clang diagnostic pop
 
 template <int D, bool PAGED, bool E4M3 = false>
-__device__ __forceinline__ void fwd_item(const TileParams& p, int item) {
+__device__ __forceinline__ void fwd_item(const TileArgs<E4M3>& p, int item) {
   static_assert(PAGED || !E4M3, "8-bit caches are paged");
   using Gm = FwdGeom<D>;
   constexpr int KT = Gm::KT, CPR = Gm::CPR, RPI = Gm::RPI, IPW = Gm::IPW, SEL = Gm::SEL;

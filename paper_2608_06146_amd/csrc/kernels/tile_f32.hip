@@ -63,8 +63,9 @@ constexpr int kGroups = kTileCols / kCols;  // column groups of a full item
 
 __device__ __forceinline__ f32x4_t load_f4(const float* p) { return *reinterpret_cast<const f32x4_t*>(p); }
 
-template <int D, bool PAGED, bool E4M3 = false>
-__global__ __launch_bounds__(64 * waves(PAGED)) void tile_f32_kernel(TileParams p, int n_full, int n_items) {
+template <int D, bool PAGED, class P>
+__global__ __launch_bounds__(64 * waves(PAGED)) void tile_f32_kernel(P p, int n_full, int n_items) {
+  constexpr bool E4M3 = std::is_same_v<P, TileParamsE4m3>;
   static_assert(PAGED || !E4M3, "8-bit caches are paged");
   constexpr int kWaves = waves(PAGED);
   constexpr int NJ = D / 16;  // float4 loads of a K or V block per lane
@@ -380,25 +381,26 @@ __global__ __launch_bounds__(64 * waves(PAGED)) void tile_f32_kernel(TileParams 
 // n_full: the first items of the schedule, of up to kTileCols columns each
 // (every packed item; the shared items of a decode step); the others are
 // private decode items of one column group.  p.scales: null, or 8-bit caches.
-hipError_t launch_tile_f32(const TileParams& p, int n_full, int n_items, int D, bool paged, hipStream_t stream) {
+hipError_t launch_tile_f32(const TileParamsE4m3& p, int n_full, int n_items, int D, bool paged, hipStream_t stream) {
   static_assert(kCols == kPrivateCols, "a private item is one column group");
   if (n_items <= 0) return hipSuccess;
   const dim3 grid((unsigned)((n_full + 7) / 8 * 8 * kGroups + (n_items - n_full))), block(64 * waves(paged));
+  const TileParams& plain = p;
   if (paged && p.scales) {
     if (D == 64)
-      hipLaunchKernelGGL((tile_f32_kernel<64, true, true>), grid, block, 0, stream, p, n_full, n_items);
+      hipLaunchKernelGGL((tile_f32_kernel<64, true, TileParamsE4m3>), grid, block, 0, stream, p, n_full, n_items);
     else
-      hipLaunchKernelGGL((tile_f32_kernel<128, true, true>), grid, block, 0, stream, p, n_full, n_items);
+      hipLaunchKernelGGL((tile_f32_kernel<128, true, TileParamsE4m3>), grid, block, 0, stream, p, n_full, n_items);
   } else if (paged) {
     if (D == 64)
-      hipLaunchKernelGGL((tile_f32_kernel<64, true>), grid, block, 0, stream, p, n_full, n_items);
+      hipLaunchKernelGGL((tile_f32_kernel<64, true, TileParams>), grid, block, 0, stream, plain, n_full, n_items);
     else
-      hipLaunchKernelGGL((tile_f32_kernel<128, true>), grid, block, 0, stream, p, n_full, n_items);
+      hipLaunchKernelGGL((tile_f32_kernel<128, true, TileParams>), grid, block, 0, stream, plain, n_full, n_items);
   } else {
     if (D == 64)
-      hipLaunchKernelGGL((tile_f32_kernel<64, false>), grid, block, 0, stream, p, n_full, n_items);
+      hipLaunchKernelGGL((tile_f32_kernel<64, false, TileParams>), grid, block, 0, stream, plain, n_full, n_items);
     else
-      hipLaunchKernelGGL((tile_f32_kernel<128, false>), grid, block, 0, stream, p, n_full, n_items);
+      hipLaunchKernelGGL((tile_f32_kernel<128, false, TileParams>), grid, block, 0, stream, plain, n_full, n_items);
   }
   return hipGetLastError();
 }

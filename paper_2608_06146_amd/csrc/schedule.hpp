@@ -7,6 +7,8 @@
 
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "padoc_attn.h"  // include/ is on the include path
 
 namespace padoc {
@@ -58,8 +60,14 @@ struct TileParams {
   float* part_ml;         // partial mode: [slots, 2] (running max in log2 units, sum)
   int32_t Hq, Hkv, G;
   float scale_log2;       // softmax_scale * log2(e)
-  const uint8_t* scales;  // 8-bit caches: [blocks, Hkv, 2, 16] (k and v hold codes)
 };
+
+// Of a step over an 8-bit cache: k and v hold codes.
+struct TileParamsE4m3 : TileParams {
+  const uint8_t* scales;  // [blocks, Hkv, 2, 16]
+};
+template <bool E4M3>
+using TileArgs = std::conditional_t<E4M3, TileParamsE4m3, TileParams>;
 
 // 8-bit caches: whether a dtype names them, and the dtype of the rows around them.
 constexpr bool is_e4m3(padoc_dtype t) { return t == PADOC_BF16_E4M3 || t == PADOC_F32_E4M3; }
