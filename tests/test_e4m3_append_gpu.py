@@ -115,6 +115,28 @@ def test_rows_of_many_runs(dtype, d, hkv, n):
     check_rows(st, before, on_host(gpu), slots, k, v, pos, wk)
 
 
+@pytest.mark.parametrize("n", [40, 900])
+def test_blocks_behind_four_gigabytes(n):
+    """Rows into blocks of a pool whose codes pass 2^32 bytes, byte by byte and by whole blocks: as into a small pool."""
+    hkv, d = 8, 128
+    blocks = (1 << 32) // (hkv * d * 16) + 64
+    if torch.cuda.mem_get_info()[0] < 3 * blocks * hkv * d * 16:
+        pytest.skip("not enough memory")
+    st = Setup(d, "bf16")
+    k, v, pos = normal((n, hkv, d), 1, "bf16"), normal((n, hkv, d), 2, "bf16"), positions(3, n, 3)
+    near, far = pa.empty_cache_e4m3(64, hkv, d, "cuda"), pa.empty_cache_e4m3(blocks, hkv, d, "cuda")
+    for a, b in zip(near, far):
+        a.view(torch.uint8).zero_()
+        b.view(torch.uint8)[-64:] = 0
+    slots = torch.from_numpy(places(n, 64, 5, together=True)).cuda()
+    print("[case] append e4m3 far blocks", n, flush=True)
+    pa.rotary_append(None, k, v, pos, slots, *near[:2], st.handle, scales=near[2])
+    pa.rotary_append(None, k, v, pos, slots + torch.tensor([blocks - 64, 0], dtype=torch.int32, device="cuda"), *far[:2], st.handle,
+                     scales=far[2])
+    assert near[2].view(torch.uint8).count_nonzero() > 0
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)[-64:]) for a, b in zip(near, far))
+
+
 def test_rows_of_every_kind():
     """Zeros, the largest and the smallest numbers, infinities and NaN: V bit for bit, K's NaN rows NaN; without
     queries, without a rotation that mixes them (position 0)."""

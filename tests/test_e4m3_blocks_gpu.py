@@ -236,3 +236,56 @@ def test_native_calls_leave_what_they_cannot_check(binding):
                 (k, v, e[0][:1], e[1], e[2], None), (k, v, *[t[:1] for t in e], None),
                 (k, v, *e, torch.zeros(2, 2, device="cuda")), (k, v, *e, torch.zeros(2, 2, dtype=torch.int32))):
         assert cast(*bad) is None
+
+
+def test_captured_casts(binding):
+    """Values to codes and back in one graph, replayed on new values with eager calls between."""
+    k = torch.empty(5, 2, 16, 16, 8, device="cuda", dtype=torch.bfloat16)
+    v = torch.empty(5, 2, 128, 16, device="cuda", dtype=torch.bfloat16)
+    e, (k2, v2) = pa.empty_cache_e4m3(4, 2, 128, "cuda"), (torch.zeros_like(k), torch.zeros_like(v))
+    pairs = torch.tensor([[0, 3], [4, 1], [2, 0], [2, 2]], dtype=torch.int32, device="cuda")
+    back = pairs.flip(1)[:3].contiguous()  # (no destination twice)
+
+    def both():
+        pa.cache_quantize(k, v, *e, pairs=pairs)
+        pa.cache_dequantize(*e, k2, v2, pairs=back)
+
+    def draw(seed):
+        for t in (k, v):
+            t.copy_(torch.randn(t.shape, generator=torch.Generator().manual_seed(seed)))
+
+    draw(0)
+    both()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for seed in range(1, 4):
+        draw(seed)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.view(torch.uint8).clone() for t in (*e, k2, v2)]
+        both()
+        assert all(torch.equal(a, b.view(torch.uint8)) for a, b in zip(got, (*e, k2, v2)))
+        assert ((k2[[0, 2, 4]].float() - k[[0, 2, 4]].float()).abs() <= 2.0 ** -4 * k[[0, 2, 4]].float().abs() + 2.0 ** -6).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_blocks_behind_four_gigabytes(binding, dtype):
+    """Blocks of an 8-bit pool whose codes pass 2^32 bytes, written and read back."""
+    hkv, d = 8, 128
+    blocks = (1 << 32) // (hkv * d * 16) + 3
+    if torch.cuda.mem_get_info()[0] < 3 * blocks * hkv * d * 16:
+        pytest.skip("not enough memory")
+    k = torch.randn(2, hkv, d // 8, 16, 8, device="cuda").to(torch_dtype(dtype))
+    v = torch.randn(2, hkv, d, 16, device="cuda").to(torch_dtype(dtype))
+    far = pa.empty_cache_e4m3(blocks, hkv, d, "cuda")
+    pairs = torch.tensor([[0, blocks - 1], [1, blocks - 2]], dtype=torch.int32, device="cuda")
+    print("[case] far blocks", dtype, flush=True)
+    pa.cache_quantize(k, v, *far, pairs=pairs)
+    near = pa.cache_quantize(k, v)
+    assert all(torch.equal(a[[blocks - 1, blocks - 2]].view(torch.uint8), b.view(torch.uint8)) for a, b in
+               zip([x.view(torch.uint8) for x in far], near))
+    k2, v2 = torch.zeros_like(k), torch.zeros_like(v)
+    pa.cache_dequantize(*far, k2, v2, pairs=pairs.flip(1).contiguous())
+    k3, v3 = pa.cache_dequantize(*near, dtype=dtype)
+    assert torch.equal(k2, k3) and torch.equal(v2, v3)
