@@ -86,12 +86,13 @@ struct Raw {
 #pragma unroll
     for (int i = 0; i < kUnits<T, D>; ++i) u[i] = load_unit<STREAM>(p + at[i]);
   }
+  __device__ __forceinline__ float elem(int i) const {
+    const uint32_t w = u[i / kUnit<T>][i % kUnit<T> * (int)sizeof(T) / 4];
+    return __uint_as_float(sizeof(T) == 4 ? w : i % 2 ? w & 0xffff0000u : w << 16);
+  }
   __device__ __forceinline__ void get(float (&x)[kElems<D>]) const {
 #pragma unroll
-    for (int i = 0; i < kElems<D>; ++i) {
-      const uint32_t w = u[i / kUnit<T>][i % kUnit<T> * (int)sizeof(T) / 4];
-      x[i] = __uint_as_float(sizeof(T) == 4 ? w : i % 2 ? w & 0xffff0000u : w << 16);
-    }
+    for (int i = 0; i < kElems<D>; ++i) x[i] = elem(i);
   }
 };
 
@@ -122,6 +123,18 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 
+template <int CTRL>
+__device__ __forceinline__ double from_lane(double v) {
+  return __hiloint2double(__builtin_amdgcn_mov_dpp(__double2hiint(v), CTRL, 0xf, 0xf, true),
+                          __builtin_amdgcn_mov_dpp(__double2loint(v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ double group_sum(double v) {
+  v += from_lane<0xB1>(v);
+  v += from_lane<0x4E>(v);
+  v += from_lane<0x141>(v);
+  return v;
+}
+
 // The value of lane ^ 4: from four lanes on for the lower half of a group (banks
 // 0 and 2 of a row of 16 lanes), from four lanes back for the upper.
 __device__ __forceinline__ float other_half(float v) {
@@ -129,6 +142,10 @@ __device__ __forceinline__ float other_half(float v) {
   int r = __builtin_amdgcn_update_dpp(0, x, 0x104, 0xf, 0x5, false);
   r = __builtin_amdgcn_update_dpp(r, x, 0x114, 0xf, 0xa, false);
   return __int_as_float(r);
+}
+__device__ __forceinline__ double other_half(double v) {
+  return __hiloint2double(__float_as_int(other_half(__int_as_float(__double2hiint(v)))),
+                          __float_as_int(other_half(__int_as_float(__double2loint(v)))));
 }
 
 // Sine and cosine of `phase` turns / 2^32.
@@ -138,6 +155,23 @@ __device__ __forceinline__ void sincos_turns(uint32_t phase, float& s, float& c)
   const float y = x * x;
   const float sx = x + x * y * (-1.f / 6 + y * (1.f / 120 + y * (-1.f / 5040 + y * (1.f / 362880))));
   const float cx = 1.f + y * (-1.f / 2 + y * (1.f / 24 + y * (-1.f / 720 + y * (1.f / 40320 + y * (-1.f / 3628800)))));
+  s = quadrant & 1 ? cx : sx;
+  c = quadrant & 1 ? sx : cx;
+  if (quadrant & 2) s = -s;
+  if ((quadrant + 1) & 2) c = -c;
+}
+
+// The same in 64 bits, of 2^64, off by less than 2^-36: the last terms of the series are
+// 2^-14 and less and stay in fp32.
+__device__ __forceinline__ void sincos_turns(uint64_t phase, double& s, double& c) {
+  const uint32_t quadrant = (uint32_t)((phase + 0x2000000000000000ull) >> 62);
+  const double x = (double)(int64_t)(phase - ((uint64_t)quadrant << 62)) * 3.40612158008655459e-19;  // 2 pi / 2^64
+  const double y = x * x;
+  const float yf = (float)y;
+  const float s7 = -1.f / 5040 + yf * (1.f / 362880 + yf * (-1.f / 39916800));
+  const float c8 = 1.f / 40320 + yf * (-1.f / 3628800 + yf * (1.f / 479001600));
+  const double sx = fma(x * y, fma(y, fma(y, (double)s7, 1. / 120), -1. / 6), x);
+  const double cx = fma(y, fma(y, fma(y, fma(y, (double)c8, -1. / 720), 1. / 24), -0.5), 1.);
   s = quadrant & 1 ? cx : sx;
   c = quadrant & 1 ? sx : cx;
   if (quadrant & 2) s = -s;
@@ -191,11 +225,12 @@ struct Place {
 
 // Cosines and sines of a tile's rows: per row and two pairs of a lane, the lanes'
 // 16 bytes side by side.
-template <typename T, int D, bool PAIRS>
+template <typename T, int D, bool PAIRS, typename F = float>
 struct AngleTable {
   typedef Place<T, D, PAIRS> P;
-  f32x4 at[kGroups][P::kSlots * P::kPairsPerSlot / 2][P::kSlotLanes];
-  static_assert(sizeof(at) == kGroups * D * sizeof(float), "D / 2 pairs a row");
+  typedef F F4 __attribute__((ext_vector_type(4)));
+  F4 at[kGroups][P::kSlots * P::kPairsPerSlot / 2][P::kSlotLanes];
+  static_assert(sizeof(at) == kGroups * D * sizeof(F), "D / 2 pairs a row");
 
   // Fill rows [0, n): thread t takes pair t % (D / 2) of rows t / (D / 2), ...;
   // scaled, the sine negated for the inverse rotation.
@@ -206,10 +241,14 @@ struct AngleTable {
     const uint64_t turn = p.table.turn[pair];
     pos += p.table.axis[pair] * stride + row0;
     const int m = P::index_of(pair);
-    float* dst = reinterpret_cast<float*>(&at[0][m / 2][P::lane_of(pair)]) + m % 2 * 2;
+    F* dst = reinterpret_cast<F*>(&at[0][m / 2][P::lane_of(pair)]) + m % 2 * 2;
     for (int r = threadIdx.x / kPairs; r < n; r += kThreads / kPairs) {
-      float s, c;
-      sincos_turns((uint32_t)((uint64_t)(int64_t)pos[r] * turn >> 32), s, c);
+      F s, c;
+      const uint64_t phase = (uint64_t)(int64_t)pos[r] * turn;
+      if constexpr (sizeof(F) == 8)
+        sincos_turns(phase, s, c);
+      else
+        sincos_turns((uint32_t)(phase >> 32), s, c);
       dst[r * D] = c * p.scale;
       dst[r * D + 1] = p.inverse ? -s * p.scale : s * p.scale;
     }
@@ -257,17 +296,6 @@ __device__ __forceinline__ float rms_scale(const float (&x)[kElems<D>], float ep
 #pragma unroll
   for (int i = 0; i < kElems<D>; ++i) s += x[i] * x[i];
   return __builtin_amdgcn_rsqf(group_sum(s) * (1.f / D) + eps);
-}
-// With a Newton step: v_rsq_f32 is off by up to a unit in the last place, and in
-// bf16 that does not show, but a row's codes are compared one by one.  (Its error
-// is NaN where the mean is 0 or infinite, and the root is exact.)
-template <int D>
-__device__ __forceinline__ float rms_scale_exact(const float (&x)[kElems<D>], float eps) {
-  float s = 0.f;
-#pragma unroll
-  for (int i = 0; i < kElems<D>; ++i) s += x[i] * x[i];
-  const float v = group_sum(s) * (1.f / D) + eps, r = __builtin_amdgcn_rsqf(v), e = fmaf(-v * r, r, 1.f);
-  return e == e ? fmaf(0.5f * r, e, r) : r;
 }
 
 template <typename T>
@@ -329,7 +357,7 @@ struct Cursor {
 // Rows of a tile: norm, rotation, and `put(row, head, values)`.  The first
 // rows are asked for before the angles are computed, the others kAhead turns
 // before theirs.
-template <bool STREAM, bool EXACT = false, typename T, int D, bool PAIRS, class Put>
+template <bool STREAM, typename T, int D, bool PAIRS, class Put>
 __device__ __forceinline__ void turn_tile(const RotaryParams& p, const Tile& t, const int32_t* pos, int64_t pos_stride,
                                           AngleTable<T, D, PAIRS>& table, const Place<T, D, PAIRS>& pl, Put put) {
   constexpr int U = kAhead;
@@ -355,7 +383,7 @@ __device__ __forceinline__ void turn_tile(const RotaryParams& p, const Tile& t, 
       if (ahead.row < t.rows) raw[u].template load<STREAM>(ahead.at<const T>(t.in, t), pl.at);
       ahead.next(t, dr, dh);
       if (t.w) {
-        const float rho = EXACT ? rms_scale_exact<D>(x, p.eps) : rms_scale<D>(x, p.eps);
+        const float rho = rms_scale<D>(x, p.eps);
 #pragma unroll
         for (int i = 0; i < kElems<D>; ++i) x[i] *= rho * wt[i];
       }
@@ -650,6 +678,77 @@ __device__ __forceinline__ uint32_t quantize_row(const float (&x)[N], uint32_t (
   return b;
 }
 
+// z rounded to fp32 to odd: where fp32 does not hold it, towards zero with the last bit
+// set, so that a second rounding, to a code, and a comparison see it as they would z.
+__device__ __forceinline__ float round_to_odd(double z) {
+  const uint32_t lo = (uint32_t)__double2loint(z);
+  const uint32_t odd = (lo & 0x1fffffffu) ? 0x20000000u : 0u;
+  return (float)__hiloint2double(__double2hiint(z), (int)((lo & 0xe0000000u) | odd));
+}
+
+// A tile of K's rows for an 8-bit cache, normed and rotated in 64 bits, off by some
+// 2^-36: a code has four significant bits, and fp32's errors in z (1.2 units of 2^-24
+// of it, 1.9 with v_rsq_f32's own) would move a value in some 2^20 across the border
+// between two of them, which then differs by a sixteenth.  K has few of a call's rows,
+// and q's, which go past memory meanwhile, hide them (K in fp32: 41.7 us where this took 47.7).
+template <bool STREAM, typename T, int D, bool PAIRS, class Put>
+__device__ __forceinline__ void turn_tile_wide(const RotaryParams& p, const Tile& t, const int32_t* pos, int64_t pos_stride,
+                                               AngleTable<T, D, PAIRS, double>& table, const Place<T, D, PAIRS>& pl, Put put) {
+  typedef Place<T, D, PAIRS> P;
+  const int dr = kGroups / t.heads, dh = kGroups - dr * t.heads;
+  Cursor at(t, threadIdx.x / kLanes);
+  Raw<T, D> raw, rw{};
+  if (at.row < t.rows) raw.template load<STREAM>(at.at<const T>(t.in, t), pl.at);
+  if (t.w) rw.template load<false>(static_cast<const T*>(t.w), pl.at);
+  table.fill(p, pos, pos_stride, t.row0, t.rows);
+  __syncthreads();
+  while (at.row < t.rows) {
+    float x[kElems<D>];
+    raw.get(x);
+    const Cursor here = at;
+    at.next(t, dr, dh);
+    if (at.row < t.rows) raw.template load<STREAM>(at.at<const T>(t.in, t), pl.at);
+    double rho = 1.;
+    if (t.w) {
+      double s = 0.;
+#pragma unroll
+      for (int i = 0; i < kElems<D>; ++i) s += (double)x[i] * (double)x[i];
+      const double v = group_sum(s) * (1. / D) + (double)p.eps;
+      rho = __builtin_amdgcn_rsq(v);
+      const double e = fma(-v * rho, rho, 1.);  // (NaN where v is 0 or infinite: the root is exact)
+      rho = e == e ? fma(0.5 * rho, e, rho) : rho;
+    }
+    // (Else the compiler keeps every element and weight in 64 bits as well.)
+#pragma unroll
+    for (int i = 0; i < kElems<D>; ++i) asm("" : "+v"(x[i]));
+#pragma unroll
+    for (int i = 0; i < kUnits<T, D>; ++i) asm("" : "+v"(rw.u[i]));
+    auto normed = [&](int i) { return t.w ? (double)x[i] * (rho * (double)rw.elem(i)) : (double)x[i]; };
+#pragma unroll
+    for (int m0 = 0; m0 < P::kSlots * P::kPairsPerSlot; m0 += 2) {
+      const bool turned = m0 / P::kPairsPerSlot < pl.turned;
+      const auto cs = table.at[here.row][m0 / 2][threadIdx.x % P::kSlotLanes];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const double c = cs[2 * j], s = cs[2 * j + 1];
+        const int a = P::first(m0 + j), b = P::second(m0 + j) % kElems<D>;
+        const double ya = normed(a);
+        if (P::kSplit) {
+          const double yb = other_half(ya);
+          x[a] = round_to_odd(!turned ? ya : ya * c + yb * (threadIdx.x % kLanes < P::kSlotLanes ? -s : s));
+        } else {
+          const double yb = normed(b);
+          x[a] = round_to_odd(turned ? ya * c - yb * s : ya);
+          x[b] = round_to_odd(turned ? yb * c + ya * s : yb);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);  // (its values are done with before the next ones)
+    }
+    put(here, x);
+  }
+  __syncthreads();
+}
+
 // V's codes of one row and head, byte by byte (d-major V).
 template <typename T, int D, bool PAIRS>
 __device__ __forceinline__ void store_bytes(uint8_t* dst, const Place<T, D, PAIRS>& pl, const uint32_t (&codes)[kElems<D> / 4]) {
@@ -691,14 +790,18 @@ __device__ __forceinline__ void append_v_e4m3(const RotaryParams& p, const Place
     const bool ok = row >= 0 && row < p.n && slot_of(p, row, blk, slot);
     m.place[tid] = ok ? (int64_t)blk * kBlock + slot : -2;
   }
+  auto in = [&](int r) { return r < kRows && first + r < p.n; };  // (a group's lanes together)
+  Raw<T, D> raw[kTurns];
+#pragma unroll
+  for (int i = 0; i < kTurns; ++i)
+    if (in(i * kGroups + group)) raw[i].template load<STREAM>(head_row<T>(p.v, first + i * kGroups + group, h), pl.at);
 #pragma unroll
   for (int i = 0; i < kTurns; ++i) {
+    __builtin_amdgcn_sched_barrier(0);  // (a turn's values at a time)
     const int r = i * kGroups + group;
-    if (r >= kRows || first + r >= p.n) continue;  // (a group's lanes together)
-    Raw<T, D> raw;
-    raw.template load<STREAM>(head_row<T>(p.v, first + r, h), pl.at);
+    if (!in(r)) continue;
     float x[kElems<D>];
-    raw.get(x);
+    raw[i].get(x);
     uint32_t codes[kElems<D> / 4];
     const uint32_t scale = quantize_row(x, codes, 0);
     if (tid % kLanes == 0) m.tile[r * kStride + D] = (uint8_t)scale;
@@ -758,69 +861,73 @@ __device__ __forceinline__ void append_v_e4m3(const RotaryParams& p, const Place
 
 // Append into an 8-bit cache: items of four roles, as above.  ROWS == 0: v's
 // tiles are cut like k's, a group takes a row of one head, and its lanes leave a
-// byte per dimension (d-major V).  Bound by memory: 20,456 rows of 16 + 2 + 2 heads
-// of 128 in bf16, in 8 runs, take 41.5 us (4.81 TB/s; a copy reaches 5.1 to 5.3),
-// with V byte by byte 52.9, with three wavefronts a SIMD instead of four 43.5.
+// byte per dimension (d-major V).  A workgroup makes one item (a loop over items
+// would keep what one role needs in registers for the others: 128 of them and spills
+// where 96 do).  Bound by memory: 20,456 rows of 16 + 2 + 2 heads of 128 in bf16, in 8
+// runs, take 40.5 us (4.92 TB/s; a copy reaches 5.1 to 5.3), with the loop 47.7, with V
+// byte by byte some 11 more; 5,439 rows of 28 + 4 + 4 heads of 64 in fp32 16.3.
 template <typename T, int D, bool PAIRS, int ROWS, bool STREAM>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) void rotary_append_e4m3_kernel(const RotaryParams p) {
+__global__ __launch_bounds__(kThreads) void rotary_append_e4m3_kernel(const RotaryParams p) {
   __shared__ union Shared {
     AngleTable<T, D, PAIRS> table;
+    AngleTable<T, D, PAIRS, double> wide;
     VCodes<D, 64> v;
     __device__ Shared() {}
   } shared;
   constexpr int E = kUnit<T>;
   const Place<T, D, PAIRS> pl(p.pairs);
-  for (int64_t b = blockIdx.x; b < p.items; b += gridDim.x) {
-    if (b < p.items_v) {
-      if constexpr (ROWS > 0) {
-        append_v_e4m3<STREAM>(p, pl, b, shared.v);
-      } else {
-        Tile t = tile_of(p, b + p.tiles_q.items);  // (k's tile of the same rows and heads)
-        t.in = p.v;
-        const int dr = kGroups / t.heads, dh = kGroups - dr * t.heads;
-        for (Cursor c(t, threadIdx.x / kLanes); c.row < t.rows; c.next(t, dr, dh)) {
-          Raw<T, D> raw;
-          raw.template load<STREAM>(c.at<const T>(t.in, t), pl.at);
-          float x[kElems<D>];
-          raw.get(x);
-          uint32_t codes[kElems<D> / 4];
-          const uint32_t scale = quantize_row(x, codes, 0);
-          int32_t blk, slot;
-          if (!slot_of(p, t.row0 + c.row, blk, slot)) continue;
-          const int h = t.h0 + c.h;
-          uint8_t* dst = static_cast<uint8_t*>(p.v_cache) + e4m3::codes_at<D>(blk, h, p.Hkv) + slot;
-          store_bytes<T, D>(dst, pl, codes);
-          if (threadIdx.x % kLanes == 0) p.scales[e4m3::scales_at(blk, h, p.Hkv) + kBlock + slot] = (uint8_t)scale;
-        }
+  const int64_t b = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+  if (b >= p.items) return;
+  if (b < p.items_v) {
+    if constexpr (ROWS > 0) {
+      append_v_e4m3<STREAM>(p, pl, b, shared.v);
+    } else {
+      Tile t = tile_of(p, b + p.tiles_q.items);  // (k's tile of the same rows and heads)
+      t.in = p.v;
+      const int dr = kGroups / t.heads, dh = kGroups - dr * t.heads;
+      for (Cursor c(t, threadIdx.x / kLanes); c.row < t.rows; c.next(t, dr, dh)) {
+        Raw<T, D> raw;
+        raw.template load<STREAM>(c.at<const T>(t.in, t), pl.at);
+        float x[kElems<D>];
+        raw.get(x);
+        uint32_t codes[kElems<D> / 4];
+        const uint32_t scale = quantize_row(x, codes, 0);
+        int32_t blk, slot;
+        if (!slot_of(p, t.row0 + c.row, blk, slot)) continue;
+        const int h = t.h0 + c.h;
+        uint8_t* dst = static_cast<uint8_t*>(p.v_cache) + e4m3::codes_at<D>(blk, h, p.Hkv) + slot;
+        store_bytes<T, D>(dst, pl, codes);
+        if (threadIdx.x % kLanes == 0) p.scales[e4m3::scales_at(blk, h, p.Hkv) + kBlock + slot] = (uint8_t)scale;
       }
-      continue;
     }
-    const int64_t i = b - p.items_v, n_q = p.tiles_q.items, n_turned = n_q + p.tiles_k.items;
-    if (i >= n_turned) {
-      const int64_t e = (i - n_turned) * kThreads + threadIdx.x;
-      if (e < p.n_patch) p.block_table[p.patch[2 * e]] = p.patch[2 * e + 1];
-      continue;
-    }
-    const Tile t = tile_of(p, i);
-    const bool is_q = i < n_q;
-    turn_tile<STREAM, true>(p, t, is_q ? p.q_pos : p.pos, is_q ? p.q_pos_stride : p.pos_stride, shared.table, pl,
-              [&](const Cursor& c, const float (&x)[kElems<D>]) {
-      if (is_q) {
-        store_row(c.at<T>(t.out, t), pl.at, x);
-        return;
-      }
-      uint32_t codes[kElems<D> / 4];
-      const uint32_t scale = quantize_row(x, codes, e4m3::kNanCodes);
-      int32_t blk, slot;
-      if (!slot_of(p, t.row0 + c.row, blk, slot)) return;
-      const int h = t.h0 + c.h;
-      uint8_t* dst = static_cast<uint8_t*>(p.k_cache) + e4m3::codes_at<D>(blk, h, p.Hkv);
-#pragma unroll
-      for (int u = 0; u < kUnits<T, D>; ++u)
-        __builtin_memcpy(__builtin_assume_aligned(dst + e4m3::k_at(slot, pl.at[u]), E), &codes[u * E / 4], E);
-      if (threadIdx.x % kLanes == 0) p.scales[e4m3::scales_at(blk, h, p.Hkv) + slot] = (uint8_t)scale;
-    });
+    return;
   }
+  const int64_t i = b - p.items_v, n_q = p.tiles_q.items, n_turned = n_q + p.tiles_k.items;
+  if (i >= n_turned) {
+    const int64_t e = (i - n_turned) * kThreads + threadIdx.x;
+    if (e < p.n_patch) p.block_table[p.patch[2 * e]] = p.patch[2 * e + 1];
+    return;
+  }
+  // (k's tiles before q's: they wait longer for each row, and q's fill the time)
+  const Tile t = tile_of(p, i < n_turned - n_q ? i + n_q : i - (n_turned - n_q));
+  if (i >= n_turned - n_q) {
+    turn_tile<STREAM>(p, t, p.q_pos, p.q_pos_stride, shared.table, pl, [&](const Cursor& c, const float (&x)[kElems<D>]) {
+      store_row(c.at<T>(t.out, t), pl.at, x);
+    });
+    return;
+  }
+  turn_tile_wide<STREAM>(p, t, p.pos, p.pos_stride, shared.wide, pl, [&](const Cursor& c, const float (&x)[kElems<D>]) {
+    uint32_t codes[kElems<D> / 4];
+    const uint32_t scale = quantize_row(x, codes, e4m3::kNanCodes);
+    int32_t blk, slot;
+    if (!slot_of(p, t.row0 + c.row, blk, slot)) return;
+    const int h = t.h0 + c.h;
+    uint8_t* dst = static_cast<uint8_t*>(p.k_cache) + e4m3::codes_at<D>(blk, h, p.Hkv);
+#pragma unroll
+    for (int u = 0; u < kUnits<T, D>; ++u)
+      __builtin_memcpy(__builtin_assume_aligned(dst + e4m3::k_at(slot, pl.at[u]), E), &codes[u * E / 4], E);
+    if (threadIdx.x % kLanes == 0) p.scales[e4m3::scales_at(blk, h, p.Hkv) + slot] = (uint8_t)scale;
+  });
 }
 
 constexpr int64_t kMaxGrid = 1 << 20;  // workgroups of a launch: the rest by strides
@@ -988,7 +1095,7 @@ hipError_t launch_rotary_append_e4m3(RotaryParams p, int D, bool bf16, bool pair
   p.items_v = tall ? ceil_div(p.n, 64) * p.Hkv : p.tiles_k.items;
   p.items = p.items_v + p.tiles_q.items + p.tiles_k.items + ceil_div(p.n_patch, kThreads);
   if (p.items == 0) return hipSuccess;
-  const dim3 grid = grid_of(p.items);
+  const dim3 grid((unsigned)std::min(p.items, kMaxGrid), (unsigned)ceil_div(p.items, kMaxGrid));  // (an item a workgroup)
   if (!tall) return dispatch<AppendE4m3<0, false>::Call>(p, D, bf16, pairs, grid, s);
   return streams((int64_t)p.n_q * p.Hq * 2 + (int64_t)p.n * p.Hkv * 3, D, bf16)
              ? dispatch<AppendE4m3<64, true>::Call>(p, D, bf16, pairs, grid, s)

@@ -115,6 +115,27 @@ def test_rows_of_many_runs(dtype, d, hkv, n):
     check_rows(st, before, on_host(gpu), slots, k, v, pos, wk)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,rd,style,axes,norm", [(128, 128, "halves", 3, True), (64, 64, "halves", 3, True),
+                                                  (64, 32, "pairs", 1, True), (128, 96, "halves", 1, False)])
+def test_codes_of_k_are_those_of_64_bits(dtype, d, rd, style, axes, norm):
+    """K's codes and scales bit for bit: z is within some 2^-36 of its 64-bit value, and of 200 thousand values drawn
+    none lies that close to the border between two codes (a chance of 200,000 x 2^-36 / 2^-4 = 5e-5)."""
+    n, hkv = 800, 2
+    st = Setup(d, dtype, rotary_dim=rd, n_axes=axes, style=style, base=1e6, scale=1.25)
+    k, v = normal((n, hkv, d), 21, dtype, spread=3.0), normal((n, hkv, d), 22, dtype)
+    wk, pos = normal((d,), 23, dtype) if norm else None, positions(axes, n, 24, far=70000)
+    slots = places(n, 60, 25)
+    before = orc.empty(60, hkv, d, 26)
+    gpu = on_gpu(before)
+    print("[case] append e4m3 exact codes", dtype, d, rd, style, flush=True)
+    pa.rotary_append(None, k, v, pos, torch.from_numpy(slots).cuda(), *gpu[:2], st.handle, None, wk, scales=gpu[2])
+    want = [w.copy() for w in before]
+    orc.write(want, slots[:, 0], slots[:, 1], st.forward(k, pos, wk)[0], f64(v))
+    for name, a, w in zip(("k", "v", "scales"), on_host(gpu), want):
+        assert (a == w).all(), (name, (a != w).sum(), np.argwhere(a != w)[:4].tolist())
+
+
 @pytest.mark.parametrize("n", [40, 900])
 def test_blocks_behind_four_gigabytes(n):
     """Rows into blocks of a pool whose codes pass 2^32 bytes, byte by byte and by whole blocks: as into a small pool."""
