@@ -519,8 +519,9 @@ padoc_status padoc_cache_copy_blocks_e4m3(const padoc_cache_e4m3* src, const pad
                                           const int32_t* pairs, int64_t n_pairs, const int32_t* pairs_host,
                                           int32_t num_heads_kv, int32_t head_dim, hipStream_t stream);
 
-/* padoc_rotary_append into an 8-bit cache: rows in the rotary's dtype, normed and
-   rotated in fp32, each row of K and V rounded once, to its codes.  args->k_cache,
+/* padoc_rotary_append into an 8-bit cache: rows in the rotary's dtype, each row of K
+   and V rounded once, to its codes (K's rows are normed and rotated in 64 bits, so
+   that their codes are those of the exact values; q's in fp32).  args->k_cache,
    v_cache and num_blocks must be 0 (they are cache's). */
 padoc_status padoc_rotary_append_e4m3(const padoc_rotary* rotary, const padoc_rotary_append_args* args,
                                       const padoc_cache_e4m3* cache, hipStream_t stream);

@@ -12,9 +12,9 @@
 // Bound by HBM for the private keys (from half of the units 4.5 TB/s, from all 6.0)
 // and by the tile items' vector and matrix work for the shared ones.  64 pages (1,600
 // queries, 2,800 shared and 24 x up to 1,024 private keys a page, 511 MB): the kernel
-// 122 us, with the schedule's copy and the combine 132; private keys alone 86, shared
-// ones alone 114; on bf16 caches 190 and 199.  Where shared keys are all, the codes
-// save nothing (dense step, 128 queries on 9,098 keys: 104 us, bf16 103).
+// 122 us, with the schedule's copy and the combine 131; private keys alone 86, shared
+// ones alone 110; on bf16 caches 190 and 199.  Where shared keys are all, the codes
+// save nothing (dense step, 128 queries on 9,098 keys: 102 us, bf16 103).
 #include <type_traits>
 
 #include "device_common.hpp"

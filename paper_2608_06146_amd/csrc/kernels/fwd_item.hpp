@@ -344,11 +344,12 @@ __device__ __forceinline__ void fwd_item(const TileArgs<E4M3>& p, int item) {
   // `vb` of the tile.  From there they go into the stages as bf16: K of tile t+2
   // and V of tile t+1 in step t, between the products of its group B.  A code is
   // converted once an item and tile, not once a wavefront that multiplies it.
-  // Decode of 64 pages, 192 columns an item: 1.95 us a tile, on bf16 caches 1.67;
-  // 252 columns 2.5 and 2.3.  Codes in registers on their way, two tiles ahead, took
+  // Decode of 64 pages, 192 columns an item: 1.9 us a tile, on bf16 caches 1.67;
+  // 252 columns 2.45 and 2.3 (with the conversions in four lumps instead of twelve
+  // pieces 2 % more of a whole step).  Codes in registers on their way, two tiles ahead, took
   // as long, and spilled some.  What bounds a tile is what the two wavefronts of a
   // SIMD do one after the other, products and exponentials (matrix cores busy 0.31
-  // of the time, over the item's start and end too); the conversion is 0.2 to 0.3 us.
+  // of the time, over the item's start and end too); the conversion is 0.15 to 0.25 us.
   using e4m3::u32x4;
   constexpr bool kBoth = D == 128;  // every wavefront has codes of both
   const int vb = kBoth ? wave >> 1 : wave & 3, unit = kBoth ? tid & 127 : lane;
@@ -378,13 +379,19 @@ __device__ __forceinline__ void fwd_item(const TileArgs<E4M3>& p, int item) {
       sn = scale_bytes[tile % 4][wave][kBlock + (unit & 15)];
     }
   };
+  // Pieces of a thread's conversion: dims 4q .. 4q+3 of K (q < 4), tokens 2q, 2q+1 of
+  // V (q < 8); 16 bytes leave with every second (fourth) one.
+  u32x4 yk, yv;
   // (a token whose V row is NaN: its score is, where a column sees it)
-  auto place_k = [&](uint16_t* st, auto hc) {
-    constexpr int h = decltype(hc)::value;
+  auto place_k = [&](uint16_t* st, auto qc) {
+    constexpr int q = decltype(qc)::value;
     if constexpr (E4M3) {
-      const uint32_t lo = sn == e4m3::kNan ? e4m3::kNanCodes : xk[2 * h], hi = sn == e4m3::kNan ? e4m3::kNanCodes : xk[2 * h + 1];
-      *reinterpret_cast<bf16x8_t*>(st + k_row * D + 8 * ((2 * (unit >> 4) + h) ^ Gm::kswz(k_row))) =
-          e4m3::values8(lo, hi, e4m3::scale_value(sk));
+      const uint32_t x = sn == e4m3::kNan ? e4m3::kNanCodes : xk[q];
+      const float scale = e4m3::scale_value(sk);
+      yk[2 * (q % 2)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false));
+      yk[2 * (q % 2) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true));
+      if constexpr (q % 2 == 1)
+        *reinterpret_cast<u32x4*>(st + k_row * D + 8 * ((2 * (unit >> 4) + q / 2) ^ Gm::kswz(k_row))) = yk;
     }
   };
   // keep: tokens of the tile that exist.  The codes of the others are cleared (their
@@ -415,18 +422,14 @@ __device__ __forceinline__ void fwd_item(const TileArgs<E4M3>& p, int item) {
       }
     }
   };
-  auto place_v = [&](uint16_t* st, auto jc) {  // tokens 8j .. 8j+7
-    constexpr int j = decltype(jc)::value;
+  auto place_v = [&](uint16_t* st, auto qc) {
+    constexpr int q = decltype(qc)::value, i = q / 2, h = q % 2, j = q / 4;
     if constexpr (E4M3) {
-      typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-      u32x4 y;
-      static_for<4>([&](auto qc) {  // two tokens
-        constexpr int i = 2 * j + decltype(qc)::value / 2, h = decltype(qc)::value % 2;
-        const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(xv[i], e4m3::scale_value((sv[i] >> (16 * h)) & 255u), h);
-        const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(xv[i], e4m3::scale_value((sv[i] >> (16 * h + 8)) & 255u), h);
-        y[decltype(qc)::value] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060100u);
-      });
-      *reinterpret_cast<u32x4*>(st + (vb * D + unit) * kBlock + 8 * (j ^ ((unit >> 3) & 1))) = y;
+      const auto a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(xv[i], e4m3::scale_value((sv[i] >> (16 * h)) & 255u), h);
+      const auto b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(xv[i], e4m3::scale_value((sv[i] >> (16 * h + 8)) & 255u), h);
+      yv[q % 4] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060100u);
+      if constexpr (q % 4 == 3)
+        *reinterpret_cast<u32x4*>(st + (vb * D + unit) * kBlock + 8 * (j ^ ((unit >> 3) & 1))) = yv;
     }
   };
   // Step t's loads: the limits of tile t+3, codes of K of tile t+5 with its scales,
@@ -700,14 +703,14 @@ __device__ __forceinline__ void fwd_item(const TileArgs<E4M3>& p, int item) {
     asm volatile("" ::: "memory");
     if (has_k) {
       read_k(0, 0);
-      place_k(smem, I0{}), place_k(smem, I1{});
+      static_for<4>([&](auto q) { place_k(smem, q); });
       read_k(1, 1);
-      place_k(smem + SEL, I0{}), place_k(smem + SEL, I1{});
+      static_for<4>([&](auto q) { place_k(smem + SEL, q); });
     }
     if (has_v) {
       read_v(0, 0);
       trim_v(R0.n_keys);
-      place_v(smem + 4 * SEL, I0{}), place_v(smem + 4 * SEL, I1{});
+      static_for<8>([&](auto q) { place_v(smem + 4 * SEL, q); });
     }
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0xC07F);
@@ -748,13 +751,13 @@ __device__ __forceinline__ void fwd_item(const TileArgs<E4M3>& p, int item) {
         advance(C);
         if (has_k) {
           read_k(slot, t + 2);
-          place_k(smem + ((t + 2) % 4) * SEL, I0{}), place_k(smem + ((t + 2) % 4) * SEL, I1{});
+          static_for<4>([&](auto q) { place_k(smem + ((t + 2) % 4) * SEL, q); });
         }
         if (has_v) {
           read_v(before(slot), t + 1);
           trim_v(C.R.n_keys - C.kt * KT);
           uint16_t* st = smem + (4 + (t + 1) % 2) * SEL;
-          place_v(st, I0{}), place_v(st, I1{});
+          static_for<8>([&](auto q) { place_v(st, q); });
         }
         load_lim(Lk, Lb[(t + 3) % 4]);
         advance(Lk);
@@ -852,18 +855,20 @@ __device__ __forceinline__ void fwd_item(const TileArgs<E4M3>& p, int item) {
           if (has_k) read_k(slot, t + 2);
           next_id = ask_step(t);
         }
-        if constexpr (i == 2 * u || i == 2 * u + 1) {
-          if (has_k) place_k(ks, std::integral_constant<int, i - 2 * u>{});
+        // 128-wide heads: K's pieces with products 2 .. 5, V's with 7 .. 14; 64-wide:
+        // two of K's with 2 and 3, two of V's with 3 .. 6.
+        constexpr int kp = 4 / (2 * u), vp = 16 / NB, v0 = kBoth ? 7 : 3;
+        if constexpr (i >= 2 && i < 2 + 2 * u) {
+          if (has_k) static_for<kp>([&](auto c) { place_k(ks, std::integral_constant<int, (i - 2) * kp + decltype(c)::value>{}); });
         }
-        if constexpr (i == (kBoth ? 6 : 0)) {
+        if constexpr (i == (kBoth ? 4 : 0)) {
           if (has_v) read_v(before(slot), t + 1);
         }
-        if constexpr (i == (kBoth ? 9 : 2)) {
+        if constexpr (i == (kBoth ? 6 : 2)) {
           if (has_v) trim_v(C.R.n_keys - C.kt * KT);
         }
-        constexpr int v0 = kBoth ? 10 : 3, apart = kBoth ? 2 : 1;
-        if constexpr (i == v0 || i == v0 + apart) {
-          if (has_v) place_v(vst(Next{}), std::integral_constant<int, (i - v0) / apart>{});
+        if constexpr (i >= v0 && i < v0 + 8 / vp) {
+          if (has_v) static_for<vp>([&](auto c) { place_v(vst(Next{}), std::integral_constant<int, (i - v0) * vp + decltype(c)::value>{}); });
         }
         if constexpr (i == NB - 1) {
           load_lim(Lk, lst(std::integral_constant<int, SC + 3>{}));
