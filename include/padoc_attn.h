@@ -787,7 +787,8 @@ padoc_status padoc_session_resize(padoc_session* session, int64_t num_blocks, vo
    the first launch and again after every resize (which forgets them; a launch
    without scales returns PADOC_ERR_ARG).  Its launches take rows in the dtype's
    bf16 or fp32 and quantise them as padoc_rotary_append_e4m3 does.
-   PADOC_ERR_DTYPE for other sessions. */
+   PADOC_ERR_DTYPE for other sessions, PADOC_ERR_ARG for scales that lie in the
+   codes or in the block table; the scales named before stay then. */
 padoc_status padoc_session_set_scales(padoc_session* session, void* scales);
 
 /* The block copies of the prepared step, which padoc_session_launch makes

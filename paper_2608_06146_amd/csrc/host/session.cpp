@@ -382,8 +382,20 @@ extern "C" padoc_status padoc_session_set_scales(padoc_session* s, void* scales)
   if (st != PADOC_OK) return st;
   if (!padoc::is_e4m3(s->desc.dtype)) return set_error(PADOC_ERR_DTYPE, "the session's caches are not 8-bit caches");
   if ((uintptr_t)scales & 15) return set_error(PADOC_ERR_ARG, "scales must be 16-byte aligned");
-  if (scales && (scales == s->desc.k_cache || scales == s->desc.v_cache))
-    return set_error(PADOC_ERR_ARG, "scales and codes must be distinct buffers");
+  // (steps write all four)
+  const padoc_session_desc& d = s->desc;
+  const int64_t rows = d.num_blocks * d.num_heads_kv * kBlk;
+  const struct {
+    const char* name;
+    const void* p;
+    int64_t bytes;
+  } others[] = {{"k_cache", d.k_cache, rows * d.head_dim},
+                {"v_cache", d.v_cache, rows * d.head_dim},
+                {"block_table", d.block_table, d.block_table_capacity * 4}};
+  for (const auto& x : others)
+    if (scales && x.p && rows > 0 && (uintptr_t)scales < (uintptr_t)x.p + (uintptr_t)x.bytes &&
+        (uintptr_t)x.p < (uintptr_t)scales + (uintptr_t)(2 * rows))
+      return set_error(PADOC_ERR_ARG, "scales overlaps %s", x.name);
   s->scales = scales;
   return PADOC_OK;
 }
