@@ -1177,11 +1177,18 @@ class DecodeSession:
             if got != (num_blocks, self.num_heads_kv, self.head_dim):
                 raise ValueError(f"caches hold {got} blocks, heads and dimensions, expected "
                                  f"{(num_blocks, self.num_heads_kv, self.head_dim)}")
-        _lib.check(_lib.lib().padoc_session_resize(self.handle, int(num_blocks),
-                                                   None if k_cache is None else k_cache.data_ptr(),
-                                                   None if v_cache is None else v_cache.data_ptr()))
+        L = _lib.lib()
+
+        def pool(n, k, v):
+            return L.padoc_session_resize(self.handle, int(n), None if k is None else k.data_ptr(), None if v is None else v.data_ptr())
+        _lib.check(pool(num_blocks, k_cache, v_cache))
         if scales is not None:
-            _lib.check(_lib.lib().padoc_session_set_scales(self.handle, scales.data_ptr()))
+            try:
+                _lib.check(L.padoc_session_set_scales(self.handle, scales.data_ptr()))
+            except PadocError:  # (the session stays as it was)
+                pool(self.num_blocks, self.k_cache, self.v_cache)
+                L.padoc_session_set_scales(self.handle, self.scales.data_ptr())
+                raise
         self.k_cache, self.v_cache, self.scales, self.num_blocks = k_cache, v_cache, scales, int(num_blocks)
         self._users = set()
 

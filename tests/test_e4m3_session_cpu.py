@@ -3,8 +3,11 @@ import ctypes as C
 
 import numpy as np
 import pytest
+import torch
 
+import paper_2608_06146_amd as pa
 from paper_2608_06146_amd import _lib
+from _streams import Gpu
 
 A = 1 << 20
 BLOCKS, HKV, D, TABLE = 8, 2, 64, 64
@@ -51,3 +54,36 @@ def test_a_pool_of_no_blocks(session):
     assert L.padoc_session_resize(session, 0, A, 2 * A) == _lib.OK
     for at in (0, A, 3 * A + 16):  # (no scale is written)
         assert L.padoc_session_set_scales(session, at) == _lib.OK
+
+
+@pytest.mark.parametrize("blocks", [5, 9, 12])
+def test_a_refused_resize_leaves_the_session_as_it_was(monkeypatch, blocks):
+    real, seen = _lib.lib(), {}
+
+    def noted(name):
+        return lambda *a: seen.__setitem__(name, a[1:]) or getattr(real, name)(*a)
+    gpu = Gpu(monkeypatch, {n: noted(n) for n in ("padoc_session_resize", "padoc_session_set_scales")})
+
+    def caches(n):
+        f8 = torch.float8_e4m3fn
+        return (gpu.tensor(torch.zeros((n, 2, 4, 16, 16), dtype=f8)), gpu.tensor(torch.zeros((n, 2, 64, 16), dtype=f8)),
+                gpu.tensor(torch.zeros((n, 2, 2, 16), dtype=torch.float8_e8m0fnu)))
+    k, v, s = caches(9)
+    session = pa.DecodeSession(4, 2, 64, 9, "bf16_e4m3", k, v, gpu.tensor(torch.zeros(64, dtype=torch.int32)), scales=s)
+    session.open()
+    session.prepare([40], [1])  # three blocks
+    session.commit()
+    k2, v2, s2 = caches(blocks)
+    inside = v2.view(torch.uint8).view(-1)[:s2.numel()].view(s2.shape).view(s2.dtype)  # (of V's codes)
+    with pytest.raises(pa.PadocError, match="scales overlaps v_cache"):
+        session.resize(blocks, k2, v2, scales=gpu.tensor(inside))
+    assert seen == {"padoc_session_resize": (9, k.data_ptr(), v.data_ptr()), "padoc_session_set_scales": (s.data_ptr(),)}
+    assert session.num_blocks == 9 and session.k_cache is k and session.v_cache is v and session.scales is s
+    session.prepare([100], [1])  # nine blocks
+    session.commit()
+    session.truncate(0, 30)
+    session.resize(blocks, k2, v2, scales=s2)
+    assert seen["padoc_session_resize"][0] == blocks and seen["padoc_session_set_scales"] == (s2.data_ptr(),)
+    assert session.num_blocks == blocks and session.scales is s2
+    with pytest.raises(pa.PadocError, match="blocks"):
+        session.prepare([16 * blocks], [1])
