@@ -105,12 +105,23 @@ Caches caches(const at::Tensor& k, const at::Tensor& v, const Where& w) {
   return c;
 }
 
+// The type of scales, in a PyTorch that has it (in another no tensor is of
+// Undefined, and calls on 8-bit caches go to Python alone).
+template <typename Type>
+constexpr auto scale_type(int) -> decltype(Type::Float8_e8m0fnu) {
+  return Type::Float8_e8m0fnu;
+}
+template <typename Type>
+constexpr Type scale_type(...) {
+  return Type::Undefined;
+}
+
 // An 8-bit cache (written or read).
 Caches caches_e4m3(const at::Tensor& k, const at::Tensor& v, const at::Tensor& s, const Where& w, bool written,
                    padoc_cache_e4m3* out) {
   need(k.device() == w.device && v.device() == w.device && s.device() == w.device &&
        k.scalar_type() == at::kFloat8_e4m3fn && v.scalar_type() == at::kFloat8_e4m3fn &&
-       s.scalar_type() == at::kFloat8_e8m0fnu && k.is_contiguous() && v.is_contiguous() && s.is_contiguous() &&
+       s.scalar_type() == scale_type<at::ScalarType>(0) && k.is_contiguous() && v.is_contiguous() && s.is_contiguous() &&
        v.dim() == 4 && k.dim() == 5 && s.dim() == 4);
   const Caches c{v.size(0), v.size(1), v.size(2)};
   need(v.size(3) == 16 && k.size(0) == c.blocks && k.size(1) == c.heads && k.size(2) == c.d / 16 && c.d % 16 == 0 &&
