@@ -68,8 +68,6 @@ __device__ __forceinline__ int64_t scales_at(int64_t blk, int32_t kvh, int32_t H
 // Byte of dims [c, ..) of token t within a (block, head)'s K codes.
 __device__ __forceinline__ int k_at(int t, int c) { return (c >> 4) * (kBlock * 16) + t * 16 + (c & 15); }
 
-// Byte t (0..15) of 16.
-__device__ __forceinline__ uint32_t byte_of(const u32x4& u, int t) { return (u[t >> 2] >> (8 * (t & 3))) & 255u; }
 // Whether a byte of w is 255.
 __device__ __forceinline__ bool has_nan(uint32_t w) { return ((~w - 0x01010101u) & w & 0x80808080u) != 0; }
 
