@@ -520,9 +520,11 @@ padoc_status padoc_cache_copy_blocks_e4m3(const padoc_cache_e4m3* src, const pad
                                           int32_t num_heads_kv, int32_t head_dim, hipStream_t stream);
 
 /* padoc_rotary_append into an 8-bit cache: rows in the rotary's dtype, each row of K
-   and V rounded once, to its codes (K's rows are normed and rotated in 64 bits, so
-   that their codes are those of the exact values; q's in fp32).  args->k_cache,
-   v_cache and num_blocks must be 0 (they are cache's). */
+   and V rounded once, to its codes.  K's rows are normed and rotated in 64 bits: z is
+   off by at most about 2^-36 + 2 pi |pos| 2^-64 of scale (|y_a| + |y_b|) of its pair,
+   and its code is the exact value's unless that lies as close to the border between
+   two codes (it is a neighbour of it then).  q's rows: in fp32, as padoc_rotary_append.
+   args->k_cache, v_cache and num_blocks must be 0 (they are cache's). */
 padoc_status padoc_rotary_append_e4m3(const padoc_rotary* rotary, const padoc_rotary_append_args* args,
                                       const padoc_cache_e4m3* cache, hipStream_t stream);
 
@@ -586,6 +588,9 @@ padoc_status padoc_branch_decode_no_alloc(const padoc_plan* plan, const void* q,
    PADOC_F32_E4M3 (which serve no other call; other plans return PADOC_ERR_DTYPE
    here).  The attention is that of the values the codes stand for: matrix
    products of bf16 (the values are exact in it) or fp32 operands with fp32 sums.
+   With bf16 queries each probability is rounded to bf16 before its product with V,
+   as on bf16 caches (some of them after a multiplication by V's scale, a power of
+   two); row sums, and so LSE, add the unrounded ones.
    cache->num_blocks must be the plan's num_kv_rows. */
 padoc_status padoc_branch_decode_e4m3(const padoc_plan* plan, const void* q, const padoc_cache_e4m3* cache,
                                       const int32_t* block_table, void* o, float* lse, void* workspace,

@@ -6,14 +6,18 @@
 // Codes become bf16 values on their way into the matrix products (a code has
 // four significant bits, so that nothing is rounded).  K's scale goes into the
 // conversion; V's, one for each key, into the probabilities before they are
-// rounded to bf16 (private items) or into the conversion too (shared ones).  Row
-// sums add the probabilities before that rounding, in fp32.
+// rounded to bf16 (private items) or into the conversion too (shared ones).  That
+// rounding, 2^-8 of a probability at most, is the price of bf16 matrix products
+// (fp32 ones reach a tenth of their rate); with it O is off by 1.8e-3 (rms), by its own
+// last rounding alone 1.63e-3.  Row sums add the probabilities before that
+// rounding, in fp32.
 //
 // Bound by HBM for the private keys (from half of the units 4.5 TB/s, from all 6.0)
 // and by the tile items' vector and matrix work for the shared ones.  64 pages (1,600
 // queries, 2,800 shared and 24 x up to 1,024 private keys a page, 511 MB): the kernel
-// 122 us, with the schedule's copy and the combine 131; private keys alone 86, shared
-// ones alone 110; on bf16 caches 190 and 199.  Where shared keys are all, the codes
+// 122 us, with the schedule's copy and the combine 131; the kernel on private keys alone
+// (16 + 16 shared ones a page) 86, on shared ones alone (a private key a branch) 113 to
+// 115; on bf16 caches 190 and 199.  Where shared keys are all, the codes
 // save nothing (dense step, 128 queries on 9,098 keys: 102 us, bf16 103).
 #include <type_traits>
 
@@ -56,9 +60,9 @@ __device__ __forceinline__ u32x2 load_pair(const uint8_t* p) {  // four bytes, a
 // Fewer bytes in flight are better here: a read of 420 MB in random 2 KB pieces
 // took 62 us (6.5 TB/s) with 8 KB sets and 68 with 16 KB sets, two a wavefront,
 // eight wavefronts a unit; and one pipeline over all items of a wavefront, whose
-// loads never pause, took 5 us more than a pause between items (99.5 for 94.7,
-// private keys alone).  With half lines (tokens 0 .. 3 and 8 .. 11 in one load)
-// instead of whole ones: 106 for 95.
+// loads never pause, took 5 us more than a pause between items (99.5 for 94.7: calls
+// on a resident schedule, private keys alone, with 9 of combine).  With half lines
+// (tokens 0 .. 3 and 8 .. 11 in one load) instead of whole ones: 106 for 95.
 template <int D>
 __device__ __forceinline__ void wave_item(const TileParamsE4m3& p, int item, int lane) {
   constexpr int NP = D / 64;   // 16-dim pieces per lane and token

@@ -161,7 +161,8 @@ __device__ __forceinline__ void sincos_turns(uint32_t phase, float& s, float& c)
   if ((quadrant + 1) & 2) c = -c;
 }
 
-// The same in 64 bits, of 2^64, off by less than 2^-36: the last terms of the series are
+// The same in 64 bits, of 2^64, off by less than 2^-36 (of this phase's: a turn's
+// own rounding, below 2^-64, goes times the position): the last terms of the series are
 // 2^-14 and less and stay in fp32.
 __device__ __forceinline__ void sincos_turns(uint64_t phase, double& s, double& c) {
   const uint32_t quadrant = (uint32_t)((phase + 0x2000000000000000ull) >> 62);
@@ -687,9 +688,11 @@ __device__ __forceinline__ float round_to_odd(double z) {
 }
 
 // A tile of K's rows for an 8-bit cache, normed and rotated in 64 bits, off by some
-// 2^-36: a code has four significant bits, and fp32's errors in z (1.2 units of 2^-24
+// 2^-36 + 2 pi |pos| 2^-64 of scale (|y_a| + |y_b|) of a pair (up to position 2^25 the first
+// is the larger): a code has four significant bits, and fp32's errors in z (1.2 units of 2^-24
 // of it, 1.9 with v_rsq_f32's own) would move a value in some 2^20 across the border
-// between two of them, which then differs by a sixteenth.  K has few of a call's rows,
+// between two of them, which then differs by a sixteenth; so is one in some 2^32, or in
+// 2^26 at the farthest positions.  K has few of a call's rows,
 // and q's, which go past memory meanwhile, hide them (K in fp32: 41.7 us where this took 47.7).
 template <bool STREAM, typename T, int D, bool PAIRS, class Put>
 __device__ __forceinline__ void turn_tile_wide(const RotaryParams& p, const Tile& t, const int32_t* pos, int64_t pos_stride,
@@ -1081,7 +1084,9 @@ hipError_t launch_rotary_append(RotaryParams p, int D, bool bf16, bool pairs, hi
 }
 
 // Rows (of all heads) from which V's go in tiles of 64 rows.  As above, the
-// count decides.  Measured without queries, us a call byte by byte and in tiles, in
+// count decides, as the kernel does not know scattered rows (a token a stream) from runs
+// before it has read the slots: above the threshold scattered ones lose 1.3 to 2.0 us by it,
+// runs win 0.6 to 3.5.  Measured without queries, us a call byte by byte and in tiles, in
 // runs and scattered: 2 heads of 128 in bf16, 2,400 rows 6.7 and 6.2, 9.4 and 11.2;
 // 3,200 rows 6.7 and 6.1, 10.6 and 12.6; 6,400 rows 9.1 and 6.3, 15.4 and 16.7; 8 heads,
 // 400 rows 6.2 and 6.2, 6.9 and 10.2; 800 rows 9.6 and 6.1, 10.3 and 12.2; 4 heads of
